@@ -344,6 +344,33 @@ int qg_int8_linear_t_zp_backward(const uint16_t* dy_bf16, const uint16_t* x_bf16
                                  const float* Sz, int64_t tokens, int64_t m, int64_t n, int group,
                                  uint16_t* dx_bf16, uint16_t* GS_bf16, void* stream);
 
+/* ---- Residual stream between two blocks of a decoder: the norm behind a block, its gate and residual scale, the sum,
+ * and the norm ahead of the next block, in one pass.  For each of `tokens` rows of d elements, rms(v) = sqrt(mean v^2 + eps):
+ *     n  = w_post * y / rms(y)            y: the block's output, bf16; w_post NULL: n = y
+ *     h' = h + scale * gate * n           gate_kind: none (1), fp32 [d], or bf16 [tokens][ld]
+ *     u  = w_pre * h' / rms(h')           bf16; from h' as it is before it is rounded to the stream's type
+ * h and h' (h_out) are bf16, or fp32 with stream_fp32 != 0.  y NULL: h' = h, h_out is not written (a norm alone).
+ * u NULL: not computed.  h_out may be h.  w_post, w_pre: fp32 [d].
+ *
+ * qg_residual_norm_backward: the gradients at h_next = h' as stored, given du and dh_next (the stream's own gradient at
+ * h', in the stream's type; either may be NULL: 0): dh of h and, in the sum, of h' alike (may be dh_next), dy (bf16),
+ * dw_pre, dw_post (fp32 [d]) and dgate (fp32 [d], or bf16 [tokens][ld]); dw_pre, dw_post and dgate are each optional.  y
+ * NULL: no block output, only dh and dw_pre.  rms is computed again from h_next and y.  Sums over tokens are added in a
+ * fixed order.  workspace: qg_residual_norm_workspace_bytes(tokens, d) bytes, 16-byte aligned; may be NULL / 0 if none of
+ * dw_pre, dw_post and a channel's dgate is asked for.
+ *
+ * tokens below 2^22, 1 <= d <= 16384.  ld: row pitch of every [tokens][d] array: d (or 0), or more and a multiple of 16;
+ * padding is neither read nor written. */
+enum { QG_GATE_NONE = 0, QG_GATE_CHANNEL = 1, QG_GATE_TOKEN = 2 };
+int qg_residual_norm_forward(const void* h, const uint16_t* y_bf16, const float* w_post, const void* gate, int gate_kind,
+                             const float* w_pre, float scale, float eps, int64_t tokens, int64_t d, int64_t ld, int stream_fp32,
+                             void* h_out, uint16_t* u_bf16, void* stream);
+size_t qg_residual_norm_workspace_bytes(int64_t tokens, int64_t d);
+int qg_residual_norm_backward(const uint16_t* du_bf16, const void* dh_next, const void* h_next, const uint16_t* y_bf16,
+                              const float* w_post, const void* gate, int gate_kind, const float* w_pre, float scale, float eps,
+                              int64_t tokens, int64_t d, int64_t ld, int stream_fp32, void* dh, uint16_t* dy_bf16,
+                              float* dw_pre, float* dw_post, void* dgate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Adaptive lazy update policy (Sec. 3.2), HOST ONLY (p is a host pointer):
  * streak counts consecutive checks with cos >= threshold; at k in a row the
  * interval doubles and the streak restarts; next_refresh advances by the

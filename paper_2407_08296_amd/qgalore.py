@@ -34,6 +34,7 @@ EXPORTS = [
     "qg_state8_quant", "qg_state8_dequant", "qg_lowrank_adam8", "qg_step8",
     "qg_subspace_cossim_static", "qg_subspace_cossim_weighted", "qg_step_ld", "qg_subspace_refresh_many_ld",
     "qg_int8_linear_forward_ld", "qg_int8_linear_backward_ld",
+    "qg_residual_norm_forward", "qg_residual_norm_workspace_bytes", "qg_residual_norm_backward",
 ]
 
 
@@ -139,6 +140,11 @@ def lib() -> C.CDLL:
         L.qg_subspace_refresh_many.argtypes = [i32, C.POINTER(RefreshDesc), i64, i64, i64, i32, i32, vp, vp, vp, sz, vp]
         L.qg_subspace_refresh_many_ld.argtypes = [i32, C.POINTER(RefreshDesc), i64, i64, i64, i64, i32, i32, vp, vp, vp, sz,
                                                   vp]
+        L.qg_residual_norm_forward.argtypes = [vp, vp, vp, vp, i32, vp, f32, f32, i64, i64, i64, i32, vp, vp, vp]
+        L.qg_residual_norm_workspace_bytes.restype = sz
+        L.qg_residual_norm_workspace_bytes.argtypes = [i64, i64]
+        L.qg_residual_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, f32, f32, i64, i64, i64, i32, vp, vp, vp, vp, vp,
+                                                vp, sz, vp]
         _lib = L
     return _lib
 
@@ -178,6 +184,12 @@ def _bf16_rows(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
     if like.dtype is torch.bfloat16 and type(like) is torch.Tensor:
         return like.new_empty(rows, cols)
     return torch.empty(rows, cols, dtype=torch.bfloat16, device=like.device)
+
+
+def _expect(t: torch.Tensor | None, *shape: int) -> None:
+    """Refuses a tensor of another shape than the sizes handed to the library say: its kernels would read past the end."""
+    if t is not None and tuple(t.shape) != shape:
+        raise QGError(f"shape {tuple(t.shape)}, expected {shape}")
 
 
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, lr=1e-3, alpha=0.25) -> HParams:
@@ -511,6 +523,79 @@ def int8_linear_t_backward(dy: torch.Tensor, x: torch.Tensor | None, Sq: torch.T
     _check(lib().qg_int8_linear_t_backward(_ptr(dy, _BF16), _ptr(x, _BF16), _ptr(Sq, (torch.int8,)),
                                            _ptr(Ss, (torch.float32,)), tokens, m, n, GROUP, _ptr(dx), _ptr(G), _stream()))
     return dx, G
+
+
+# ---------------------------------------------------------------- residual stream
+_F32 = (torch.float32,)
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
+
+
+def _gate(gate: torch.Tensor | None, tokens: int, d: int):
+    """(pointer, kind) of a gate: None, fp32 [d] or bf16 [tokens][d]."""
+    if gate is None:
+        return None, GATE_NONE
+    if gate.dim() == 1:
+        _expect(gate, d)
+        return _ptr(gate, _F32), GATE_CHANNEL
+    _expect(gate, tokens, d)
+    return _ptr(gate, _BF16), GATE_TOKEN
+
+
+def _stream_type(h: torch.Tensor):
+    if h.dtype is torch.float32:
+        return _F32, 1
+    return _BF16, 0
+
+
+def residual_norm_forward(h: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
+                          gate: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, scale: float = 1.0,
+                          eps: float = 1e-6, out: torch.Tensor | None = None):
+    """Returns (h', u): h' = h + scale * gate * norm(y; w_post), u = norm(h'; w_pre).  h: bf16 or fp32 [tokens][d], gate: None, fp32
+    [d] or bf16 [tokens][d].  Without y, h' is h itself; without w_pre, u is None.  out: where h' is written (h itself: in place)."""
+    tokens, d = h.shape
+    stype, fp32 = _stream_type(h)
+    for v in (w_post, w_pre):
+        _expect(v, d)
+    _expect(y, tokens, d)
+    g, kind = _gate(gate if y is not None else None, tokens, d)
+    if out is None and y is not None:
+        out = torch.empty_like(h)
+    elif y is None:
+        out = None
+    _expect(out, tokens, d)
+    u = torch.empty(tokens, d, dtype=torch.bfloat16, device=h.device) if w_pre is not None else None
+    _check(lib().qg_residual_norm_forward(_ptr(h, stype), _ptr(y, _BF16), _ptr(w_post, _F32), g, kind, _ptr(w_pre, _F32), scale, eps,
+                                          tokens, d, d, fp32, _ptr(out, (h.dtype,)), _ptr(u), _stream()))
+    return (h if out is None else out), u
+
+
+def residual_norm_backward(du: torch.Tensor | None, dh_next: torch.Tensor | None, h_next: torch.Tensor, y: torch.Tensor | None = None,
+                           w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None, w_pre: torch.Tensor | None = None,
+                           scale: float = 1.0, eps: float = 1e-6, out: torch.Tensor | None = None):
+    """Returns (dh, dy, dw_pre, dw_post, dgate), None for what has no input: the gradients of residual_norm_forward at its h' =
+    h_next, from du and the stream's gradient dh_next (either may be None).  out: where dh is written (dh_next itself: in place)."""
+    tokens, d = h_next.shape
+    stype, fp32 = _stream_type(h_next)
+    for v in (w_post, w_pre):
+        _expect(v, d)
+    for v in (du, dh_next, y, out):
+        _expect(v, tokens, d)
+    if y is None:
+        w_post = gate = None
+    g, kind = _gate(gate, tokens, d)
+    dev = h_next.device
+    dh = torch.empty_like(h_next) if out is None else out
+    dy = torch.empty(tokens, d, dtype=torch.bfloat16, device=dev) if y is not None else None
+    dw_pre = torch.empty(d, dtype=torch.float32, device=dev) if du is not None else None
+    dw_post = torch.empty(d, dtype=torch.float32, device=dev) if w_post is not None else None
+    dgate = torch.empty_like(gate) if gate is not None else None
+    nbytes = lib().qg_residual_norm_workspace_bytes(tokens, d)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _check(lib().qg_residual_norm_backward(_ptr(du, _BF16), _ptr(dh_next, stype), _ptr(h_next, stype), _ptr(y, _BF16),
+                                           _ptr(w_post, _F32), g, kind, _ptr(w_pre, _F32), scale, eps, tokens, d, d, fp32,
+                                           _ptr(dh, stype), _ptr(dy), _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), _ptr(ws), nbytes,
+                                           _stream()))
+    return dh, dy, dw_pre, dw_post, dgate
 
 
 # ---------------------------------------------------------------- subspace refresh

@@ -1,0 +1,236 @@
+"""The residual stream's norms against the fp64 reference (oracle/layers.py), on the same decoded inputs.
+
+Bars.  bf16 outputs are rounded once from fp32: every element within half a bf16 spacing (2^-8 of it at most) plus the fp32 noise of
+its terms.  fp32 outputs per element: a few roundings (2^-24 each) of the terms they are sums of.  Sums over tokens: T terms, added in
+fp32, within T 2^-24 of the sum of their magnitudes in the worst case; the bar is 8 (1 + sqrt T) 2^-24 of it (the error of such sums
+grows with the root of their length; a wrong or lost term is orders of magnitude above it)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers as O
+from paper_2407_08296_amd import qgalore as qg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U24, EPS = 2.0 ** -24, 1e-6
+
+# (tokens, d): one token, one element, around the widths that the kernels change at, odd ones, several rows per workgroup
+SHAPES = [(1, 1), (1, 7), (5, 8), (3, 100), (130, 513), (2, 512), (67, 1023), (1, 1024), (6, 1025), (9, 2047), (1, 2048), (3, 2049),
+          (2, 4096), (1100, 4100), (3, 8192), (2, 8193), (1, 16384), (2100, 96), (513, 2048)]
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def inputs(tokens, d, fp32, gate, seed=0, amp=1.0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s, std=1.0, mean=0.0: torch.randn(*s, generator=g) * std + mean
+    stream = torch.float32 if fp32 else torch.bfloat16
+    s = dict(h=(amp * r(tokens, d, std=2)).to(stream), y=(amp * r(tokens, d)).bfloat16(), w_post=r(d, std=0.1, mean=1), w_pre=r(d, std=0.1, mean=1),
+             gate={None: None, "channel": r(d), "token": r(tokens, d).bfloat16()}[gate], du=r(tokens, d, std=1e-3).bfloat16(),
+             dh=r(tokens, d, std=1e-3).to(stream))
+    return {k: None if v is None else v.to(DEV) for k, v in s.items()}
+
+
+def check(got, want, noise):
+    """noise: magnitude of the fp32 terms of each element."""
+    err = np.abs(f64(got) - want)
+    bar = 16 * U24 * noise + (2.0 ** -8 * np.abs(want) if got.dtype is torch.bfloat16 else 0.0)
+    assert got.shape == want.shape and np.all(err <= bar), float(np.max(err - bar))
+
+
+def check_sum(got, terms):
+    """got: the fp32 sum over the first axis of `terms`."""
+    bar = 8 * (1 + np.sqrt(len(terms))) * U24 * np.abs(terms).sum(0)
+    assert np.all(np.abs(f64(got) - terms.sum(0)) <= bar)
+
+
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("gate", [None, "channel", "token"])
+@pytest.mark.parametrize("tokens,d", SHAPES)
+def test_forward(tokens, d, gate, fp32):
+    s = inputs(tokens, d, fp32, gate)
+    h, u = qg.residual_norm_forward(s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"], scale=0.7, eps=EPS)
+    f = {k: f64(v) for k, v in s.items()}
+    wh, wu = O.residual_norm_forward(f["h"], f["y"], f["w_post"], f["gate"], f["w_pre"], 0.7, EPS)
+    check(h, wh, np.abs(f["h"]) + np.abs(wh - f["h"]))
+    check(u, wu, np.abs(wu) + np.abs(wu / np.where(wh == 0, 1, wh)) * (np.abs(f["h"]) + np.abs(wh - f["h"])))
+
+
+def sums_noise(f, d):
+    """Magnitudes of the terms of dh and dy, the sums over a row taken over magnitudes (mean over d of products)."""
+    r = 1 / np.sqrt(np.mean(f["h"] ** 2, axis=1, keepdims=True) + EPS)
+    a = np.abs(f["w_pre"] * f["du"])
+    dh = np.abs(f["dh"]) + r * (a + np.abs(f["h"]) * r * r * np.mean(a * np.abs(f["h"]), axis=1, keepdims=True))
+    q = 1 / np.sqrt(np.mean(f["y"] ** 2, axis=1, keepdims=True) + EPS)
+    b = np.abs(f["w_post"] * 0.7 * (1.0 if f["gate"] is None else f["gate"])) * dh
+    return dh, q * (b + np.abs(f["y"]) * q * q * np.mean(b * np.abs(f["y"]), axis=1, keepdims=True)), q
+
+
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("gate", [None, "channel", "token"])
+@pytest.mark.parametrize("tokens,d", SHAPES)
+def test_backward(tokens, d, gate, fp32):
+    s = inputs(tokens, d, fp32, gate, seed=1)
+    dh, dy, dw_pre, dw_post, dgate = qg.residual_norm_backward(s["du"], s["dh"], s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"],
+                                                               scale=0.7, eps=EPS)
+    f = {k: f64(v) for k, v in s.items()}
+    want = O.residual_norm_backward(f["du"], f["dh"], f["h"], f["y"], f["w_post"], f["gate"], f["w_pre"], 0.7, EPS)
+    mh, my, q = sums_noise(f, d)
+    check(dh, want[0], mh)
+    check(dy, want[1], my)
+    r = 1 / np.sqrt(np.mean(f["h"] ** 2, axis=1, keepdims=True) + EPS)
+    check_sum(dw_pre, f["du"] * f["h"] * r)
+    gv = 1.0 if f["gate"] is None else f["gate"]
+    # the terms of dw_post and of a channel's dgate are products with dh, which is itself a sum: its terms' magnitude counts
+    bar = 8 * (1 + np.sqrt(tokens)) * U24 * np.sum(0.7 * np.abs(gv * f["y"]) * q * mh, axis=0)
+    assert np.all(np.abs(f64(dw_post) - want[3]) <= bar)
+    if gate is None:
+        assert dgate is None
+    elif gate == "channel":
+        bar = 8 * (1 + np.sqrt(tokens)) * U24 * np.sum(0.7 * np.abs(f["w_post"] * f["y"]) * q * mh, axis=0)
+        assert np.all(np.abs(f64(dgate) - want[4]) <= bar)
+    else:
+        check(dgate, want[4], 0.7 * np.abs(f["w_post"] * f["y"]) * q * mh)
+
+
+@pytest.mark.parametrize("tokens,d", [(3, 7), (37, 768), (5, 2047)])
+def test_parts_alone(tokens, d):
+    """A norm alone; no norm behind the block; no norm ahead; gradients from one side only; in place."""
+    s = inputs(tokens, d, True, "channel", seed=2)
+    f = {k: f64(v) for k, v in s.items()}
+    h, u = qg.residual_norm_forward(s["h"], w_pre=s["w_pre"], eps=EPS)
+    assert h is s["h"]
+    wu = O.residual_norm_forward(f["h"], w_pre=f["w_pre"], eps=EPS)[1]
+    check(u, wu, np.abs(wu))
+    h, u = qg.residual_norm_forward(s["h"], s["y"], None, s["gate"], scale=0.5)
+    wh = O.residual_norm_forward(f["h"], f["y"], None, f["gate"], scale=0.5)[0]
+    assert u is None
+    check(h, wh, np.abs(f["h"]) + np.abs(wh - f["h"]))
+    mine = s["h"].clone()
+    same, _ = qg.residual_norm_forward(mine, s["y"], None, s["gate"], scale=0.5, out=mine)
+    assert same is mine and torch.equal(mine, h)
+    # a norm alone, backward
+    dh, dy, dw_pre, dw_post, dgate = qg.residual_norm_backward(s["du"], None, s["h"], w_pre=s["w_pre"], eps=EPS)
+    want = O.residual_norm_backward(f["du"], None, f["h"], w_pre=f["w_pre"], eps=EPS)
+    zero = dict(f, dh=0 * f["h"])
+    check(dh, want[0], sums_noise(zero, d)[0])
+    assert dy is None and dw_post is None and dgate is None
+    # only the stream's gradient, no norm behind the block
+    dh, dy, dw_pre, dw_post, dgate = qg.residual_norm_backward(None, s["dh"], s["h"], s["y"], None, s["gate"], scale=0.5)
+    want = O.residual_norm_backward(None, f["dh"], f["h"], f["y"], None, f["gate"], scale=0.5)
+    assert torch.equal(dh, s["dh"]) and dw_pre is None and dw_post is None
+    check(dy, want[1], np.abs(want[1]))
+    check_sum(dgate, 0.5 * f["dh"] * f["y"])
+    # in place
+    mine = s["dh"].clone()
+    a = qg.residual_norm_backward(s["du"], s["dh"], s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"])
+    b = qg.residual_norm_backward(s["du"], mine, s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"], out=mine)
+    assert b[0] is mine and all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("d", [96, 2047, 4096])
+def test_zero_rows_large_values_and_what_is_not_finite(d):
+    s = inputs(4, d, True, None, seed=3, amp=1e15)
+    s["h"][0] = 0
+    s["y"][0] = 0
+    s["h"][3, d // 2] = float("inf")
+    h, u = qg.residual_norm_forward(s["h"], s["y"], s["w_post"], None, s["w_pre"], eps=EPS)
+    assert not h[0].any() and not u[0].any()                 # 0 / sqrt(eps)
+    f = {k: f64(v)[:3] if k in ("h", "y") else f64(v) for k, v in s.items()}
+    wh, wu = O.residual_norm_forward(f["h"], f["y"], f["w_post"], None, f["w_pre"], 1.0, EPS)
+    check(h[:3], wh, np.abs(f["h"]) + np.abs(wh - f["h"]))
+    check(u[:3], wu, 2 * np.abs(wu) + 1e-9)
+    assert torch.isinf(h[3, d // 2]) and torch.isnan(u[3, d // 2])     # inf / inf, in its own row only
+
+
+def test_row_pitch_and_padding():
+    """The C entry points on padded rows: the same results, padding neither read nor written."""
+    tokens, d, ld = 70, 2047, 2064
+    s = inputs(tokens, d, False, "token", seed=4)
+    want_h, want_u = qg.residual_norm_forward(s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"], scale=0.7, eps=EPS)
+    want = qg.residual_norm_backward(s["du"], s["dh"], s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"], scale=0.7, eps=EPS)
+
+    def pad(t):
+        p = torch.full((tokens, ld), float("nan"), dtype=t.dtype, device=DEV)
+        p[:, :d] = t
+        return p
+    p = {k: pad(s[k]) for k in ("h", "y", "gate", "du", "dh")}
+    h, u, dh, dy, dgate = (torch.full((tokens, ld), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(5))
+    dw_pre, dw_post = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    L, at = qg.lib(), lambda t: t.data_ptr()
+    nbytes = L.qg_residual_norm_workspace_bytes(tokens, d)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    st = torch.cuda.current_stream().cuda_stream
+    assert L.qg_residual_norm_forward(at(p["h"]), at(p["y"]), at(s["w_post"]), at(p["gate"]), 2, at(s["w_pre"]), 0.7, EPS, tokens, d, ld,
+                                      0, at(h), at(u), st) == 0
+    assert L.qg_residual_norm_backward(at(p["du"]), at(p["dh"]), at(p["h"]), at(p["y"]), at(s["w_post"]), at(p["gate"]), 2, at(s["w_pre"]),
+                                       0.7, EPS, tokens, d, ld, 0, at(dh), at(dy), at(dw_pre), at(dw_post), at(dgate), at(ws), nbytes,
+                                       st) == 0
+    for got, ref in [(h, want_h), (u, want_u), (dh, want[0]), (dy, want[1]), (dgate, want[4])]:
+        assert torch.equal(got[:, :d], ref) and bool((got[:, d:] == 7).all())
+    assert torch.equal(dw_pre, want[2]) and torch.equal(dw_post, want[3])
+
+
+def test_gradient_against_differences_of_the_forward_kernel():
+    """A fp32 stream, so that the forward pass resolves a step: sum(c h') along a random direction of h and of the vectors."""
+    tokens, d = 6, 768
+    s = inputs(tokens, d, True, "channel", seed=5)
+    c = s["dh"].double() * 1e3
+
+    def f(**kw):
+        v = dict(s, **kw)
+        return float((c * qg.residual_norm_forward(v["h"], v["y"], v["w_post"], v["gate"], scale=0.7)[0].double()).sum())
+    g = qg.residual_norm_backward(None, c.float(), s["h"], s["y"], s["w_post"], s["gate"], scale=0.7)
+    for name, grad in (("h", g[0]), ("w_post", g[3]), ("gate", g[4])):
+        e = torch.randn(s[name].shape, generator=torch.Generator().manual_seed(6)).to(DEV)
+        step = 1.0 / 64       # h' is linear in each of these: no truncation error, only roundings of about 2^-24 |h'| per element
+        diff = (f(**{name: s[name] + step * e}) - f(**{name: s[name] - step * e})) / (2 * step)
+        want = float((grad.double() * e.double()).sum())
+        noise = 4 * U24 * float((c * 8).norm()) / step
+        assert abs(diff - want) <= noise + 1e-5 * float((grad.double() * e.double()).abs().sum())
+
+
+def test_refusals():
+    s = inputs(4, 64, False, "channel")
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"], s["y"][:3], s["w_post"], None, s["w_pre"])       # another number of tokens
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"], s["y"], s["w_post"][:32], None, s["w_pre"])
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"], s["y"].float(), s["w_post"], None, s["w_pre"])   # type
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"].t(), w_pre=s["w_pre"])                            # strided
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"])                                                  # nothing to compute
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_backward(None, None, s["h"], s["y"])
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_backward(s["du"], None, s["h"])                                  # du without w_pre
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(torch.zeros(0, 64, dtype=torch.bfloat16, device=DEV), w_pre=s["w_pre"])
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(torch.zeros(1, 16385, dtype=torch.bfloat16, device=DEV), w_pre=torch.ones(16385, device=DEV))
+
+
+def test_another_stream_and_capture():
+    s = inputs(300, 2048, False, "channel", seed=8)
+    args = (s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"])
+    want = qg.residual_norm_forward(*args) + qg.residual_norm_backward(s["du"], s["dh"], *args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = qg.residual_norm_forward(*args) + qg.residual_norm_backward(s["du"], s["dh"], *args)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = qg.residual_norm_forward(*args) + qg.residual_norm_backward(s["du"], s["dh"], *args)
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
