@@ -371,6 +371,54 @@ int qg_residual_norm_backward(const uint16_t* du_bf16, const void* dh_next, cons
                               int64_t tokens, int64_t d, int64_t ld, int stream_fp32, void* dh, uint16_t* dy_bf16,
                               float* dw_pre, float* dw_post, void* dgate, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- INT8 linear layer with an epilogue, and the gated pair of a feed-forward block.  Weights, dequantization, pitches and
+ * limits as for qg_int8_linear_forward_ld (ld_n: x, dx, W, G; ld_m: y, z, residual, dy, dz; 0: dense).
+ * act: one of QG_ACT_*; silu(z) = z / (1 + exp(-z)), gelu(z) = z Phi(z) with the normal distribution's cdf.
+ *
+ * qg_int8_linear_act_forward:  z = x W^T + bias (bf16 [m], nullable);  y = act(z) + residual (bf16 [tokens][ld_m], nullable).  The
+ *   activation takes the fp32 sum; z (nullable) is what the backward pass wants, rounded to bf16.  y may be residual.
+ * qg_int8_linear_act_backward: dz = dy act'(z);  dx = dz W, G = dz^T x, dbias (fp32 [m]) = sum over tokens of dz, each of them
+ *   nullable (and then the inputs only it needs are too).  dz (bf16 [tokens][ld_m], may be dy or z) is written where a product is
+ *   asked for; QG_ACT_NONE needs neither z nor dz.  The residual's gradient is dy.  workspace (dbias only):
+ *   qg_int8_linear_act_workspace_bytes(tokens, m) bytes, 16-byte aligned.
+ * qg_int8_gated_forward:  y = act(x Wg^T) * (x Wu^T), both weights m x n; zg, zu: both (for the backward pass) or neither.
+ * qg_int8_gated_backward: dzg = dy zu act'(zg), dzu = dy act(zg) (bf16 [tokens][ld_m], written; may be zg and zu);
+ *   dx = dzg Wg + dzu Wu (nullable), Gg = dzg^T x and Gu = dzu^T x (both or neither). */
+enum { QG_ACT_NONE = 0, QG_ACT_RELU = 1, QG_ACT_SILU = 2, QG_ACT_GELU = 3 };
+int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* Wq, const float* Ws, const uint16_t* bias_bf16,
+                               const uint16_t* residual_bf16, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n,
+                               int64_t ld_m, int group, uint16_t* z_bf16, uint16_t* y_bf16, void* stream);
+size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m);
+int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16_t* z_bf16, const uint16_t* x_bf16, const int8_t* Wq,
+                                const float* Ws, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group,
+                                uint16_t* dz_bf16, uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias, void* workspace,
+                                size_t workspace_bytes, void* stream);
+int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus, int act,
+                          int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* zg_bf16,
+                          uint16_t* zu_bf16, uint16_t* y_bf16, void* stream);
+int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, const uint16_t* zu_bf16, const uint16_t* x_bf16,
+                           const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus, int act, int64_t tokens,
+                           int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* dzg_bf16, uint16_t* dzu_bf16,
+                           uint16_t* dx_bf16, uint16_t* Gg_bf16, uint16_t* Gu_bf16, void* stream);
+
+/* ---- Loss of a language model's head: softmax cross entropy over the vocabulary, without the logits in memory.
+ * z = x W^T with x bf16 [tokens][h] and W bf16 [vocab][h]; labels int64 [tokens], a label outside [0, vocab) marks a token
+ * without a loss (padding, a prompt): its loss is 0, its row of dx is 0, and it adds nothing to dW whatever its row of x holds.
+ * qg_head_loss_forward:  lse = log sum_v exp z_v, loss = lse - z_label, fp32 [tokens].
+ * qg_head_loss_backward: from lse and dloss (fp32 [tokens], the gradient of each token's loss: a mean's 1/count, a weight),
+ *   dz = dloss (exp(z - lse) - onehot), rounded to bf16;  dx = dz W, dW = dz^T x, either may be NULL.  The vocabulary is
+ *   taken in pieces: the logits of a piece are computed again, and only tokens x piece numbers are stored.
+ * ld: row pitch of x, W, dx and dW: h (or 0), or more and a multiple of 16.  tokens and vocab below 2^24, h below 2^16,
+ * tokens * vocab below 2^38, tokens * h below 2^34.  workspace: qg_head_loss_workspace_bytes(tokens, h, vocab) bytes, 16-byte
+ * aligned, enough for either call. */
+size_t qg_head_loss_workspace_bytes(int64_t tokens, int64_t h, int64_t vocab);
+int qg_head_loss_forward(const uint16_t* x_bf16, const uint16_t* W_bf16, const int64_t* labels, int64_t tokens, int64_t h,
+                         int64_t vocab, int64_t ld, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                         void* stream);
+int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const int64_t* labels, const float* lse,
+                          const float* dloss, int64_t tokens, int64_t h, int64_t vocab, int64_t ld, uint16_t* dx_bf16,
+                          uint16_t* dW_bf16, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Adaptive lazy update policy (Sec. 3.2), HOST ONLY (p is a host pointer):
  * streak counts consecutive checks with cos >= threshold; at k in a row the
  * interval doubles and the streak restarts; next_refresh advances by the

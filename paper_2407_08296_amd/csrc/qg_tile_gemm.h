@@ -57,6 +57,12 @@ struct LinOperand {
     int sgroups;
     const float* zeros = nullptr;   // INT8 with zero points only: [rows][sgroups]
 };
+// Two INT8 operands of one shape with k fast, interleaved in a tile: of every 64 x indices of the tile the first 32 are rows of the
+// one, the other 32 the same rows of the other, so that a wave holds both products of an output element.
+struct LinPairOperand : LinOperand {
+    const void* base2;
+    const float* scales2;
+};
 
 // Several GEMMs of one shape in one launch (gridDim.y of them): GEMM z takes its A operand from a[z], its B operand
 // strideB_bytes * z past B's base and writes C + strideC * z.  One GEMM: a[0] = A's base, strides 0.
@@ -94,12 +100,22 @@ struct LinStage {
     // KI: int or int64_t.  Over a 64-bit k0 the compiler turns the addresses of a loop into running pointers; over a 32-bit
     // one it recomputes a 64-bit product per chunk and step (grad_W with 128 x 128 x 32 tiles, 2048 tokens, 2560 x 2048:
     // 36.2 against 38.6 us), which takes fewer registers.
-    template <int FETCH, typename KI>
-    __device__ __forceinline__ void fetch(const LinOperand& op, int x0, int X, KI k0, int K) {
+    template <int FETCH, typename KI, typename OP>
+    __device__ __forceinline__ void fetch(const OP& op, int x0, int X, KI k0, int K) {
+        constexpr bool kPair = std::is_same_v<OP, LinPairOperand>;
+        static_assert(!kPair || (kFast && kInt8 && !kZero), "pairs: INT8 with k fast");
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
             const int idx = thread() + NT * q;
-            const int tr = idx / CPR, tc = (idx % CPR) * CH;         // row and first column inside the tile
+            const int in_tile = idx / CPR, tc = (idx % CPR) * CH;    // row and first column inside the tile
+            const bool second = kPair && (in_tile & 32) != 0;
+            const int tr = kPair ? (in_tile >> 6) * 32 + (in_tile & 31) : in_tile;
+            const void* base = op.base;
+            const float* scales = op.scales;
+            if constexpr (kPair) {
+                base = second ? op.base2 : base;
+                scales = second ? op.scales2 : scales;
+            }
             int x = x0 + (kFast ? tr : tc);                          // ... and inside the matrix
             const int xs = min(x, X - 1);                            // for the block scale: the chunk's own block
             const int past = FETCH == kFetchShifted && !kFast ? min(max(x - (X - CH), 0), CH - 1) : 0;
@@ -113,14 +129,14 @@ struct LinStage {
             }
             const int64_t off = (int64_t)row * op.ld + col;
             if constexpr (kInt8) {
-                const int8_t* src = static_cast<const int8_t*>(op.base) + off;
+                const int8_t* src = static_cast<const int8_t*>(base) + off;
                 if constexpr (FETCH == kFetchAligned) v[q] = *reinterpret_cast<const u32x4*>(src);
                 else v[q] = load16_i8_guarded(src, valid);
                 const auto block = (!kFast && FETCH == kFetchShifted ? xs : col) >> 8;
-                s[q] = valid > 0 ? op.scales[(int64_t)row * op.sgroups + block] : 0.f;
+                s[q] = valid > 0 ? scales[(int64_t)row * op.sgroups + block] : 0.f;
                 if constexpr (kZero) z[q] = valid > 0 ? op.zeros[(int64_t)row * op.sgroups + block] : 0.f;
             } else {
-                const uint16_t* src = static_cast<const uint16_t*>(op.base) + off;
+                const uint16_t* src = static_cast<const uint16_t*>(base) + off;
                 if constexpr (FETCH == kFetchAligned) v[q] = *reinterpret_cast<const u32x4*>(src);
                 else v[q] = load8_bf16_guarded(src, valid);
             }
@@ -193,8 +209,58 @@ __device__ __forceinline__ void store_block(const f32x16& acc, float bj, float* 
     }
 }
 
-// C[M][N] (bf16 or fp32) = sum_k A(i, k) B(k, j) (+ bias[j]); A's x index runs over the rows of C, B's over its
-// columns.  Tile TM = 32 MB WM rows x TN columns, a wave computes 32 MB x TN / 2.
+// R consecutive bf16 elements of a row (R: 4 or 8), of which the first `left` exist; rows may start at any element.
+template <int R>
+__device__ __forceinline__ void store_run(uint16_t* dst, int left, const float (&v)[R]) {
+    uint32_t o[R / 2];
+#pragma unroll
+    for (int e = 0; e < R / 2; ++e) o[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    if (left >= R) {
+        if constexpr (R == 4) *reinterpret_cast<u32x2_align2*>(dst) = u32x2{o[0], o[1]};
+        else *reinterpret_cast<u32x4_align2*>(dst) = u32x4{o[0], o[1], o[2], o[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < R - 1; ++e)
+            if (e < left) dst[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+    }
+}
+
+// What becomes of a wave's sums, its MB x NB blocks of 32 x 32 from row row0 and column col0 of C on: here C = sum (+ bias[j]).
+// `tp`: kTransposeFloats floats of LDS of the wave's own; inside: all blocks lie inside C.
+template <typename OUT>
+struct PlainEpilogue {
+    static constexpr bool kPair = false;
+    const uint16_t* bias;
+    OUT* C;
+    int64_t ldc;
+    template <bool EXACT, int MB, int NB>
+    __device__ __forceinline__ void tile(const f32x16 (&acc)[MB][NB], float* tp, int row0, int col0, bool inside, int M, int N,
+                                         int lane) const {
+#pragma unroll
+        for (int a = 0; a < MB; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int r = row0 + a * 32, c = col0 + b * 32, col = c + (lane & 31);
+                const float bj = (bias != nullptr && (EXACT || col < N)) ? __builtin_bit_cast(float, (uint32_t)bias[col] << 16) : 0.f;
+                if (EXACT || inside) store_block<true>(acc[a][b], bj, tp, C, ldc, r, c, M, N, lane);
+                else store_block<false>(acc[a][b], bj, tp, C, ldc, r, c, M, N, lane);
+            }
+    }
+    // R consecutive elements of a row, of which the first `left` lie inside C
+    template <int R>
+    __device__ __forceinline__ void run(int row, int col, int left, float (&v)[R]) const {
+        if (bias != nullptr) {
+#pragma unroll
+            for (int e = 0; e < R; ++e)
+                if (e < left) v[e] += __builtin_bit_cast(float, (uint32_t)bias[col + e] << 16);
+        }
+        store_run(C + (int64_t)row * ldc + col, left, v);
+    }
+};
+
+// C[M][N] (bf16 or fp32) = sum_k A(i, k) B(k, j) (+ bias[j]), or what the epilogue makes of the sum; A's x index runs over the
+// rows of C, B's over its columns.  Tile TM = 32 MB WM rows x TN columns, a wave computes 32 MB x TN / 2.  A paired B (and an
+// epilogue for pairs): TN / 2 columns of each product.  A2, B2: a second product of the same shape, added (TERMS == 2).
 // Two LDS stages, one barrier per step.  DEEP: two register sets - while the MFMAs of step kt read stage kt & 1, the
 // operands of step kt + 1 are written to the other stage and those of step kt + 2 are fetched, all of it between the
 // MFMAs: for workgroups that have a CU to themselves.  Otherwise one set - the operands of step kt + 1 are fetched before
@@ -222,10 +288,9 @@ struct TileGemm {
     static constexpr int SMEM = STAGING > TRANSPOSE ? STAGING : TRANSPOSE;   // uint16 elements
 };
 
-template <int AL, int BL, bool EXACT, typename OUT, int MB, int TN, int BK, int WM, bool DEEP, int KG = 1>
-__device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand& B, const uint16_t* __restrict__ bias,
-                                          OUT* __restrict__ C, int64_t ldc, int M, int N, int K, int tiles_m, int tiles_n,
-                                          uint32_t tile, uint16_t* smem) {
+template <int AL, int BL, bool EXACT, int MB, int TN, int BK, int WM, bool DEEP, int KG, int TERMS, typename OPB, typename EPI>
+__device__ __forceinline__ void tile_gemm_epi(const LinOperand& A1, const OPB& B1, const LinOperand& A2, const OPB& B2, const EPI& epi,
+                                              int M, int N, int K, int tiles_m, int tiles_n, uint32_t tile, uint16_t* smem) {
     using T = TileGemm<AL, BL, MB, TN, BK, WM, KG>;
     using SA = typename T::SA;
     using SB = typename T::SB;
@@ -241,7 +306,9 @@ __device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand&
     // eight A panels and a few B panels.
     const int strip = (int)(tile / (uint32_t)(kLinStrip * tiles_n)), in_strip = (int)(tile % (uint32_t)(kLinStrip * tiles_n));
     const int strip_rows = min(kLinStrip, tiles_m - strip * kLinStrip);
-    const int i0 = (strip * kLinStrip + in_strip % strip_rows) * TM, j0 = (in_strip / strip_rows) * TN;
+    constexpr int TC = EPI::kPair ? TN / 2 : TN;      // columns of C per tile
+    static_assert(!EPI::kPair || TN % 128 == 0, "pairs: both blocks of an output element in one wave");
+    const int i0 = (strip * kLinStrip + in_strip % strip_rows) * TM, j0 = (in_strip / strip_rows) * TC;
     SA sa[DEEP ? 2 : 1];
     SB sb[DEEP ? 2 : 1];
     constexpr int NB = TN / 64;                // 32 x 32 blocks of a wave: MB x NB
@@ -273,6 +340,8 @@ __device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand&
     // The KT steps from k = 0 on, every chunk of them fetched under FETCH's terms.
     // (64-deep steps with two register sets have no registers left for running pointers.)
     using KI = std::conditional_t<DEEP && BK == 64, int, int64_t>;
+    bool inside = true;
+    auto contraction = [&](const LinOperand& A, const OPB& B) {
     auto steps = [&](auto fetch_mode, int KT) {
         constexpr int FETCH = decltype(fetch_mode)::value;
         auto fetch = [&](KI k0, int set) {
@@ -336,11 +405,10 @@ __device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand&
             lds_barrier();
         }
     };
-    bool inside = true;
     if constexpr (EXACT) {
         steps(std::integral_constant<int, kFetchAligned>(), K / BK);
     } else {
-        inside = i0 + TM <= M && j0 + TN <= N;
+        inside = i0 + TM <= M && j0 + TC <= N;
         const int whole = K / BK;
         const bool shiftable = SA::shiftable(M) && SB::shiftable(N);
         if (!shiftable) {
@@ -364,6 +432,9 @@ __device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand&
             }
         }
     }
+    };
+    contraction(A1, B1);
+    if constexpr (TERMS == 2) contraction(A2, B2);
     if constexpr (KG > 1) {   // the groups' sums through LDS, group 0 adds them in order
         static_assert(MB * NB * T::NT * 16 * 4 <= T::SMEM * 2, "they fit in a group's staging buffers");
         const int t = threadIdx.x & (T::NT - 1);
@@ -385,16 +456,18 @@ __device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand&
                 for (int e = 0; e < 4; ++e) acc[q / 4 / NB][q / 4 % NB][q % 4 * 4 + e] += x[e];
             }
     }
-    float* tp = reinterpret_cast<float*>(smem) + wave * kTransposeFloats;
-#pragma unroll
-    for (int a = 0; a < MB; ++a)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int row0 = i0 + wm * 32 * MB + a * 32, col0 = j0 + wn * (TN / 2) + b * 32, col = col0 + (lane & 31);
-            const float bj = (bias != nullptr && (EXACT || col < N)) ? __builtin_bit_cast(float, (uint32_t)bias[col] << 16) : 0.f;
-            if (EXACT || inside) store_block<true>(acc[a][b], bj, tp, C, ldc, row0, col0, M, N, lane);
-            else store_block<false>(acc[a][b], bj, tp, C, ldc, row0, col0, M, N, lane);
-        }
+    constexpr int kBuffers = EPI::kPair ? 2 : 1;
+    static_assert(kBuffers * T::TRANSPOSE <= T::SMEM, "the transpose buffers fit in the staging buffers");
+    epi.template tile<EXACT>(acc, reinterpret_cast<float*>(smem) + wave * kBuffers * kTransposeFloats, i0 + wm * 32 * MB,
+                             j0 + wn * (TC / 2), inside, M, N, lane);
+}
+
+template <int AL, int BL, bool EXACT, typename OUT, int MB, int TN, int BK, int WM, bool DEEP, int KG = 1>
+__device__ __forceinline__ void tile_gemm(const LinOperand& A, const LinOperand& B, const uint16_t* __restrict__ bias,
+                                          OUT* __restrict__ C, int64_t ldc, int M, int N, int K, int tiles_m, int tiles_n,
+                                          uint32_t tile, uint16_t* smem) {
+    tile_gemm_epi<AL, BL, EXACT, MB, TN, BK, WM, DEEP, KG, 1>(A, B, A, B, PlainEpilogue<OUT>{bias, C, ldc}, M, N, K, tiles_m, tiles_n,
+                                                              tile, smem);
 }
 
 template <int AL, int BL, bool EXACT, typename OUT, int MB, int TN, int BK, int WM, bool DEEP, int KG = 1>
@@ -425,21 +498,22 @@ struct LinProduct {
 // counts is the length of a workgroup's serial chain (fetch, commit, fragments, MFMAs per step): it is KW times shorter than
 // with the tile split over the waves, there are four times as many workgroups as with 64 x 64 tiles, and since a wave stages
 // its own operands (its LDS accesses complete in order) there is no barrier before the final sum.
-template <int AL, int BL, int KW>
+// NB: 2 for a paired B, the two products of 32 x 32 output elements.
+template <int AL, int BL, int KW, int NB = 1>
 struct KSplit {
     static constexpr int BK = 64, NT = 64 * KW;
     using SA = LinStage<AL, 32, BK, 64>;
-    using SB = LinStage<BL, 32, BK, 64>;
-    static constexpr int WAVE = SA::ELEMS + SB::ELEMS;   // uint16 elements of a wave's operands, then of its partial tile
-    static_assert(2 * kTransposeFloats <= WAVE, "the partial tile fits where the operands were");
+    using SB = LinStage<BL, 32 * NB, BK, 64>;
+    static constexpr int WAVE = SA::ELEMS + SB::ELEMS;   // uint16 elements of a wave's operands, then of its partial tiles
+    static_assert(2 * NB * kTransposeFloats <= WAVE, "the partial tiles fit where the operands were");
     static constexpr int SMEM = KW * WAVE;
 };
 
-template <int AL, int BL, bool EXACT, int KW>
-__device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperand& B, const uint16_t* __restrict__ bias,
-                                            uint16_t* __restrict__ C, int64_t ldc, int M, int N, int K, int tiles_m, int tiles_n,
-                                            uint32_t tile, uint16_t* smem) {
-    using T = KSplit<AL, BL, KW>;
+template <int AL, int BL, bool EXACT, int KW, int TERMS, typename OPB, typename EPI>
+__device__ __forceinline__ void ksplit_epi(const LinOperand& A1, const OPB& B1, const LinOperand& A2, const OPB& B2, const EPI& epi, int M,
+                                           int N, int K, int tiles_m, int tiles_n, uint32_t tile, uint16_t* smem) {
+    constexpr int NB = EPI::kPair ? 2 : 1;
+    using T = KSplit<AL, BL, KW, NB>;
     using SA = typename T::SA;
     using SB = typename T::SB;
     constexpr int BK = T::BK;
@@ -452,9 +526,11 @@ __device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperan
     auto steps_below = [&](int n) { return n > wave ? (n - wave + KW - 1) / KW : 0; };   // of this wave, below step n
     SA sa[2];
     SB sb[2];
-    f32x16 acc;
+    f32x16 acc[NB];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[b][v] = 0.f;
     // between a wave's writes of its tiles and its reads, and back: its LDS instructions complete in order, so what has to
     // be kept is the order in which they are issued (the scheduler does not see the transposing reads as accesses)
     auto in_order = [] {
@@ -466,17 +542,21 @@ __device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperan
         sa[set].commit(At);
         sb[set].commit(Bt);
         in_order();
-        bf16x8 af[BK / 16], bf[BK / 16];
+        bf16x8 af[BK / 16], bf[NB][BK / 16];
 #pragma unroll
         for (int kk = 0; kk < BK / 16; ++kk) {
             af[kk] = SA::frag(At, 0, kk, lane);
-            bf[kk] = SB::frag(Bt, 0, kk, lane);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) bf[b][kk] = SB::frag(Bt, 32 * b, kk, lane);
         }
         in_order();
         fetch_next();
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[kk], bf[kk], acc, 0, 0, 0);
+        for (int kk = 0; kk < BK / 16; ++kk)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[kk], bf[b][kk], acc[b], 0, 0, 0);
     };
+    auto contraction = [&](const LinOperand& A, const OPB& B) {
     // this wave's steps first, first + KW, ... (`count` of them), fetched two ahead under FETCH's terms
     auto run = [&](auto fetch_mode, int first, int count) {
         constexpr int FETCH = decltype(fetch_mode)::value;
@@ -505,35 +585,39 @@ __device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperan
     } else {
         run(Guarded(), wave, steps_below(total));
     }
+    };
+    contraction(A1, B1);
+    if constexpr (TERMS == 2) contraction(A2, B2);
     float* tp = reinterpret_cast<float*>(At);
 #pragma unroll
-    for (int v = 0; v < 16; ++v) tp[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * kTransposePitch + (lane & 31)] = acc[v];
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            tp[b * kTransposeFloats + (8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * kTransposePitch + (lane & 31)] = acc[b][v];
     __syncthreads();
     if (threadIdx.x >= 256) return;
     const int row = threadIdx.x / 8, col = (threadIdx.x % 8) * 4;        // four columns of a row per thread
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float sum[NB][4] = {};
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * T::WAVE) +
-                                                        row * kTransposePitch + col);
+    for (int w = 0; w < KW; ++w)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += x[e];
-    }
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * T::WAVE) + b * kTransposeFloats +
+                                                            row * kTransposePitch + col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[b][e] += x[e];
+        }
     const int left = EXACT ? 4 : (i0 + row < M ? N - (j0 + col) : 0);
-    if (bias != nullptr) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) sum[e] += __builtin_bit_cast(float, (uint32_t)bias[j0 + col + e] << 16);
-    }
-    const u32x2 o = {pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
-    uint16_t* dst = C + (int64_t)(i0 + row) * ldc + j0 + col;
-    if (left >= 4) {
-        *reinterpret_cast<u32x2_align2*>(dst) = o;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < left) dst[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
-    }
+    if (left <= 0) return;
+    if constexpr (EPI::kPair) epi.run(i0 + row, j0 + col, left, sum[0], sum[1]);
+    else epi.run(i0 + row, j0 + col, left, sum[0]);
+}
+
+template <int AL, int BL, bool EXACT, int KW>
+__device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperand& B, const uint16_t* __restrict__ bias,
+                                            uint16_t* __restrict__ C, int64_t ldc, int M, int N, int K, int tiles_m, int tiles_n,
+                                            uint32_t tile, uint16_t* smem) {
+    ksplit_epi<AL, BL, EXACT, KW, 1>(A, B, A, B, PlainEpilogue<uint16_t>{bias, C, ldc}, M, N, K, tiles_m, tiles_n, tile, smem);
 }
 
 template <int BL, bool EXACT, int KW>

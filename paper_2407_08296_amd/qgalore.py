@@ -35,6 +35,8 @@ EXPORTS = [
     "qg_subspace_cossim_static", "qg_subspace_cossim_weighted", "qg_step_ld", "qg_subspace_refresh_many_ld",
     "qg_int8_linear_forward_ld", "qg_int8_linear_backward_ld",
     "qg_residual_norm_forward", "qg_residual_norm_workspace_bytes", "qg_residual_norm_backward",
+    "qg_int8_linear_act_forward", "qg_int8_linear_act_workspace_bytes", "qg_int8_linear_act_backward", "qg_int8_gated_forward",
+    "qg_int8_gated_backward", "qg_head_loss_workspace_bytes", "qg_head_loss_forward", "qg_head_loss_backward",
 ]
 
 
@@ -145,6 +147,16 @@ def lib() -> C.CDLL:
         L.qg_residual_norm_workspace_bytes.argtypes = [i64, i64]
         L.qg_residual_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, f32, f32, i64, i64, i64, i32, vp, vp, vp, vp, vp,
                                                 vp, sz, vp]
+        L.qg_int8_linear_act_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp]
+        L.qg_int8_linear_act_workspace_bytes.restype = sz
+        L.qg_int8_linear_act_workspace_bytes.argtypes = [i64, i64]
+        L.qg_int8_linear_act_backward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.qg_int8_gated_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp]
+        L.qg_int8_gated_backward.argtypes = [vp] * 8 + [i32, i64, i64, i64, i64, i64, i32] + [vp] * 6
+        L.qg_head_loss_workspace_bytes.restype = sz
+        L.qg_head_loss_workspace_bytes.argtypes = [i64, i64, i64]
+        L.qg_head_loss_forward.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
+        L.qg_head_loss_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -176,6 +188,7 @@ def _stream() -> int:
 
 
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+_F32 = (torch.float32,)
 
 
 def _bf16_rows(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
@@ -525,8 +538,92 @@ def int8_linear_t_backward(dy: torch.Tensor, x: torch.Tensor | None, Sq: torch.T
     return dx, G
 
 
+# ---------------------------------------------------------------- INT8 linear layer with an epilogue
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_I8 = (torch.int8,)
+
+
+def _act(name: str) -> int:
+    if name not in ACTIVATIONS:
+        raise QGError(f"activation {name!r} is none of {sorted(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
+
+
+def _weight(q: torch.Tensor | None, s: torch.Tensor | None, m: int, n: int):
+    """Pointers to the codes and scales of an m x n weight."""
+    _expect(q, m, n)
+    _expect(s, m, (n + GROUP - 1) // GROUP)
+    return _ptr(q, _I8), _ptr(s, _F32)
+
+
+def int8_linear_act_forward(x: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor, bias: torch.Tensor | None = None,
+                            residual: torch.Tensor | None = None, act: str = "none", want_z: bool = False):
+    """Returns (y, z): z = x W^T + bias, y = act(z) + residual; z is None unless want_z."""
+    tokens, n = x.shape
+    m = Wq.shape[0]
+    _expect(bias, m)
+    _expect(residual, tokens, m)
+    w = _weight(Wq, Ws, m, n)
+    y = _bf16_rows(x, tokens, m)
+    z = _bf16_rows(x, tokens, m) if want_z else None
+    _check(lib().qg_int8_linear_act_forward(_ptr(x, _BF16), *w, _ptr(bias, _BF16), _ptr(residual, _BF16), _act(act), tokens, m, n, n, m,
+                                            GROUP, _ptr(z), _ptr(y), _stream()))
+    return y, z
+
+
+def int8_linear_act_backward(dy: torch.Tensor, z: torch.Tensor | None, x: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor,
+                             act: str = "none", want_dx: bool = True, want_G: bool = True, want_dbias: bool = False):
+    """Returns (dx, G, dbias) of int8_linear_act_forward (None where not wanted); the residual's gradient is dy itself."""
+    tokens, m = dy.shape
+    n = x.shape[1]
+    kind = _act(act)
+    _expect(x, tokens, n)
+    _expect(z, tokens, m)
+    w = _weight(Wq, Ws, m, n)
+    dx = _bf16_rows(dy, tokens, n) if want_dx else None
+    G = _bf16_rows(dy, m, n) if want_G else None
+    dz = _bf16_rows(dy, tokens, m) if kind and (want_dx or want_G) else None
+    dbias = ws = None
+    nbytes = 0
+    if want_dbias:
+        dbias = torch.empty(m, dtype=torch.float32, device=dy.device)
+        nbytes = lib().qg_int8_linear_act_workspace_bytes(tokens, m)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device)
+    _check(lib().qg_int8_linear_act_backward(_ptr(dy, _BF16), _ptr(z, _BF16), _ptr(x, _BF16), *w, kind, tokens, m, n, n, m, GROUP,
+                                             _ptr(dz), _ptr(dx), _ptr(G), _ptr(dbias), _ptr(ws), nbytes, _stream()))
+    return dx, G, dbias
+
+
+def int8_gated_forward(x: torch.Tensor, Wgq: torch.Tensor, Wgs: torch.Tensor, Wuq: torch.Tensor, Wus: torch.Tensor, act: str = "silu",
+                       want_z: bool = False):
+    """Returns (y, zg, zu): y = act(x Wg^T) * (x Wu^T); zg and zu, which the backward pass takes, are None unless want_z."""
+    tokens, n = x.shape
+    m = Wgq.shape[0]
+    w = _weight(Wgq, Wgs, m, n) + _weight(Wuq, Wus, m, n)
+    y = _bf16_rows(x, tokens, m)
+    zg, zu = (_bf16_rows(x, tokens, m), _bf16_rows(x, tokens, m)) if want_z else (None, None)
+    _check(lib().qg_int8_gated_forward(_ptr(x, _BF16), *w, _act(act), tokens, m, n, n, m, GROUP, _ptr(zg), _ptr(zu), _ptr(y), _stream()))
+    return y, zg, zu
+
+
+def int8_gated_backward(dy: torch.Tensor, zg: torch.Tensor, zu: torch.Tensor, x: torch.Tensor, Wgq: torch.Tensor, Wgs: torch.Tensor,
+                        Wuq: torch.Tensor, Wus: torch.Tensor, act: str = "silu", want_dx: bool = True, want_G: bool = True):
+    """Returns (dx, Gg, Gu) of int8_gated_forward (None where not wanted)."""
+    tokens, m = dy.shape
+    n = x.shape[1]
+    _expect(x, tokens, n)
+    for v in (zg, zu):
+        _expect(v, tokens, m)
+    w = _weight(Wgq, Wgs, m, n) + _weight(Wuq, Wus, m, n)
+    dx = _bf16_rows(dy, tokens, n) if want_dx else None
+    Gg, Gu = (_bf16_rows(dy, m, n), _bf16_rows(dy, m, n)) if want_G else (None, None)
+    dzg, dzu = _bf16_rows(dy, tokens, m), _bf16_rows(dy, tokens, m)
+    _check(lib().qg_int8_gated_backward(_ptr(dy, _BF16), _ptr(zg, _BF16), _ptr(zu, _BF16), _ptr(x, _BF16), *w, _act(act), tokens, m, n, n,
+                                        m, GROUP, _ptr(dzg), _ptr(dzu), _ptr(dx), _ptr(Gg), _ptr(Gu), _stream()))
+    return dx, Gg, Gu
+
+
 # ---------------------------------------------------------------- residual stream
-_F32 = (torch.float32,)
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
 
 
@@ -596,6 +693,43 @@ def residual_norm_backward(du: torch.Tensor | None, dh_next: torch.Tensor | None
                                            _ptr(dh, stype), _ptr(dy), _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), _ptr(ws), nbytes,
                                            _stream()))
     return dh, dy, dw_pre, dw_post, dgate
+
+
+# ---------------------------------------------------------------- loss of a language model's head
+def _head(x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, workspace: torch.Tensor | None):
+    (tokens, h), vocab = x.shape, W.shape[0]
+    _expect(W, vocab, h)
+    _expect(labels, tokens)
+    if workspace is None:
+        nbytes = lib().qg_head_loss_workspace_bytes(tokens, h, vocab)
+        if nbytes == 0:
+            raise QGError("libqgalore: shape out of range")
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    return tokens, h, vocab, workspace
+
+
+def head_loss_forward(x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, workspace: torch.Tensor | None = None):
+    """Returns (loss, lse), fp32 [tokens]: cross entropy of softmax(x W^T) against int64 labels; outside [0, vocab): no loss, 0.
+    workspace: uint8, qg_head_loss_workspace_bytes(tokens, h, vocab) of them (allocated if None)."""
+    tokens, h, vocab, ws = _head(x, W, labels, workspace)
+    loss = torch.empty(tokens, dtype=torch.float32, device=x.device)
+    lse = torch.empty(tokens, dtype=torch.float32, device=x.device)
+    _check(lib().qg_head_loss_forward(_ptr(x, _BF16), _ptr(W, _BF16), _ptr(labels, (torch.int64,)), tokens, h, vocab, h, _ptr(loss),
+                                      _ptr(lse), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+    return loss, lse
+
+
+def head_loss_backward(x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                       want_dx: bool = True, want_dW: bool = True, workspace: torch.Tensor | None = None):
+    """Returns (dx, dW) of sum_t dloss[t] loss[t] (None where not wanted), from the lse of head_loss_forward."""
+    tokens, h, vocab, ws = _head(x, W, labels, workspace)
+    _expect(lse, tokens)
+    _expect(dloss, tokens)
+    dx = _bf16_rows(x, tokens, h) if want_dx else None
+    dW = _bf16_rows(x, vocab, h) if want_dW else None
+    _check(lib().qg_head_loss_backward(_ptr(x, _BF16), _ptr(W, _BF16), _ptr(labels, (torch.int64,)), _ptr(lse, _F32), _ptr(dloss, _F32),
+                                       tokens, h, vocab, h, _ptr(dx), _ptr(dW), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+    return dx, dW
 
 
 # ---------------------------------------------------------------- subspace refresh

@@ -50,3 +50,73 @@ def test_residual_norm_backward(L):
     assert call(a19=None) == 5 and call(a20=nbytes - 1) == 5
     for i in (0, 1, 2, 3, 4, 5, 7, 14, 15, 16, 17, 18, 19):
         assert call(**{f"a{i}": FAKE + 4}) == 4
+
+
+def test_int8_linear_act(L):
+    # x, Wq, Ws, bias, residual, act, tokens, m, n, ld_n, ld_m, group, z, y, stream
+    call = caller(L.qg_int8_linear_act_forward, FAKE, FAKE, FAKE, FAKE, FAKE, 2, 16, 512, 256, 0, 0, 256, FAKE, FAKE, None)
+    for i in (0, 1, 2, 13):
+        assert call(**{f"a{i}": None}) == 1
+    assert call(a5=4) == 2 and call(a5=-1) == 2
+    assert call(a6=0) == 2 and call(a7=-1) == 2 and call(a8=0) == 2 and call(a6=1 << 20, a7=1 << 12) == 2
+    assert call(a9=255) == 2 and call(a9=264) == 2 and call(a10=520) == 2
+    assert call(a11=128) == 3
+    for i in (0, 1, 2, 3, 4, 12, 13):
+        assert call(**{f"a{i}": FAKE + 2}) == 4
+    nbytes = L.qg_int8_linear_act_workspace_bytes(16, 512)
+    assert nbytes >= 512 * 4 and L.qg_int8_linear_act_workspace_bytes(0, 512) == 0 and L.qg_int8_linear_act_workspace_bytes(1 << 20, 1 << 20) == 0
+    # dy, z, x, Wq, Ws, act, tokens, m, n, ld_n, ld_m, group, dz, dx, G, dbias, ws, bytes, stream
+    call = caller(L.qg_int8_linear_act_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 3, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, FAKE, nbytes,
+                  None)
+    for i in (0, 1, 2, 3, 4, 12):
+        assert call(**{f"a{i}": None}) == 1
+    assert call(a13=None, a14=None, a15=None) == 1
+    assert call(a5=9) == 2 and call(a6=0) == 2 and call(a9=8) == 2 and call(a10=500) == 2 and call(a11=64) == 3
+    assert call(a16=None) == 5 and call(a17=nbytes - 1) == 5
+    for i in (0, 1, 2, 3, 4, 12, 13, 14, 15, 16):
+        assert call(**{f"a{i}": FAKE + 8}) == 4
+
+
+def test_int8_gated(L):
+    # x, Wgq, Wgs, Wuq, Wus, act, tokens, m, n, ld_n, ld_m, group, zg, zu, y, stream
+    call = caller(L.qg_int8_gated_forward, FAKE, FAKE, FAKE, FAKE, FAKE, 2, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, None)
+    for i in (0, 1, 2, 3, 4, 12, 13, 14):
+        assert call(**{f"a{i}": None}) == 1          # zg without zu, and the other way round, too
+    assert call(a5=4) == 2 and call(a6=0) == 2 and call(a9=250) == 2 and call(a10=513) == 2 and call(a11=32) == 3
+    for i in (0, 1, 2, 3, 4, 12, 13, 14):
+        assert call(**{f"a{i}": FAKE + 4}) == 4
+    # dy, zg, zu, x, Wgq, Wgs, Wuq, Wus, act, tokens, m, n, ld_n, ld_m, group, dzg, dzu, dx, Gg, Gu, stream
+    call = caller(L.qg_int8_gated_backward, *[FAKE] * 8, 2, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, FAKE, None)
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 15, 16, 18, 19):
+        assert call(**{f"a{i}": None}) == 1
+    assert call(a17=None, a18=None, a19=None) == 1
+    assert call(a8=7) == 2 and call(a10=0) == 2 and call(a12=1) == 2 and call(a13=528 + 1) == 2 and call(a14=1) == 3
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 15, 16, 17, 18, 19):
+        assert call(**{f"a{i}": FAKE + 8}) == 4
+
+
+def test_head_loss(L):
+    nbytes = L.qg_head_loss_workspace_bytes(16, 64, 1000)
+    assert nbytes >= 16 * 64 * 2 + 16 * 1000 * 2
+    for bad in ((0, 64, 1000), (16, 0, 1000), (16, 64, -1), (1 << 24, 64, 1000), (16, 65536, 1000), (16, 64, 1 << 24), (1 << 20, 64, 1 << 18),
+                (1 << 23, 2048, 1000)):
+        assert L.qg_head_loss_workspace_bytes(*bad) == 0
+    # a long batch over a wide vocabulary: far below its logits in 16 bits
+    assert L.qg_head_loss_workspace_bytes(65536, 4096, 128000) < 65536 * 128000 * 2 // 8
+    # x, W, labels, tokens, h, vocab, ld, loss, lse, ws, bytes, stream
+    call = caller(L.qg_head_loss_forward, FAKE, FAKE, FAKE, 16, 64, 1000, 0, FAKE, FAKE, FAKE, nbytes, None)
+    for i in (0, 1, 2, 7, 8):
+        assert call(**{f"a{i}": None}) == 1
+    assert call(a3=0) == 2 and call(a4=0) == 2 and call(a5=0) == 2 and call(a6=63) == 2 and call(a6=72) == 2
+    for i in (0, 1, 2, 7, 8, 9):
+        assert call(**{f"a{i}": FAKE + 8}) == 4
+    assert call(a9=None) == 5 and call(a10=64) == 5
+    # x, W, labels, lse, dloss, tokens, h, vocab, ld, dx, dW, ws, bytes, stream
+    call = caller(L.qg_head_loss_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 16, 64, 1000, 0, FAKE, FAKE, FAKE, nbytes, None)
+    for i in (0, 1, 2, 3, 4):
+        assert call(**{f"a{i}": None}) == 1
+    assert call(a9=None, a10=None) == 1
+    assert call(a5=-4) == 2 and call(a8=65) == 2
+    for i in (0, 1, 2, 3, 4, 9, 10, 11):
+        assert call(**{f"a{i}": FAKE + 4}) == 4
+    assert call(a11=None) == 5 and call(a12=64) == 5

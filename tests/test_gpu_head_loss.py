@@ -1,0 +1,206 @@
+"""The loss of a head and its gradients against the fp64 reference (oracle/layers.py) on the decoded inputs.
+
+Bars.  A logit is a fp32 sum of h products: 4 h 2^-24 of the root of their squares' sum.  lse and loss inherit that, plus the roundings of
+exponentials and sums (some 2^-24 of 1 + |lse|; the chain over the vocabulary is a tree of sums of positive numbers of at most
+log2(V) + 40 terms).  dz is rounded to bf16 for the products: each term of dx and dW is off by at most 2^-8 of itself, independently; the
+bar is six standard deviations, 4 * 2^-8 of the root of their squares' sum, and half a spacing for the output's own rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers as O
+from paper_2407_08296_amd import qgalore as qg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U24 = 2.0 ** -24
+
+# (tokens, h, vocab): one of everything, odd everything, around the tiles (64, 128, 256), several pieces (a long batch, a wide vocabulary)
+CASES = [(1, 1, 1), (1, 8, 2), (3, 7, 5), (1, 768, 4001), (33, 65, 130), (64, 64, 64), (65, 72, 257), (130, 521, 1000), (256, 128, 8192),
+         (300, 40, 20001), (2100, 64, 4100), (1100, 24, 16640), (40000, 16, 2600), (33000, 24, 1025)]
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def inputs(tokens, h, vocab, seed=0, spread=1.0):
+    g = torch.Generator().manual_seed(seed + tokens + h + vocab)
+    x = torch.randn(tokens, h, generator=g).bfloat16()
+    W = (torch.randn(vocab, h, generator=g) * (2 * spread / h ** 0.5)).bfloat16()
+    labels = torch.randint(0, vocab, (tokens,), generator=g)
+    labels[torch.rand(tokens, generator=g) < 0.2] = -100
+    if tokens > 4:
+        labels[0], labels[1], labels[2], labels[3] = 0, vocab - 1, vocab, 1 << 40      # both ends; two that are out of range
+    dloss = torch.randn(tokens, generator=g)
+    return tuple(t.to(DEV) for t in (x, W, labels, dloss))
+
+
+def noise_of(X, W):
+    return 4 * X.shape[1] * U24 * np.sqrt((X * X).sum(1).max() * (W * W).sum(1).max())
+
+
+@pytest.mark.parametrize("tokens,h,vocab", CASES)
+def test_forward(tokens, h, vocab):
+    x, W, labels, _ = inputs(tokens, h, vocab)
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    X, WW = f64(x), f64(W)
+    want, wlse = O.head_loss_forward(X, WW, labels.cpu().numpy())
+    bar = noise_of(X, WW) + (np.log2(vocab) + 40) * U24 * (1 + np.abs(wlse))
+    assert np.all(np.abs(f64(lse) - wlse) <= bar)
+    assert np.all(np.abs(f64(loss) - want) <= 2 * bar + 4 * U24 * np.abs(wlse - want))
+    learned = (labels >= 0) & (labels < vocab)
+    assert not loss[~learned].any()
+
+
+@pytest.mark.parametrize("tokens,h,vocab", CASES)
+def test_backward(tokens, h, vocab):
+    x, W, labels, dloss = inputs(tokens, h, vocab, seed=1)
+    _, lse = qg.head_loss_forward(x, W, labels)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    X, WW, lab, dl_t = f64(x), f64(W), labels.cpu().numpy(), f64(dloss)
+    want_dx, want_dW = O.head_loss_backward(X, WW, lab, dl_t)
+    learned = (lab >= 0) & (lab < vocab)
+    z = X @ WW.T
+    p = np.exp(z - z.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    # what the logits' and lse's noise does to p, and the cancellation of p - 1 at the label
+    rel = 2 * noise_of(X, WW) + 2 * (np.log2(vocab) + 40) * U24 * (1 + np.abs(np.log(np.exp(z - z.max(1, keepdims=True)).sum(1)) + z.max(1)))[:, None]
+    perr = np.where(learned, np.abs(dl_t), 0)[:, None] * p * rel
+    p[np.arange(tokens), np.where(learned, lab, 0)] -= 1
+    dl = np.where(learned, dl_t, 0)[:, None] * p
+    for got, want, a, e, b in ((dx, want_dx, dl, perr, WW), (dW, want_dW, dl.T, perr.T, X)):
+        k = a.shape[1]
+        bar = 2.0 ** -8 * np.abs(want) + (4 * 2.0 ** -8 + 4 * np.sqrt(k) * U24) * np.sqrt((a * a) @ (b * b)) + e @ np.abs(b)
+        err = np.abs(f64(got) - want)
+        assert got.dtype is torch.bfloat16 and np.all(err <= bar), float(np.max(err - bar))
+    assert not dx[torch.from_numpy(~learned).to(DEV)].any()
+    assert torch.equal(qg.head_loss_backward(x, W, labels, lse, dloss, want_dW=False)[0], dx)
+    assert torch.equal(qg.head_loss_backward(x, W, labels, lse, dloss, want_dx=False)[1], dW)
+
+
+@pytest.mark.parametrize("tokens,h,vocab", [(5, 24, 70), (300, 40, 20001), (33000, 24, 1025)])
+def test_rows_without_a_loss_may_hold_anything(tokens, h, vocab):
+    x, W, labels, dloss = inputs(tokens, h, vocab, seed=2)
+    learned = (labels >= 0) & (labels < vocab)
+    x = torch.where(learned[:, None], x, torch.zeros_like(x))
+    _, lse = qg.head_loss_forward(x, W, labels)
+    want = qg.head_loss_backward(x, W, labels, lse, dloss)
+    for junk in (float("nan"), float("inf"), 3e38):
+        xj = torch.where(learned[:, None], x, torch.full_like(x, junk))
+        dj = torch.where(learned, dloss, torch.full_like(dloss, float("nan")))
+        loss, lse = qg.head_loss_forward(xj, W, labels)
+        assert torch.isfinite(loss).all() and not loss[~learned].any()
+        for a, b in zip(want, qg.head_loss_backward(xj, W, labels, lse, dj)):
+            assert torch.equal(a, b)
+
+
+def test_no_token_with_a_loss():
+    x, W, labels, dloss = inputs(70, 64, 300, seed=3)
+    labels.fill_(-1)
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    assert not loss.any() and not dx.any() and not dW.any()
+
+
+def test_large_logits():
+    """Logits of some thousands, where exp of them would overflow, and a label that has all the mass."""
+    x, W, labels, dloss = inputs(100, 64, 999, seed=4, spread=2000.0)
+    X, WW = f64(x), f64(W)
+    labels = torch.from_numpy((X @ WW.T).argmax(1)).to(DEV)
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    want, wlse = O.head_loss_forward(X, WW, labels.cpu().numpy())
+    bar = noise_of(X, WW) + 60 * U24 * (1 + np.abs(wlse))
+    assert np.all(np.abs(f64(lse) - wlse) <= bar) and np.all(np.abs(f64(loss) - want) <= 2 * bar)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    assert torch.isfinite(dx).all() and torch.isfinite(dW).all()
+
+
+def test_a_token_that_is_not_finite_keeps_to_itself():
+    x, W, labels, dloss = inputs(70, 64, 300, seed=5)
+    labels[:] = 7
+    want = qg.head_loss_forward(x, W, labels)[0]
+    x[10, 3] = float("nan")
+    loss, _ = qg.head_loss_forward(x, W, labels)
+    assert torch.isnan(loss[10])
+    others = torch.arange(70, device=DEV) != 10
+    assert torch.equal(loss[others], want[others])
+
+
+def test_gradient_against_differences_of_the_forward_kernel():
+    """Along random directions of x and W, from losses in fp32: truncation is of third order in the step."""
+    x, W, labels, dloss = inputs(64, 128, 1000, seed=6)
+    _, lse = qg.head_loss_forward(x, W, labels)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    g = torch.Generator().manual_seed(7)
+    f = lambda a, b: float((dloss.double() * qg.head_loss_forward(a, b, labels)[0].double()).sum())
+    for which, grad in ((0, dx), (1, dW)):
+        base = (x, W)[which].float()
+        e = torch.randn(base.shape, generator=g).to(DEV) * base.std() / 32
+        plus, minus = (base + e).bfloat16(), (base - e).bfloat16()
+        moved = plus.double() - minus.double()
+        diff = f(plus, W) - f(minus, W) if which == 0 else f(x, plus) - f(x, minus)
+        terms = grad.double() * moved
+        bar = 4 * 2.0 ** -8 * float(terms.norm()) + 16 * 128 * U24 * 64 ** 0.5 + 2e-3 * float(terms.abs().sum()) ** 0.5
+        assert abs(diff - float(terms.sum())) <= bar
+
+
+def test_row_pitch():
+    tokens, h, vocab, ld = 70, 521, 1000, 528
+    x, W, labels, dloss = inputs(tokens, h, vocab, seed=8)
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+
+    def pad(t):
+        p = torch.full((t.shape[0], ld), float("nan"), dtype=t.dtype, device=DEV)
+        p[:, :h] = t
+        return p
+    xp, Wp, dxp, dWp = pad(x), pad(W), pad(x), pad(W)
+    L, at, st = qg.lib(), (lambda t: t.data_ptr()), torch.cuda.current_stream().cuda_stream
+    nbytes = L.qg_head_loss_workspace_bytes(tokens, h, vocab)
+    ws, loss2, lse2 = torch.empty(nbytes, dtype=torch.uint8, device=DEV), torch.empty_like(loss), torch.empty_like(lse)
+    assert L.qg_head_loss_forward(at(xp), at(Wp), at(labels), tokens, h, vocab, ld, at(loss2), at(lse2), at(ws), nbytes, st) == 0
+    assert L.qg_head_loss_backward(at(xp), at(Wp), at(labels), at(lse2), at(dloss), tokens, h, vocab, ld, at(dxp), at(dWp), at(ws), nbytes,
+                                   st) == 0
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    for p, t in ((dxp, dx), (dWp, dW)):
+        assert torch.equal(p[:, :h], t) and torch.isnan(p[:, h:].float()).all()
+
+
+def test_refusals():
+    x, W, labels, dloss = inputs(8, 16, 32, seed=9)
+    lse = torch.zeros(8, device=DEV)
+    for bad in (lambda: qg.head_loss_forward(x, W[:, :8].contiguous(), labels), lambda: qg.head_loss_forward(x, W, labels[:7]),
+                lambda: qg.head_loss_forward(x, W, labels.int()), lambda: qg.head_loss_forward(x.float(), W, labels),
+                lambda: qg.head_loss_forward(x[:0], W, labels[:0]), lambda: qg.head_loss_forward(x, W[:, ::2], labels),
+                lambda: qg.head_loss_forward(x, W, labels, workspace=torch.empty(16, dtype=torch.uint8, device=DEV)),
+                lambda: qg.head_loss_backward(x, W, labels, lse[:4], dloss), lambda: qg.head_loss_backward(x, W, labels, lse, dloss.double()),
+                lambda: qg.head_loss_backward(x, W, labels, lse, dloss, want_dx=False, want_dW=False)):
+        with pytest.raises(qg.QGError):
+            bad()
+
+
+def test_another_stream_and_capture():
+    x, W, labels, dloss = inputs(300, 40, 20001, seed=10)
+    ws = torch.empty(qg.lib().qg_head_loss_workspace_bytes(300, 40, 20001), dtype=torch.uint8, device=DEV)
+
+    def both():
+        loss, lse = qg.head_loss_forward(x, W, labels, workspace=ws)
+        return (loss, lse) + qg.head_loss_backward(x, W, labels, lse, dloss, workspace=ws)
+    want = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = both()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

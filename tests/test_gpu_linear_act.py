@@ -1,0 +1,263 @@
+"""The INT8 linear layer with an epilogue and the gated pair against the fp64 reference (oracle/layers.py), on the weights that the
+library's products see (dequantized and rounded to bf16) and the decoded activations.
+
+Bars, per element.  Every output is rounded once from fp32: half a bf16 spacing, 2^-8 of it at most.  fp32 sums of K products: 4 K 2^-24
+of the root of their squares' sum is far above what such sums lose.  The backward products take dz rounded to bf16, each term off by at
+most 2^-8 of itself independently: the bar is six standard deviations, 4 * 2^-8 of the root of the terms' squares' sum.  The gelu's cdf is
+good to 1.5e-7 absolutely, which a factor z or zu scales."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers as O
+from oracle import qgalore as Q
+from paper_2407_08296_amd import qgalore as qg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U24 = 2.0 ** -24
+
+# (tokens, m, n): one token, one element, ragged and odd everything, around the tiles and the split contraction, 256 x 256 tiles
+CASES = [(1, 1, 1), (3, 5, 7), (1, 2050, 768), (33, 64, 130), (130, 333, 264), (77, 200, 521), (64, 519, 256), (200, 2112, 65),
+         (500, 1100, 600), (2100, 600, 200), (1200, 5000, 72), (4096, 4096, 64), (4100, 4111, 72)]
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def normal(g, *shape, std=1.0):
+    return (torch.randn(*shape, generator=g) * std).bfloat16().to(DEV)
+
+
+def weight(g, m, n):
+    q, s = qg.quant_int8((torch.randn(m, n, generator=g) * 0.02).to(DEV))
+    return (q, s), Q.dequant_w_bf16(q.cpu().numpy(), s.cpu().numpy())
+
+
+def rss(a, b):
+    return np.sqrt((a * a) @ (b * b))
+
+
+def check(got, want, noise):
+    err = np.abs(f64(got) - want)
+    bar = 2.0 ** -8 * np.abs(want) + noise
+    assert got.dtype is torch.bfloat16 and got.shape == want.shape and np.all(err <= bar), float(np.max(err - bar))
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("tokens,m,n", CASES)
+def test_act_forward(tokens, m, n, act):
+    g = torch.Generator().manual_seed(tokens + m + n)
+    w, W = weight(g, m, n)
+    x, bias, res = normal(g, tokens, n), normal(g, m), normal(g, tokens, m)
+    X = f64(x)
+    noise = 4 * n * U24 * rss(X, W.T) + 1e-30
+    for b, r in ((bias, res), (None, None), (bias, None)):
+        y, z = qg.int8_linear_act_forward(x, *w, bias=b, residual=r, act=act, want_z=True)
+        wy, wz = O.linear_act_forward(X, W, f64(b), f64(r), act)
+        check(z, wz, noise + 4 * U24 * np.abs(wz))
+        # act' stays below 1.2; the activation's own error, and the residual's addition
+        check(y, wy, 1.2 * (noise + 4 * U24 * np.abs(wz)) + (3e-7 + 8 * U24) * np.abs(wz) + 2 * U24 * np.abs(wy))
+        alone, none = qg.int8_linear_act_forward(x, *w, bias=b, residual=r, act=act)
+        assert none is None and torch.equal(alone, y)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("tokens,m,n", CASES)
+def test_act_backward(tokens, m, n, act):
+    g = torch.Generator().manual_seed(tokens + m + n + 1)
+    w, W = weight(g, m, n)
+    x, dy, z = normal(g, tokens, n), normal(g, tokens, m, std=0.05), normal(g, tokens, m, std=2.0)
+    X, DY, Z = f64(x), f64(dy), f64(z)
+    dx, G, db = qg.int8_linear_act_backward(dy, None if act == "none" else z, x, *w, act=act, want_dbias=True)
+    dz = DY if act == "none" else DY * O.act(Z, act)[1]
+    want = O.linear_act_backward(DY, Z, X, W, act)
+    rounded = 0.0 if act == "none" else 4 * 2.0 ** -8      # dy itself is exact
+    check(dx, want[0], (rounded + 4 * m * U24) * rss(dz, W) + 1e-6 * rss(DY, W))
+    check(G, want[1], (rounded + 4 * tokens * U24) * rss(dz.T, X) + 1e-6 * rss(DY.T, X))
+    assert np.all(np.abs(f64(db) - want[2]) <= 8 * (1 + np.sqrt(tokens)) * U24 * np.abs(dz).sum(0) + 5e-7 * np.abs(DY).sum(0))
+    # each output alone: the same bits
+    zz = None if act == "none" else z
+    assert torch.equal(qg.int8_linear_act_backward(dy, zz, x, *w, act=act, want_G=False)[0], dx)
+    assert torch.equal(qg.int8_linear_act_backward(dy, zz, x, *w, act=act, want_dx=False)[1], G)
+    assert torch.equal(qg.int8_linear_act_backward(dy, zz, x, *w, act=act, want_dx=False, want_G=False, want_dbias=True)[2], db)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("tokens,m,n", CASES)
+def test_gated_forward(tokens, m, n, act):
+    g = torch.Generator().manual_seed(tokens + m + n + 2)
+    (wg, Wg), (wu, Wu) = weight(g, m, n), weight(g, m, n)
+    x = normal(g, tokens, n)
+    X = f64(x)
+    y, zg, zu = qg.int8_gated_forward(x, *wg, *wu, act=act, want_z=True)
+    wy, wzg, wzu = O.gated_forward(X, Wg, Wu, act)
+    ng, nu = 4 * n * U24 * rss(X, Wg.T) + 1e-30, 4 * n * U24 * rss(X, Wu.T) + 1e-30
+    check(zg, wzg, ng)
+    check(zu, wzu, nu)
+    check(y, wy, 1.2 * ng * np.abs(wzu) + nu * np.abs(O.act(wzg, act)[0]) + 4e-7 * np.abs(wzg * wzu) + ng * nu)
+    alone, a, b = qg.int8_gated_forward(x, *wg, *wu, act=act)
+    assert a is None and b is None and torch.equal(alone, y)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("tokens,m,n", CASES + [(64, 5461, 256), (4096, 72, 4100), (1500, 200, 2050)])
+def test_gated_backward(tokens, m, n, act):
+    g = torch.Generator().manual_seed(tokens + m + n + 3)
+    (wg, Wg), (wu, Wu) = weight(g, m, n), weight(g, m, n)
+    x, dy, zg, zu = normal(g, tokens, n), normal(g, tokens, m, std=0.05), normal(g, tokens, m, std=2.0), normal(g, tokens, m)
+    X, DY, ZG, ZU = (f64(t) for t in (x, dy, zg, zu))
+    dx, Gg, Gu = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu, act=act)
+    want = O.gated_backward(DY, ZG, ZU, X, Wg, Wu, act)
+    a, da = O.act(ZG, act)
+    dzg, dzu = DY * ZU * da, DY * a
+    r = 4 * 2.0 ** -8
+    check(dx, want[0], (r + 4 * m * U24) * (rss(dzg, Wg) + rss(dzu, Wu)) + 1e-6 * (rss(DY * ZU, Wg) + rss(DY * ZG, Wu)))
+    check(Gg, want[1], (r + 4 * tokens * U24) * rss(dzg.T, X) + 1e-6 * rss((DY * ZU).T, X))
+    check(Gu, want[2], (r + 4 * tokens * U24) * rss(dzu.T, X) + 1e-6 * rss((DY * ZG).T, X))
+    only = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu, act=act, want_G=False)
+    assert only[1] is None and torch.equal(only[0], dx)
+    only = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu, act=act, want_dx=False)
+    assert only[0] is None and torch.equal(only[1], Gg) and torch.equal(only[2], Gu)
+
+
+def test_without_an_epilogue_it_is_the_plain_layer():
+    g = torch.Generator().manual_seed(9)
+    for tokens, m, n in CASES:
+        w, W = weight(g, m, n)
+        x, bias = normal(g, tokens, n), normal(g, m)
+        y, z = qg.int8_linear_act_forward(x, *w, bias=bias, want_z=True)
+        assert torch.equal(y, z)
+        # another tile may add the contraction in another order: within the spacing that the noise can move a rounding by
+        a, b = f64(y), f64(qg.int8_linear_forward(x, *w, bias))
+        assert np.all(np.abs(a - b) <= 2.0 ** -7 * np.maximum(np.abs(a), np.abs(b)) + 8 * n * U24 * rss(f64(x), W.T))
+
+
+def test_activations_at_the_ends_of_the_range():
+    """Values where the exponential overflows or vanishes, infinities and NaN, against torch in fp64."""
+    z = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 20.0, -20.0, 100.0, -100.0, 3e38, -3e38, float("inf"), float("nan")]).bfloat16().to(DEV)
+    m = len(z)
+    eye, s = qg.quant_int8(torch.eye(m, device=DEV))
+    dy = torch.ones(1, m, dtype=torch.bfloat16, device=DEV)
+    for name, f in (("relu", torch.relu), ("silu", torch.nn.functional.silu), ("gelu", torch.nn.functional.gelu)):
+        d = z.double().requires_grad_()
+        f(d).sum().backward()
+        _, _, db = qg.int8_linear_act_backward(dy, z[None].contiguous(), dy, eye, s, act=name, want_dx=False, want_G=False, want_dbias=True)
+        want = d.grad
+        fine = torch.isfinite(z.double())
+        assert torch.allclose(db.double()[fine], want[fine], atol=1e-6, rtol=1e-6), name
+        assert torch.isnan(db[-1]) or name == "relu"
+        x = torch.zeros(1, m, dtype=torch.bfloat16, device=DEV)
+        y = qg.int8_linear_act_forward(x, eye, s, bias=z, act=name)[0][0].double()
+        assert torch.allclose(y[fine], f(z.double())[fine], atol=1e-6, rtol=2.0 ** -8), name
+        assert y[-2] == float("inf") and torch.isnan(y[-1])
+
+
+def test_row_pitch_in_place_and_padding():
+    tokens, m, n, ld_m, ld_n = 100, 5461 // 8, 521, 688, 528
+    g = torch.Generator().manual_seed(10)
+    (wg, _), (wu, _) = weight(g, m, n), weight(g, m, n)
+    x, bias, res, dy, zu = normal(g, tokens, n), normal(g, m), normal(g, tokens, m), normal(g, tokens, m), normal(g, tokens, m)
+
+    def pad(t, ld):
+        p = torch.full((t.shape[0], ld), 77 if t.dtype is torch.int8 else float("nan"), dtype=t.dtype, device=DEV)
+        p[:, :t.shape[1]] = t
+        return p
+    L, at, st = qg.lib(), (lambda t: t.data_ptr()), torch.cuda.current_stream().cuda_stream
+    xp, wgp, wup = pad(x, ld_n), pad(wg[0], ld_n), pad(wu[0], ld_n)
+    want, wz = qg.int8_linear_act_forward(x, *wg, bias=bias, residual=res, act="gelu", want_z=True)
+    y, z = pad(res, ld_m), pad(res, ld_m)                     # y on top of the residual
+    assert L.qg_int8_linear_act_forward(at(xp), at(wgp), at(wg[1]), at(bias), at(y), 3, tokens, m, n, ld_n, ld_m, 256, at(z), at(y), st) == 0
+    close = lambda a, b, ld: bool(((a[:, :b.shape[1]].float() - b.float()).abs() <= 2.0 ** -6 * b.float().abs() + 1e-4).all()) and \
+        bool(torch.isnan(a[:, b.shape[1]:].float()).all())
+    assert close(y, want, ld_m) and close(z, wz, ld_m)
+    dx, G, db = qg.int8_linear_act_backward(dy, wz, x, *wg, act="gelu", want_dbias=True)
+    dyp, zp, dxp, Gp, dbp = pad(dy, ld_m), pad(wz, ld_m), pad(x, ld_n), pad(G, ld_n), torch.empty(m, device=DEV)
+    nbytes = L.qg_int8_linear_act_workspace_bytes(tokens, m)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    assert L.qg_int8_linear_act_backward(at(dyp), at(zp), at(xp), at(wgp), at(wg[1]), 3, tokens, m, n, ld_n, ld_m, 256, at(dyp), at(dxp),
+                                         at(Gp), at(dbp), at(ws), nbytes, st) == 0       # dz on top of dy
+    assert close(dxp, dx, ld_n) and close(Gp, G, ld_n) and torch.equal(dbp, db)
+    want, zg, zu = qg.int8_gated_forward(x, *wg, *wu, want_z=True)
+    yp, zgp, zup = pad(res, ld_m), pad(res, ld_m), pad(res, ld_m)
+    assert L.qg_int8_gated_forward(at(xp), at(wgp), at(wg[1]), at(wup), at(wu[1]), 2, tokens, m, n, ld_n, ld_m, 256, at(zgp), at(zup), at(yp),
+                                   st) == 0
+    assert close(yp, want, ld_m) and close(zgp, zg, ld_m) and close(zup, zu, ld_m)
+    dx, Gg, Gu = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu)
+    dyp, zgp, zup, Ggp, Gup = pad(dy, ld_m), pad(zg, ld_m), pad(zu, ld_m), pad(Gg, ld_n), pad(Gu, ld_n)
+    assert L.qg_int8_gated_backward(at(dyp), at(zgp), at(zup), at(xp), at(wgp), at(wg[1]), at(wup), at(wu[1]), 2, tokens, m, n, ld_n, ld_m,
+                                    256, at(zgp), at(zup), at(dxp), at(Ggp), at(Gup), st) == 0
+    assert close(dxp, dx, ld_n) and close(Ggp, Gg, ld_n) and close(Gup, Gu, ld_n)
+
+
+def test_gradient_against_differences_of_the_forward_kernel():
+    """sum(c y) along a random direction of x; y is rounded to bf16, so the step is long and the bar is its noise."""
+    g = torch.Generator().manual_seed(11)
+    tokens, m, n = 64, 512, 256
+    (wg, _), (wu, _) = weight(g, m, n), weight(g, m, n)
+    x = normal(g, tokens, n)
+    c = normal(g, tokens, m)
+    e = normal(g, tokens, n)
+    step = 1.0 / 16
+    plus, minus = (x.float() + step * e.float()).bfloat16(), (x.float() - step * e.float()).bfloat16()
+    moved = (plus.double() - minus.double())
+    for forward, backward in (
+        (lambda v: qg.int8_linear_act_forward(v, *wg, act="gelu", want_z=True),
+         lambda out: qg.int8_linear_act_backward(c, out[1], x, *wg, act="gelu")[0]),
+        (lambda v: qg.int8_gated_forward(v, *wg, *wu, want_z=True),
+         lambda out: qg.int8_gated_backward(c, out[1], out[2], x, *wg, *wu)[0])):
+        diff = float((c.double() * (forward(plus)[0].double() - forward(minus)[0].double())).sum())
+        want = float((backward(forward(x)).double() * moved).sum())
+        y = forward(x)[0].double()
+        noise = 6 * 2.0 ** -8 * float((c.double() * y).norm())          # both sides' roundings
+        curve = 0.02 * float((backward(forward(x)).double() * moved).norm()) * tokens ** 0.5     # third derivative times step^2 / 6
+        assert abs(diff - want) <= noise + curve
+
+
+def test_refusals():
+    g = torch.Generator().manual_seed(12)
+    w, _ = weight(g, 64, 48)
+    w2, _ = weight(g, 64, 32)
+    x, dy = normal(g, 4, 48), normal(g, 4, 64)
+    for bad in (lambda: qg.int8_linear_act_forward(x, *w, act="swish"),
+                lambda: qg.int8_linear_act_forward(x, *w2),                               # another n
+                lambda: qg.int8_linear_act_forward(x, *w, bias=dy[0, :32]),
+                lambda: qg.int8_linear_act_forward(x, *w, residual=dy[:3]),
+                lambda: qg.int8_linear_act_forward(x.float(), *w),
+                lambda: qg.int8_linear_act_forward(x[:0], *w),                            # no tokens
+                lambda: qg.int8_linear_act_backward(dy, None, x, *w, act="silu"),         # z missing
+                lambda: qg.int8_linear_act_backward(dy, dy, x, *w, want_dx=False, want_G=False),
+                lambda: qg.int8_gated_forward(x, *w, *w2),
+                lambda: qg.int8_gated_backward(dy, dy, dy[:3], x, *w, *w),
+                lambda: qg.int8_gated_backward(dy, dy, dy, x, *w, *w, want_dx=False, want_G=False)):
+        with pytest.raises(qg.QGError):
+            bad()
+
+
+def test_another_stream_and_capture():
+    g = torch.Generator().manual_seed(13)
+    (wg, _), (wu, _) = weight(g, 512, 256), weight(g, 512, 256)
+    x, dy = normal(g, 130, 256), normal(g, 130, 512)
+
+    def all_of_it():
+        y, zg, zu = qg.int8_gated_forward(x, *wg, *wu, want_z=True)
+        a, z = qg.int8_linear_act_forward(x, *wg, act="gelu", want_z=True)
+        return (y, zg, zu, a, z) + qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu) + \
+            qg.int8_linear_act_backward(dy, z, x, *wg, act="gelu", want_dbias=True)
+    want = all_of_it()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = all_of_it()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = all_of_it()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
