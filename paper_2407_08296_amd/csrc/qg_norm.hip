@@ -16,16 +16,23 @@ constexpr int kNormMaxD = 16384;
 constexpr int64_t kNormMaxTokens = int64_t(1) << 22;   // (a workgroup of up to 1024 threads per token, 2^32 threads per launch)
 enum : int { kGateNone = QG_GATE_NONE, kGateChannel = QG_GATE_CHANNEL, kGateToken = QG_GATE_TOKEN };
 
-// 8 consecutive elements of a row, of which the first `valid` exist (the others read as 0); rows may start at any element.
-__device__ __forceinline__ void load8(const uint16_t* p, int valid, float (&v)[8]) {
+// 8 consecutive elements of a row, of which the first `valid` exist (the others read as 0); rows may start at any element.  Past
+// the end the last element is read again: the loads of a row's end are independent of each other, where seven conditional ones
+// would wait for one another (1000 rows of 2047, five arrays: 26 us of which the row ends took half).
+__device__ __forceinline__ u32x4 load8_raw(const uint16_t* p, int valid) {
+    if (valid >= 8) return *reinterpret_cast<const u32x4_align2*>(p);
     u32x4 w = {0u, 0u, 0u, 0u};
-    if (valid >= 8) {
-        w = *reinterpret_cast<const u32x4_align2*>(p);
-    } else {
+    if (valid > 0) {
+        uint32_t e[7];
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < valid) w[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+        for (int j = 0; j < 7; ++j) e[j] = p[min(j, valid - 1)];
+#pragma unroll
+        for (int j = 0; j < 7; ++j) w[j >> 1] |= j < valid ? e[j] << (16 * (j & 1)) : 0u;
     }
+    return w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int valid, float (&v)[8]) {
+    const u32x4 w = load8_raw(p, valid);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[2 * j] = __builtin_bit_cast(float, w[j] << 16);
@@ -41,8 +48,12 @@ __device__ __forceinline__ void load8(const float* p, int valid, float (&v)[8]) 
             v[4 + j] = __builtin_bit_cast(float, (uint32_t)b[j]);
         }
     } else {
+        float e[7] = {};
+        if (valid > 0)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < valid ? p[j] : 0.f;
+            for (int j = 0; j < 7; ++j) e[j] = p[min(j, valid - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < valid ? e[min(j, 6)] : 0.f;
     }
 }
 __device__ __forceinline__ void store8(uint16_t* p, int valid, const float (&v)[8]) {
@@ -72,27 +83,75 @@ __device__ __forceinline__ void store8(float* p, int valid, const float (&v)[8])
     }
 }
 
-// Sums of N values over the WPR waves that share a row, the same value in every lane; `slot`: WPR * N floats of LDS, a set of
-// its own for each of two calls in a row.  A fixed order: the result does not depend on timing.
+// Sum over the 64 lanes, the same in each, without LDS: neighbours, quads and halves of 16 lanes by data-parallel moves, then the 16s
+// and 32s swapped.
+__device__ __forceinline__ float lanes_sum(float v) {
+    auto moved = [&](auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    v += moved(std::integral_constant<int, 0xB1>());    // lane ^ 1
+    v += moved(std::integral_constant<int, 0x4E>());    // lane ^ 2
+    v += moved(std::integral_constant<int, 0x141>());   // the 8 lanes mirrored
+    v += moved(std::integral_constant<int, 0x140>());   // the 16 lanes mirrored
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    v = __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+    const uint32_t c = __builtin_bit_cast(uint32_t, v);
+    const auto u = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return __builtin_bit_cast(float, (uint32_t)u[0]) + __builtin_bit_cast(float, (uint32_t)u[1]);
+}
+
+// Sums of N values over the WPR waves that share a row, the same value in every lane; `slot`: N floats of LDS per wave of the
+// workgroup, another set than that of the call before.  A fixed order: the result does not depend on timing.
 template <int N, int WPR>
 __device__ __forceinline__ void row_sums(float (&s)[N], float* slot) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    for (int i = 0; i < N; ++i) s[i] = lanes_sum(s[i]);
     if constexpr (WPR > 1) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0)
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave / WPR * WPR;
+        if (lane == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) slot[wave * N + i] = s[i];
         __syncthreads();
+        // lane l takes wave l's sums, zero beyond the last; all lanes add
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float t = slot[i];
-#pragma unroll
-            for (int w = 1; w < WPR; ++w) t += slot[w * N + i];
-            s[i] = t;
-        }
+        for (int i = 0; i < N; ++i) s[i] = lanes_sum(lane < WPR ? slot[(first + min(lane, WPR - 1)) * N + i] : 0.f);
     }
 }
+
+// 8 elements as they come from memory, kept so between their two uses.
+template <typename S>
+struct Raw8 {
+    u32x4 w[sizeof(S) / 2];
+    __device__ __forceinline__ void load(const S* p, int valid) {
+        if constexpr (sizeof(S) == 2) {
+            w[0] = load8_raw(p, valid);
+        } else if (valid >= 8) {
+            w[0] = *reinterpret_cast<const u32x4_align4*>(p);
+            w[1] = *reinterpret_cast<const u32x4_align4*>(p + 4);
+        } else {
+            float e[8];
+            load8(p, valid, e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j / 4][j % 4] = __builtin_bit_cast(uint32_t, e[j]);
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(S) / 2; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+    // a use of the words from here on converts them again, instead of keeping what was converted before
+    __device__ __forceinline__ void again() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(S) / 2; ++i) asm("" : "+v"(w[i]));
+    }
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (sizeof(S) == 2)
+            return __builtin_bit_cast(float, j & 1 ? (uint32_t)w[0][j >> 1] & 0xFFFF0000u : (uint32_t)w[0][j >> 1] << 16);
+        else
+            return __builtin_bit_cast(float, (uint32_t)w[j / 4][j % 4]);
+    }
+};
 
 struct NormArgs {
     int64_t tokens, ld;            // ld: row pitch of every [tokens][d] array
@@ -171,117 +230,157 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void k_residual_norm_fwd
 }
 
 // The sums over a row that dh and dy need are all known ahead of dh: mean(k dh y) is linear in dh = dh' + r a - r c h', so
-// one reduction of six sums serves both norms.  A workgroup goes over `per` rows and keeps the columns' sums over them in
-// registers: dw_pre's, and E = sum_t dh y q (times the gate where that is per token), of which dw_post and a channel's dgate
-// are multiples.
-template <typename S, int WPR, int CH>
-__global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void k_residual_norm_bwd(
+// one reduction of six sums serves both norms.  A workgroup has ROWS rows at a time, `per` times, and keeps the columns' sums over
+// them in registers: dw_pre's, and E = sum_t dh y q (times the gate where that is per token), of which dw_post and a channel's dgate
+// are multiples.  At its end the ROWS sums are added in order.
+// CH == 1 (rows of up to 8192): the vectors stay in registers; with two chunks per lane there are none left for them.  (Fetching the
+// next rows ahead of the present ones' sums as well: 8192 x 4096 the same, 4096 x 2048 with a gate per token 65 us against 38, for the
+// registers that it spills.)
+template <typename S, int WPR, int CH, int ROWS, bool TOKEN_GATE>
+__global__ __launch_bounds__(64 * WPR * ROWS, 4) void k_residual_norm_bwd(
     NormArgs a, const uint16_t* __restrict__ du, const S* dh_next, const S* __restrict__ h, const uint16_t* __restrict__ y, S* dh,
-    uint16_t* __restrict__ dy, uint16_t* __restrict__ dgate, float* __restrict__ part, int64_t per) {
-    constexpr int NT = 64 * WPR, WAVES = WPR == 1 ? 4 : WPR;
-    __shared__ float slots[2][WPR * 6];
-    const int tid = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    uint16_t* __restrict__ dy, uint16_t* __restrict__ dgate, float* __restrict__ part, int per) {
+    constexpr int NT = 64 * WPR;
+    constexpr bool kHold = CH == 1;
+    __shared__ float slots[2][WPR * ROWS * 6];
+    const int tid = threadIdx.x % NT, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const bool post = a.w_post != nullptr, has_y = y != nullptr, has_u = du != nullptr;
     const float rd = 1.f / (float)a.d;
-    float sum_pre[CH][8], sum_e[CH][8], wk[CH][8], wp[CH][8];   // wk: scale * w_post (* gate of the channel)
+    float sum_pre[CH][8], sum_e[CH][8];
 #pragma unroll
-    for (int q = 0; q < CH; ++q) {
+    for (int q = 0; q < CH; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum_pre[q][j] = sum_e[q][j] = 0.f;
+    // wk: scale * w_post (* gate of the channel), wp: w_pre
+    auto vectors = [&](int q, float (&wk)[8], float (&wp)[8]) {
         const int c = 8 * (tid + NT * q), valid = a.d - c;
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            sum_pre[q][j] = sum_e[q][j] = 0.f;
-            wk[q][j] = a.scale;
-            wp[q][j] = 0.f;
+            wk[j] = a.scale;
+            wp[j] = 0.f;
         }
-        if (has_u) load8(a.w_pre + c, valid, wp[q]);
+        if (has_u) load8(a.w_pre + c, valid, wp);
         if (post) {
             load8(a.w_post + c, valid, g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) wk[q][j] *= g[j];
+            for (int j = 0; j < 8; ++j) wk[j] *= g[j];
         }
         if (a.gate_kind == kGateChannel) {
             load8(static_cast<const float*>(a.gate) + c, valid, g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) wk[q][j] *= g[j];
+            for (int j = 0; j < 8; ++j) wk[j] *= g[j];
         }
-    }
-    const int64_t first = ((int64_t)blockIdx.x * (WPR == 1 ? 4 : 1) + (WPR == 1 ? threadIdx.x >> 6 : 0)) * per;
-    const int64_t last = min(first + per, a.tokens);
-    for (int64_t t = first; t < last; ++t) {
+    };
+    struct Row {
+        Raw8<S> h[CH], d[CH];
+        Raw8<uint16_t> u[CH], y[CH], g[TOKEN_GATE ? CH : 1];
+    };
+    auto fetch = [&](Row& w, int64_t t) {
         const int64_t row = t * a.ld;
-        float hv[CH][8], uv[CH][8], dv[CH][8], yv[CH][8], gv[CH][8];
 #pragma unroll
         for (int q = 0; q < CH; ++q) {
-            const int c = 8 * (tid + NT * q), valid = a.d - c;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) hv[q][j] = uv[q][j] = dv[q][j] = yv[q][j] = 0.f;
+            const int c = 8 * (tid + NT * q), valid = t < a.tokens ? a.d - c : 0;   // past the end: zeros, which add nothing
             if (has_u) {
-                load8(h + row + c, valid, hv[q]);
-                load8(du + row + c, valid, uv[q]);
+                w.h[q].load(h + row + c, valid);
+                w.u[q].load(du + row + c, valid);
+            } else {
+                w.h[q].zero();
+                w.u[q].zero();
             }
-            if (dh_next != nullptr) load8(dh_next + row + c, valid, dv[q]);
-            if (has_y) load8(y + row + c, valid, yv[q]);
-            if (a.gate_kind == kGateToken) load8(static_cast<const uint16_t*>(a.gate) + row + c, valid, gv[q]);
+            if (dh_next != nullptr) w.d[q].load(dh_next + row + c, valid);
+            else w.d[q].zero();
+            if (has_y) w.y[q].load(y + row + c, valid);
+            else w.y[q].zero();
+            if constexpr (TOKEN_GATE) w.g[q].load(static_cast<const uint16_t*>(a.gate) + row + c, valid);
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * per * ROWS + sub;
+    Row w;
+    fetch(w, first);                                       // ahead of the vectors: one latency for both
+    float held_k[8], held_p[8];
+    if constexpr (kHold) vectors(0, held_k, held_p);
+    auto compute = [&](Row& w, int64_t t, float* slot) {
+        const int64_t row = t * a.ld;
         float s[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // h h, a h, y y, k y dh', k y a, k y h
 #pragma unroll
-        for (int q = 0; q < CH; ++q)
+        for (int q = 0; q < CH; ++q) {
+            float wk[8], wp[8];
+            if constexpr (!kHold) vectors(q, wk, wp);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float hh = hv[q][j], av = uv[q][j] * wp[q][j], yy = yv[q][j];
-                const float ky = yy * wk[q][j] * (a.gate_kind == kGateToken ? gv[q][j] : 1.f);
+                const float hh = w.h[q][j], av = w.u[q][j] * (kHold ? held_p[j] : wp[j]), yy = w.y[q][j];
+                float ky = yy * (kHold ? held_k[j] : wk[j]);
+                if constexpr (TOKEN_GATE) ky *= w.g[q][j];
                 s[0] = __builtin_fmaf(hh, hh, s[0]);
                 s[1] = __builtin_fmaf(av, hh, s[1]);
                 s[2] = __builtin_fmaf(yy, yy, s[2]);
-                s[3] = __builtin_fmaf(ky, dv[q][j], s[3]);
+                s[3] = __builtin_fmaf(ky, w.d[q][j], s[3]);
                 s[4] = __builtin_fmaf(ky, av, s[4]);
                 s[5] = __builtin_fmaf(ky, hh, s[5]);
             }
-        row_sums<6, WPR>(s, slots[t & 1]);
+        }
+        row_sums<6, WPR>(s, slot);
+#pragma unroll
+        for (int q = 0; q < CH; ++q) {
+            w.h[q].again();
+            w.d[q].again();
+            w.u[q].again();
+            w.y[q].again();
+            if constexpr (TOKEN_GATE) w.g[q].again();
+        }
         const float r = has_u ? 1.f / sqrtf(s[0] * rd + a.eps) : 0.f, qi = post ? 1.f / sqrtf(s[2] * rd + a.eps) : 1.f;
-        const float c1 = r * r * s[1] * rd;                                        // dh = dh' + r (a - c1 h')
+        const float c1 = r * r * s[1] * rd;                                             // dh = dh' + r (a - c1 h')
         const float c2 = post ? qi * qi * rd * (s[3] + r * (s[4] - c1 * s[5])) : 0.f;   // dy = q (k dh - c2 y)
 #pragma unroll
         for (int q = 0; q < CH; ++q) {
-            const int c = 8 * (tid + NT * q), valid = a.d - c;
-            float o[8], p[8], e[8];
+            const int c = 8 * (tid + NT * q), valid = t < a.tokens ? a.d - c : 0;
+            float wk[8], wp[8], o[8], p[8], e[8];
+            if constexpr (!kHold) vectors(q, wk, wp);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float gt = a.gate_kind == kGateToken ? gv[q][j] : 1.f;
-                sum_pre[q][j] = __builtin_fmaf(uv[q][j] * hv[q][j], r, sum_pre[q][j]);
-                o[j] = __builtin_fmaf(r, __builtin_fmaf(-c1, hv[q][j], uv[q][j] * wp[q][j]), dv[q][j]);
-                p[j] = qi * __builtin_fmaf(-c2, yv[q][j], wk[q][j] * gt * o[j]);
-                const float x = o[j] * yv[q][j] * qi;
-                e[j] = wk[q][j] * x;
+                float gt = 1.f;
+                if constexpr (TOKEN_GATE) gt = w.g[q][j];
+                const float uu = w.u[q][j], hh = w.h[q][j], yy = w.y[q][j], k = kHold ? held_k[j] : wk[j];
+                sum_pre[q][j] = __builtin_fmaf(uu * hh, r, sum_pre[q][j]);
+                o[j] = __builtin_fmaf(r, __builtin_fmaf(-c1, hh, uu * (kHold ? held_p[j] : wp[j])), w.d[q][j]);
+                p[j] = qi * __builtin_fmaf(-c2, yy, k * gt * o[j]);
+                const float x = o[j] * yy * qi;
+                e[j] = k * x;
                 sum_e[q][j] = __builtin_fmaf(x, gt, sum_e[q][j]);
             }
             store8(dh + row + c, valid, o);
             if (has_y) store8(dy + row + c, valid, p);
-            if (dgate != nullptr) store8(dgate + row + c, valid, e);
+            if constexpr (TOKEN_GATE)
+                if (dgate != nullptr) store8(dgate + row + c, valid, e);
         }
+    };
+    for (int i = 0; i < per; ++i) {
+        const int64_t t = first + (int64_t)i * ROWS;
+        compute(w, t, slots[i & 1]);
+        if (i + 1 < per) fetch(w, t + ROWS);
     }
     if (part == nullptr) return;
-    if constexpr (WPR == 1) {   // the workgroup's four waves: their columns' sums through LDS, added in order
-        __shared__ float sums[WAVES][2 * 512 * CH];
-        const int wave = threadIdx.x >> 6;
+    if constexpr (ROWS > 1) {
+        __shared__ float sums[ROWS - 1][2 * 8 * CH * NT];
+        if (sub != 0)
 #pragma unroll
-        for (int q = 0; q < CH; ++q)
+            for (int q = 0; q < CH; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sums[wave][(q * 8 + j) * 64 + tid] = sum_pre[q][j];
-                sums[wave][((CH + q) * 8 + j) * 64 + tid] = sum_e[q][j];
-            }
+                for (int j = 0; j < 8; ++j) {
+                    sums[sub - 1][(q * 8 + j) * NT + tid] = sum_pre[q][j];
+                    sums[sub - 1][((CH + q) * 8 + j) * NT + tid] = sum_e[q][j];
+                }
         __syncthreads();
-        if (wave != 0) return;
+        if (sub != 0) return;
 #pragma unroll
         for (int q = 0; q < CH; ++q)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int w = 1; w < 4; ++w) {
-                    sum_pre[q][j] += sums[w][(q * 8 + j) * 64 + tid];
-                    sum_e[q][j] += sums[w][((CH + q) * 8 + j) * 64 + tid];
+                for (int w = 0; w < ROWS - 1; ++w) {
+                    sum_pre[q][j] += sums[w][(q * 8 + j) * NT + tid];
+                    sum_e[q][j] += sums[w][((CH + q) * 8 + j) * NT + tid];
                 }
     }
 #pragma unroll
@@ -293,22 +392,27 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void k_residual_norm_bwd
     }
 }
 
-// Columns' sums over the workgroups' partial ones, in a fixed order: 64 columns of a row of 2 d per workgroup, 16 waves.
+// Columns' sums over the workgroups' partial ones, in a fixed order: 32 of the 2 d columns per workgroup, 32 slices of the groups.
 __global__ __launch_bounds__(1024) void k_residual_norm_cols(NormArgs a, const float* __restrict__ part, int groups, bool has_u, bool has_y,
                                                              float* __restrict__ dw_pre, float* __restrict__ dw_post,
                                                              float* __restrict__ dgate) {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * 64 + lane;                       // below d: dw_pre's, then E's
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + lane;                       // below d: dw_pre's, then E's
     const bool mine = col < 2 * a.d && (col < a.d ? has_u : has_y);
     float s = 0.f;
-    if (mine)
-        for (int g = wave; g < groups; g += 16) s += part[(int64_t)g * 2 * a.d + col];
-    sums[wave][lane] = s;
+    if (mine) {
+        const float* p = part + col;
+        const int64_t step = (int64_t)32 * 2 * a.d;
+        p += (int64_t)slice * 2 * a.d;
+#pragma unroll 8
+        for (int g = slice; g < groups; g += 32, p += step) s += *p;
+    }
+    sums[slice][lane] = s;
     __syncthreads();
-    if (wave != 0 || !mine) return;
+    if (slice != 0 || !mine) return;
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    for (int w = 1; w < 32; ++w) s += sums[w][lane];
     if (col < a.d) {
         if (dw_pre != nullptr) dw_pre[col] = s;
     } else {
@@ -331,16 +435,28 @@ static void norm_shape(int64_t d, F f) {
     else if (d <= 8192) f(integral_constant<int, 8>(), integral_constant<int, 2>());
     else f(integral_constant<int, 16>(), integral_constant<int, 2>());
 }
+// ... of the backward pass: f(waves per row, chunks per lane, rows per workgroup).
+template <typename F>
+static void norm_bwd_shape(int64_t d, F f) {
+    using std::integral_constant;
+    if (d <= 512) f(integral_constant<int, 1>(), integral_constant<int, 1>(), integral_constant<int, 8>());
+    else if (d <= 1024) f(integral_constant<int, 2>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+    else if (d <= 2048) f(integral_constant<int, 4>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+    else if (d <= 4096) f(integral_constant<int, 8>(), integral_constant<int, 1>(), integral_constant<int, 2>());
+    else if (d <= 8192) f(integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 1>());
+    else f(integral_constant<int, 16>(), integral_constant<int, 2>(), integral_constant<int, 1>());
+}
 
-// Workgroups of the backward pass and the rows that a row's waves take in turn.
+// Workgroups of the backward pass and the rows that they take in turn.
 struct NormSplit {
-    int64_t per;
-    int groups;
+    int per, groups;
 };
 static NormSplit norm_split(int64_t tokens, int64_t d) {
-    const int64_t rows = d <= 1024 ? 4 : 1, most = 512;
+    int64_t rows = 1;
+    norm_bwd_shape(d, [&](auto, auto, auto r) { rows = r.value; });
+    const int64_t most = 256;
     const int64_t per = (tokens + rows * most - 1) / (rows * most);
-    return {per, (int)((tokens + rows * per - 1) / (rows * per))};
+    return {(int)per, (int)((tokens + rows * per - 1) / (rows * per))};
 }
 
 static int check_norm(int64_t tokens, int64_t d, int64_t& ld) {
@@ -406,19 +522,18 @@ extern "C" int qg_residual_norm_backward(const uint16_t* du_bf16, const void* dh
     const NormSplit split = norm_split(tokens, d);
     float* part = cols ? static_cast<float*>(workspace) : nullptr;
     uint16_t* dgate_tokens = gate_kind == QG_GATE_TOKEN ? static_cast<uint16_t*>(dgate) : nullptr;
-    norm_shape(d, [&](auto wpr, auto ch) {
-        const dim3 grid((unsigned)split.groups), block(wpr.value == 1 ? 256 : 64 * wpr.value);
-        if (stream_fp32)
-            hipLaunchKernelGGL((k_residual_norm_bwd<float, wpr.value, ch.value>), grid, block, 0, (hipStream_t)stream, a, du_bf16,
-                               static_cast<const float*>(dh_next), static_cast<const float*>(h_next), y_bf16, static_cast<float*>(dh),
-                               dy_bf16, dgate_tokens, part, split.per);
-        else
-            hipLaunchKernelGGL((k_residual_norm_bwd<uint16_t, wpr.value, ch.value>), grid, block, 0, (hipStream_t)stream, a, du_bf16,
-                               static_cast<const uint16_t*>(dh_next), static_cast<const uint16_t*>(h_next), y_bf16,
-                               static_cast<uint16_t*>(dh), dy_bf16, dgate_tokens, part, split.per);
+    norm_bwd_shape(d, [&](auto wpr, auto ch, auto rows) {
+        auto launch = [&](auto s, auto token) {
+            using S = decltype(s);
+            hipLaunchKernelGGL((k_residual_norm_bwd<S, wpr.value, ch.value, rows.value, token.value>), dim3((unsigned)split.groups),
+                               dim3(64 * wpr.value * rows.value), 0, (hipStream_t)stream, a, du_bf16, static_cast<const S*>(dh_next),
+                               static_cast<const S*>(h_next), y_bf16, static_cast<S*>(dh), dy_bf16, dgate_tokens, part, split.per);
+        };
+        auto pick = [&](auto s) { gate_kind == QG_GATE_TOKEN ? launch(s, std::true_type()) : launch(s, std::false_type()); };
+        stream_fp32 ? pick(float()) : pick(uint16_t());
     });
     if (cols)
-        hipLaunchKernelGGL(k_residual_norm_cols, dim3((unsigned)((2 * d + 63) / 64)), dim3(1024), 0, (hipStream_t)stream, a, part,
+        hipLaunchKernelGGL(k_residual_norm_cols, dim3((unsigned)((2 * d + 31) / 32)), dim3(1024), 0, (hipStream_t)stream, a, part,
                            split.groups, du_bf16 != nullptr, y_bf16 != nullptr, dw_pre, dw_post,
                            dgate_cols ? static_cast<float*>(dgate) : nullptr);
     return check_launch();

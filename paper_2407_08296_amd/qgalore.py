@@ -201,7 +201,7 @@ def _bf16_rows(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
 
 def _expect(t: torch.Tensor | None, *shape: int) -> None:
     """Refuses a tensor of another shape than the sizes handed to the library say: its kernels would read past the end."""
-    if t is not None and tuple(t.shape) != shape:
+    if t is not None and t.shape != shape:
         raise QGError(f"shape {tuple(t.shape)}, expected {shape}")
 
 
@@ -660,7 +660,7 @@ def residual_norm_forward(h: torch.Tensor, y: torch.Tensor | None = None, w_post
     elif y is None:
         out = None
     _expect(out, tokens, d)
-    u = torch.empty(tokens, d, dtype=torch.bfloat16, device=h.device) if w_pre is not None else None
+    u = _bf16_rows(h if y is None else y, tokens, d) if w_pre is not None else None
     _check(lib().qg_residual_norm_forward(_ptr(h, stype), _ptr(y, _BF16), _ptr(w_post, _F32), g, kind, _ptr(w_pre, _F32), scale, eps,
                                           tokens, d, d, fp32, _ptr(out, (h.dtype,)), _ptr(u), _stream()))
     return (h if out is None else out), u
@@ -680,14 +680,13 @@ def residual_norm_backward(du: torch.Tensor | None, dh_next: torch.Tensor | None
     if y is None:
         w_post = gate = None
     g, kind = _gate(gate, tokens, d)
-    dev = h_next.device
     dh = torch.empty_like(h_next) if out is None else out
-    dy = torch.empty(tokens, d, dtype=torch.bfloat16, device=dev) if y is not None else None
-    dw_pre = torch.empty(d, dtype=torch.float32, device=dev) if du is not None else None
-    dw_post = torch.empty(d, dtype=torch.float32, device=dev) if w_post is not None else None
+    dy = _bf16_rows(y, tokens, d) if y is not None else None
+    dw_pre = torch.empty_like(w_pre) if du is not None and w_pre is not None else None
+    dw_post = torch.empty_like(w_post) if w_post is not None else None
     dgate = torch.empty_like(gate) if gate is not None else None
     nbytes = lib().qg_residual_norm_workspace_bytes(tokens, d)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = h_next.new_empty(nbytes, dtype=torch.uint8)
     _check(lib().qg_residual_norm_backward(_ptr(du, _BF16), _ptr(dh_next, stype), _ptr(h_next, stype), _ptr(y, _BF16),
                                            _ptr(w_post, _F32), g, kind, _ptr(w_pre, _F32), scale, eps, tokens, d, d, fp32,
                                            _ptr(dh, stype), _ptr(dy), _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), _ptr(ws), nbytes,
