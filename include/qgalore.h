@@ -403,7 +403,8 @@ int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, con
 
 /* ---- Loss of a language model's head: softmax cross entropy over the vocabulary, without the logits in memory.
  * z = x W^T with x bf16 [tokens][h] and W bf16 [vocab][h]; labels int64 [tokens], a label outside [0, vocab) marks a token
- * without a loss (padding, a prompt): its loss is 0, its row of dx is 0, and it adds nothing to dW whatever its row of x holds.
+ * without a loss (padding, a prompt): its loss, lse and row of dx are 0, and it adds nothing to dW whatever its row of x holds.
+ * Such tokens take no part in the products and cost next to nothing.
  * qg_head_loss_forward:  lse = log sum_v exp z_v, loss = lse - z_label, fp32 [tokens].
  * qg_head_loss_backward: from lse and dloss (fp32 [tokens], the gradient of each token's loss: a mean's 1/count, a weight),
  *   dz = dloss (exp(z - lse) - onehot), rounded to bf16;  dx = dz W, dW = dz^T x, either may be NULL.  The vocabulary is

@@ -121,7 +121,7 @@ struct RunEpilogue : E {
 
 // z = sum + bias, y = act(z) + residual; z and residual may be missing.
 struct ActRun {
-    static constexpr bool kPair = false;
+    static constexpr bool kPair = false, kCounted = false;
     const uint16_t *bias, *residual;
     uint16_t *z, *y;
     int64_t ldc;
@@ -149,7 +149,7 @@ struct ActRun {
 
 // y = act(g) * u; g and u are stored where the backward pass will want them.
 struct GatedRun {
-    static constexpr bool kPair = true;
+    static constexpr bool kPair = true, kCounted = false;
     uint16_t *zg, *zu, *y;
     int64_t ldc;
     int kind;
@@ -167,18 +167,47 @@ struct GatedRun {
 };
 
 // ---- kernels ----
+enum : int { kDimM = 0, kDimN = 1, kDimK = 2 };
 template <typename OPB, typename EPI>
 struct EpiProduct {
     LinOperand A, A2;
     OPB B, B2;
     EPI epi;
     int M, N, K, tiles_m, tiles_n;
+    // An extent that only the device knows: *count elements along `dim`, at most what M, N or K says, and a multiple of 256 (so
+    // that tiles and steps are as whole as the host takes them to be).  The grid is the largest one's; the rest ends at once.
+    const int32_t* count = nullptr;
+    int dim = kDimM;
+    // The contraction over `splits` workgroups per tile (blockIdx.y): `k_chunk` of it each (a multiple of 64), epi.split(s) for the
+    // s-th one.
+    int splits = 1, k_chunk = 0;
 };
 
 template <int AL, int BL, bool EXACT, int MB, int TN, int BK, int WM, bool DEEP, int KG, int TERMS, typename OPB, typename EPI>
 __global__ __launch_bounds__(WM * 128 * KG, KG > 1 ? (MB == 1 ? 4 : 2) : WM == 2 ? 2 : 1) void k_gemm_epilogue(EpiProduct<OPB, EPI> p) {
     __shared__ __attribute__((aligned(16))) uint16_t smem[KG * TileGemm<AL, BL, MB, TN, BK, WM, KG>::SMEM];
-    const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x);
+    uint32_t grid = gridDim.x;
+    if constexpr (EPI::kCounted) {
+        if (p.count != nullptr) {
+            const int n = *p.count;
+            if (p.dim == kDimM) p.tiles_m = ((p.M = n) + 32 * MB * WM - 1) / (32 * MB * WM);
+            else if (p.dim == kDimN) p.tiles_n = ((p.N = n) + TN - 1) / TN;
+            else p.K = n;
+            grid = (uint32_t)(p.tiles_m * p.tiles_n + 7) / 8 * 8;      // the XCDs share what there is
+            if (blockIdx.x >= grid) return;
+        }
+        if (p.splits > 1) {
+            const int k0 = (int)blockIdx.y * p.k_chunk;
+            auto at = [&](LinOperand& op, auto slow) {
+                op.base = static_cast<const uint16_t*>(op.base) + (slow.value ? k0 * op.ld : (int64_t)k0);
+            };
+            at(p.A, std::integral_constant<bool, AL == kBf16KSlow>());
+            at(p.B, std::integral_constant<bool, BL == kBf16KSlow>());
+            p.K = min(p.k_chunk, p.K - k0);
+            p.epi.split((int)blockIdx.y);
+        }
+    }
+    const uint32_t tile = xcd_tile(blockIdx.x, grid);
     if (tile >= (uint32_t)(p.tiles_m * p.tiles_n)) return;
     tile_gemm_epi<AL, BL, EXACT, MB, TN, BK, WM, DEEP, KG, TERMS>(p.A, p.B, p.A2, p.B2, p.epi, p.M, p.N, p.K, p.tiles_m, p.tiles_n, tile,
                                                                   smem);
@@ -203,10 +232,10 @@ static int launch_epilogue_shape(EpiProduct<OPB, EPI> p, hipStream_t st) {
     const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
     const bool exact = p.M % TM == 0 && p.N % TC == 0 && p.K % BK == 0 && p.A.ld % 8 == 0 && p.B.ld % 16 == 0;
     if (exact)
-        hipLaunchKernelGGL((k_gemm_epilogue<AL, BL, true, MB, TN, BK, WM, DEEP_EXACT, KG, TERMS, OPB, EPI>), dim3(grid),
+        hipLaunchKernelGGL((k_gemm_epilogue<AL, BL, true, MB, TN, BK, WM, DEEP_EXACT, KG, TERMS, OPB, EPI>), dim3(grid, p.splits),
                            dim3(128 * WM * KG), 0, st, p);
     else
-        hipLaunchKernelGGL((k_gemm_epilogue<AL, BL, false, MB, TN, BK, WM, DEEP_RAGGED, KG, TERMS, OPB, EPI>), dim3(grid),
+        hipLaunchKernelGGL((k_gemm_epilogue<AL, BL, false, MB, TN, BK, WM, DEEP_RAGGED, KG, TERMS, OPB, EPI>), dim3(grid, p.splits),
                            dim3(128 * WM * KG), 0, st, p);
     return check_launch();
 }

@@ -2,6 +2,9 @@
 // z = x W^T:
 //     lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,label
 //     dl_tv = dloss_t (exp(z_tv - lse_t) - [v = label]),   dx = dl W,   dW = dl^T x
+// rows:     the tokens that have a loss, put together: their rows of x, zeros up to a multiple of 256 of them, and how many there
+//           are, which only the device knows.  Prompts and padding cost nothing from there on, and what they hold never meets a
+//           product (0 times it would be NaN in dW if it is not finite).
 // forward:  one product whose epilogue leaves, of every tile, each token's maximum and sum of exponentials over the tile's
 //           entries, and the label's logit; a second kernel joins them.  The product is computed as W x^T, so that a lane's sums
 //           belong to one token and most of the reduction stays in its registers.
@@ -18,10 +21,13 @@ constexpr float kLog2e = 1.44269504f;
 // Rows of the product are vocabulary entries, columns tokens.  A lane has 16 entries of each block of its column's token, the lane 32
 // further the other 16.
 struct StatsEpilogue {
-    static constexpr bool kPair = false;
-    const int64_t* labels;
+    static constexpr bool kPair = false, kCounted = true;
+    const int32_t* label32;       // of the tokens put together, or
+    const int64_t* labels;        // as the caller has them
     float* label_logit;
-    f32x2* part;        // [slots][N]: maximum and sum of exp(z - maximum) over a wave's 32 MB rows
+    f32x2* part;        // [slots][stride]: maximum and sum of exp(z - maximum) over a wave's 32 MB rows
+    int64_t stride;
+    __device__ void split(int) {}
     template <bool EXACT, int MB, int NB>
     __device__ __forceinline__ void tile(const f32x16 (&acc)[MB][NB], float*, int row0, int col0, bool inside, int M, int N,
                                          int lane) const {
@@ -30,8 +36,12 @@ struct StatsEpilogue {
         for (int b = 0; b < NB; ++b) {
             const int col = col0 + b * 32 + (lane & 31);
             const bool token = EXACT || inside || col < N;
-            const int64_t label = token ? labels[col] : -1;
-            const int at = label >= 0 && label < M ? (int)label - row0 - sub : -1;     // row of the label among the lane's
+            int label = -1;
+            if (token) {
+                if (label32 != nullptr) label = label32[col];
+                else if (const int64_t l = labels[col]; l >= 0 && l < M) label = (int)l;
+            }
+            const int at = label - row0 - sub;      // row of the label among the lane's
             float top = -INFINITY, z = 0.f;
             bool mine = false;
 #pragma unroll
@@ -58,73 +68,167 @@ struct StatsEpilogue {
                     sum += EXACT || inside || row0 + sub + r < M ? e : 0.f;
                 }
             sum += __shfl_xor(sum, 32, 64);
-            if (lane < 32 && token) part[(int64_t)slot * N + col] = f32x2{top, sum};
+            if (lane < 32 && token) part[(int64_t)slot * stride + col] = f32x2{top, sum};
         }
     }
 };
 
-__device__ __forceinline__ void join(float& top, float& sum, float top2, float sum2) {
-    const float t = fmaxf(top, top2);
-    const float ref = t == -INFINITY ? 0.f : t;
-    sum = sum * __builtin_amdgcn_exp2f((top - ref) * kLog2e) + sum2 * __builtin_amdgcn_exp2f((top2 - ref) * kLog2e);
-    top = t;
-}
-
-// 16 tokens per workgroup, 64 slices of the slots, joined in a fixed order.
-__global__ __launch_bounds__(1024) void k_head_join(const f32x2* __restrict__ part, int slots, const int64_t* __restrict__ labels,
-                                                    const float* __restrict__ label_logit, int tokens, int64_t vocab,
-                                                    float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float tops[64][17], sums[64][17];
-    const int lane = threadIdx.x & 15, slice = threadIdx.x >> 4, t = blockIdx.x * 16 + lane;
+// 16 tokens per workgroup, 64 slices of the slots: maxima first, then the sums below the token's maximum, in a fixed order.
+__global__ __launch_bounds__(1024) void k_head_join(const f32x2* __restrict__ part, int slots, int64_t stride,
+                                                    const int64_t* __restrict__ labels, int64_t vocab,
+                                                    const int32_t* __restrict__ rows, const float* __restrict__ label_logit,
+                                                    const int32_t* __restrict__ count, int tokens, float* __restrict__ loss,
+                                                    float* __restrict__ lse) {
+    __shared__ float most[16][17], sums[16][17];
+    if (count != nullptr) tokens = *count;
+    if ((int)blockIdx.x * 16 >= tokens) return;
+    const int lane = threadIdx.x & 15, slice = threadIdx.x >> 4, wave = threadIdx.x >> 6, t = blockIdx.x * 16 + lane;
     float top = -INFINITY, sum = 0.f;
-    if (t < tokens)
-        for (int s = slice; s < slots; s += 64) {
-            const f32x2 p = part[(int64_t)s * tokens + t];
-            join(top, sum, p[0], p[1]);
-        }
-    tops[slice][lane] = top;
-    sums[slice][lane] = sum;
+    const bool mine = t < tokens;
+    // slots of this slice, eight at a time: loads ahead of the exponentials
+    for (int s0 = slice; s0 < slots; s0 += 512) {
+        f32x2 p[8];
 #pragma unroll
-    for (int n = 32; n > 0; n >>= 1) {
-        __syncthreads();
-        if (slice < n) {
-            join(top, sum, tops[slice + n][lane], sums[slice + n][lane]);
-            tops[slice][lane] = top;
-            sums[slice][lane] = sum;
+        for (int i = 0; i < 8; ++i) {
+            const int s = s0 + 64 * i;
+            p[i] = mine && s < slots ? part[(int64_t)s * stride + t] : f32x2{-INFINITY, 0.f};
         }
+        float now = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) now = fmaxf(now, p[i][0]);
+        const float ref = now == -INFINITY ? 0.f : now;
+        sum *= __builtin_amdgcn_exp2f((top - ref) * kLog2e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(p[i][1], __builtin_amdgcn_exp2f((p[i][0] - ref) * kLog2e), sum);
+        top = now;
     }
-    if (slice != 0 || t >= tokens) return;
-    const float l = top + logf(sum);
-    const int64_t label = labels[t];
-    lse[t] = l;
-    loss[t] = label >= 0 && label < vocab ? l - label_logit[t] : 0.f;
+    float all = fmaxf(top, __shfl_xor(top, 16, 64));      // the wave's four slices
+    all = fmaxf(all, __shfl_xor(all, 32, 64));
+    if ((threadIdx.x & 63) < 16) most[wave][lane] = all;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all = fmaxf(all, most[i][lane]);
+    const float ref = all == -INFINITY ? 0.f : all;
+    sum *= __builtin_amdgcn_exp2f((top - ref) * kLog2e);
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if ((threadIdx.x & 63) < 16) sums[wave][lane] = sum;
+    __syncthreads();
+    if (slice != 0 || !mine) return;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += sums[i][lane];
+    const int row = rows != nullptr ? rows[t] : t;
+    if (row < 0) return;
+    const float l = all + logf(sum);
+    const bool learned = rows != nullptr || (labels[t] >= 0 && labels[t] < vocab);
+    lse[row] = learned ? l : 0.f;
+    loss[row] = learned ? l - label_logit[t] : 0.f;
 }
 
-// ---- backward ----
-// x with zeros where a token has no loss (0 times what stands there would be NaN in dW if that is not finite), rows padded to whole
-// 16-byte chunks; and each token's label in 32 bits, -1 for none.
-__global__ __launch_bounds__(256) void k_head_rows(const uint16_t* __restrict__ x, const int64_t* __restrict__ labels, int tokens, int h,
-                                                   int64_t ld, int hp, int64_t vocab, uint16_t* __restrict__ xm, int32_t* __restrict__ label32) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = hp / 8;
-    const int64_t t = i / per;
-    if (t >= tokens) return;
-    const int col = (int)(i - t * per) * 8;
-    const int64_t label = labels[t];
-    const bool learned = label >= 0 && label < vocab;
-    float v[8] = {};
-    if (learned) load_run(x + t * ld + col, h - col, v);
-    store_run(xm + t * hp + col, 8, v);
-    if (col == 0) label32[t] = learned ? (int)label : -1;
+// ---- the tokens that have a loss ----
+// Of each such token: its row of x, its number, its label in 32 bits and (backward) its lse and dloss; then rows of zeros up to a
+// multiple of `unit`.  The others' loss and lse, or row of dx, become zero here.  A workgroup counts the labels for itself
+// (they are few bytes and stay in the cache): one launch, and an order that does not depend on timing.
+struct HeadRows {
+    const uint16_t* x;
+    const int64_t* labels;
+    const float *lse_in, *dloss_in;      // backward only
+    int64_t ld, vocab;
+    int tokens, padded, unit, h, hp, per;   // padded: tokens up to a multiple of unit; per: tokens of a workgroup
+    uint16_t* xc;
+    int32_t *rows, *label32, *count;
+    float *lse, *dloss;                  // backward only
+    float *loss_out, *lse_out;           // forward only
+    uint16_t* dx;                        // backward only, may be NULL
+};
+__global__ __launch_bounds__(256) void k_head_rows(HeadRows a) {
+    __shared__ int before_s[4], all_s[4];
+    const int first = (int)blockIdx.x * a.per, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto learned = [&](int t) {
+        const int64_t l = a.labels[t];
+        return l >= 0 && l < a.vocab;
+    };
+    int before = 0, all = 0;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < a.tokens; t += 256) {
+        const int one = learned(t);
+        all += one;
+        before += t < first ? one : 0;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        all += __shfl_xor(all, off, 64);
+        before += __shfl_xor(before, off, 64);
+    }
+    if (lane == 0) {
+        before_s[wave] = before;
+        all_s[wave] = all;
+    }
+    __syncthreads();
+    all = all_s[0] + all_s[1] + all_s[2] + all_s[3];
+    before = before_s[0] + before_s[1] + before_s[2] + before_s[3];
+    // (rows of zeros where no token has a loss: no product is empty)
+    const int up = max((all + a.unit - 1) / a.unit, 1) * a.unit;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = up;
+    const int last = min(first + a.per, a.padded), chunks = a.hp / 8;
+    for (int t0 = first; t0 < last; t0 += 64) {
+        // where the tokens go: those with a loss in their order, the others behind them while there are rows to fill with zeros
+        const int t = t0 + lane;
+        const bool here = t < last, one = here && t < a.tokens && learned(t);
+        const uint64_t mask = __ballot(one);
+        const int rank = __popcll(mask & ((1ull << lane) - 1));
+        const int dst = one ? before + rank : all + (t0 - before) + (lane - rank);
+        const int to = here && dst < up ? dst : -1;
+        if (wave == 0) {
+            if (to >= 0) {
+                a.rows[to] = one ? t : -1;
+                a.label32[to] = one ? (int)a.labels[t] : -1;
+                if (a.lse != nullptr) {
+                    a.lse[to] = one ? a.lse_in[t] : 0.f;
+                    a.dloss[to] = one ? a.dloss_in[t] : 0.f;
+                }
+            }
+            if (a.loss_out != nullptr && here && t < a.tokens && !one) {
+                a.loss_out[t] = 0.f;
+                a.lse_out[t] = 0.f;
+            }
+        }
+        const int n = min(64, last - t0);
+        for (int r = wave; r < n; r += 4) {              // a row per wave, four chunks of a lane at a time
+            const int row = __builtin_amdgcn_readlane(to, r);
+            const bool copy = (mask >> r) & 1;
+            const uint16_t* src = a.x + (int64_t)(t0 + r) * a.ld;
+            uint16_t* zero = !copy && a.dx != nullptr && t0 + r < a.tokens ? a.dx + (int64_t)(t0 + r) * a.ld : nullptr;
+            if (row < 0 && zero == nullptr) continue;
+            for (int c0 = lane; c0 < chunks; c0 += 256) {
+                float v[4][8] = {};
+                if (copy)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c0 + 64 * i < chunks) load_run(src + (c0 + 64 * i) * 8, a.h - (c0 + 64 * i) * 8, v[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = (c0 + 64 * i) * 8;
+                    if (c >= a.hp) break;
+                    if (row >= 0) store_run(a.xc + (int64_t)row * a.hp + c, 8, v[i]);
+                    if (zero != nullptr) store_run(zero + c, a.h - c, v[i]);
+                }
+            }
+        }
+        before += __popcll(mask);
+    }
 }
 
 // dl of the entries from v0 on
 struct DLogitsRun {
-    static constexpr bool kPair = false;
+    static constexpr bool kPair = false, kCounted = true;
     const int32_t* label32;
     const float *lse, *dloss;
     uint16_t* dl;
     int64_t ldc;
     int v0;
+    __device__ void split(int) {}
     template <int R>
     __device__ __forceinline__ void run(int row, int col, int left, float (&v)[R]) const {
         const int label = label32[row];
@@ -139,34 +243,54 @@ struct DLogitsRun {
     }
 };
 
-// dx over the pieces: in fp32 up to the last one, which rounds.
+// dx over the pieces and the parts of a split contraction: in fp32 up to the last one, which rounds.
 struct AddRun {
-    static constexpr bool kPair = false;
-    const float* before;     // NULL: the first piece
-    float* sum;              // NULL: the last piece
+    static constexpr bool kPair = false, kCounted = true;
+    float* sum;              // [splits][padded tokens][ld_sum]
     uint16_t* out;
-    int64_t ld_sum, ld_out;
+    const int32_t* rows;
+    int64_t ld_sum, ld_out, stride;
+    bool begins, ends;       // with this piece; ends only where there is one split
+    __device__ void split(int s) { sum += s * stride; }
     template <int R>
     __device__ __forceinline__ void run(int row, int col, int left, float (&v)[R]) const {
-        const int64_t at = (int64_t)row * ld_sum + col;      // rows of whole 16-byte chunks
-        if (before != nullptr) {
+        float* p = sum + (int64_t)row * ld_sum + col;      // rows of whole 16-byte chunks
+        if (!begins) {
 #pragma unroll
             for (int e = 0; e < R; e += 4)
                 if (e < left) {
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(before + at + e);
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(p + e);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[e + k] += b[k];
                 }
         }
-        if (sum != nullptr) {
+        if (!ends) {
 #pragma unroll
             for (int e = 0; e < R; e += 4)
-                if (e < left) *reinterpret_cast<f32x4*>(sum + at + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-        } else {
-            store_run(out + (int64_t)row * ld_out + col, left, v);
+                if (e < left) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+        } else if (const int to = rows[row]; to >= 0) {
+            store_run(out + (int64_t)to * ld_out + col, left, v);
         }
     }
 };
+
+// dx = the splits' sums, added in order.
+__global__ __launch_bounds__(256) void k_head_dx(const float* __restrict__ sum, int64_t stride, int splits, const int32_t* __restrict__ rows,
+                                                 const int32_t* __restrict__ count, int h, int hp, uint16_t* __restrict__ dx, int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = hp / 8, row = i / chunks;
+    if (row >= *count) return;
+    const int to = rows[row], col = (int)(i - row * chunks) * 8;
+    if (to < 0) return;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    const float* p = sum + row * hp + col;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s, p += stride) {
+        a += reinterpret_cast<const f32x4*>(p)[0];
+        b += reinterpret_cast<const f32x4*>(p)[1];
+    }
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    store_run(dx + (int64_t)to * ld + col, h - col, v);
+}
 
 // ---- sizes ----
 static int check_head(int64_t tokens, int64_t h, int64_t vocab, int64_t& ld) {
@@ -187,8 +311,8 @@ static int head_tile(int64_t M, int64_t N) {
     return ((M + 127) / 128) * ((N + 127) / 128) < 256 ? kTile64 : kTile128;
 }
 template <int AL, int BL, typename EPI>
-static int launch_head(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
-    switch (head_tile(p.M, p.N)) {
+static int launch_head(EpiProduct<LinOperand, EPI> p, int tile, hipStream_t st) {
+    switch (tile) {
         case kTile256: return launch_epilogue_shape<AL, BL, 2, 256, 64, 4, true, true, 1, 1>(p, st);
         case kTile128: return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 1, 1>(p, st);
         default: return launch_epilogue_shape<AL, BL, 1, 64, 64, 2, true, true, 1, 1>(p, st);
@@ -201,39 +325,87 @@ static int64_t head_slots(int64_t tokens, int64_t vocab) {
     return up(vocab, rows * per_tile) / rows;
 }
 
-// Entries of a piece: dl of one piece stays below 64 MiB (so that both products find it in the 256 MB cache behind the L2s), 1024
+// dx has tokens x h elements and a contraction as long as the vocabulary: where its tiles would leave CUs idle, the contraction of a
+// piece is split over workgroups, 1024 of it each at least, up to two workgroups of 128 x 128 (or 64 x 64) tiles per CU.
+static int head_dx_tile(int64_t tokens, int64_t h) {
+    const int tile = head_tile(tokens, h);
+    return tile == kTile64 && tokens > 64 && h > 64 ? kTile128 : tile;
+}
+static int64_t head_chunk(int64_t tokens, int64_t h, int64_t piece) {
+    const int tile = head_dx_tile(tokens, h);
+    if (tile == kTile256) return piece;
+    const int64_t side = tile == kTile64 ? 64 : 128, tiles = ((tokens + side - 1) / side) * ((h + side - 1) / side);
+    const int64_t room = 1024 / tiles, most = piece / 1024, splits = room < most ? room : most;
+    return splits <= 1 ? piece : up((piece + splits - 1) / splits, 64);
+}
+
+// Entries of a piece: dl of one piece stays below 128 MiB (so that both products find it in the 256 MB cache behind the L2s), 1024
 // entries at least, pieces of about one size.
 static int64_t head_piece(int64_t tokens, int64_t vocab) {
-    const int64_t most = (int64_t(1) << 25) / tokens;
+    const int64_t most = (int64_t(1) << 26) / tokens;
     const int64_t piece = most < 1024 ? 1024 : most;
     const int64_t pieces = (vocab + piece - 1) / piece;
     const int64_t even = up((vocab + pieces - 1) / pieces, 256);
     return even < vocab ? even : vocab;
 }
 
-struct HeadSpace {     // the backward pass's workspace, in bytes
-    int64_t piece, hp;
-    size_t labels, x, sum, dl, total;
+struct HeadSpace {     // a call's workspace, in bytes
+    int64_t piece, chunk, splits, hp, unit, padded, slots;     // chunk: contraction of dx per workgroup
+    size_t count, rows, labels, lse, dloss, x, sum, dl, part, logit, total;
 };
-static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab) {
-    HeadSpace s;
-    s.piece = head_piece(tokens, vocab);
-    s.hp = up(h, 8);
+static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab, bool backward) {
+    HeadSpace s = {};
+    s.hp = up(h, backward ? 256 : 8);
+    s.unit = tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256;
+    s.padded = up(tokens, s.unit);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += (bytes + 255) / 256 * 256;
         return from;
     };
-    s.labels = take((size_t)tokens * 4);
-    s.x = take((size_t)tokens * s.hp * 2);
-    s.sum = take(s.piece < vocab ? (size_t)tokens * s.hp * 4 : 0);
-    s.dl = take((size_t)tokens * up(s.piece, 16) * 2);
+    s.count = take(4);
+    s.rows = take((size_t)s.padded * 4);
+    s.labels = take((size_t)s.padded * 4);
+    s.x = take((size_t)s.padded * s.hp * 2);
+    if (backward) {
+        s.piece = head_piece(tokens, vocab);
+        s.chunk = head_chunk(s.padded, h, s.piece);
+        s.splits = (s.piece + s.chunk - 1) / s.chunk;
+        s.lse = take((size_t)s.padded * 4);
+        s.dloss = take((size_t)s.padded * 4);
+        s.sum = take(s.piece < vocab || s.splits > 1 ? (size_t)s.padded * s.hp * 4 * s.splits : 0);
+        s.dl = take((size_t)s.padded * up(s.piece, kLinTM) * 2);
+    } else {
+        s.slots = head_slots(s.padded, vocab);
+        s.part = take((size_t)s.padded * 8 * s.slots);
+        s.logit = take((size_t)s.padded * 4);
+    }
     s.total = at;
     return s;
 }
-static size_t head_forward_bytes(int64_t tokens, int64_t vocab) {
-    return (size_t)tokens * 8 * head_slots(tokens, vocab) + (size_t)up(tokens, 4) * 4;
+
+// Whether the forward pass puts the tokens that have a loss together: it costs one launch and a copy of x, 6 us and more, which
+// a product of 2^36 flop (some 80 us) or more is worth; the backward pass, of three products, always does.
+static bool head_put_together(int64_t tokens, int64_t h, int64_t vocab) { return 2. * tokens * h * vocab >= 68719476736.; }
+
+static int launch_head_rows(HeadRows a, hipStream_t st) {
+    // a token per wave, or as many as make a thousand workgroups (each counts all labels)
+    const int64_t per = (a.padded + 1023) / 1024;
+    a.per = (int)(per < 4 ? 4 : per);
+    hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.padded + a.per - 1) / a.per)), dim3(256), 0, st, a);
+    return check_launch();
+}
+
+// dW's rows of a piece, dl^T x: direct loads of whole tiles.  dl's rows are a multiple of 128 elements apart, x's of 256, so that a
+// tile never leaves its row; what stands between their ends and that only reaches elements that are not stored.
+static int launch_head_dw(const uint16_t* dl, int64_t pitch, const uint16_t* x, int64_t hp, uint16_t* dW, int64_t ldc, int64_t width,
+                          int64_t h, int64_t padded, const int32_t* count, hipStream_t st) {
+    const int64_t tiles_m = pitch / kLinTM, tiles_n = hp / 256;
+    const KSlowOut out = {(int)width, (int)h, ldc, count};
+    hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(256), 0, st, dl, x, dW,
+                       (int)pitch, (int)hp, (int)padded, (int)tiles_m, (int)tiles_n, out);
+    return check_launch();
 }
 
 }  // namespace qg
@@ -243,7 +415,7 @@ using namespace qg;
 extern "C" size_t qg_head_loss_workspace_bytes(int64_t tokens, int64_t h, int64_t vocab) {
     int64_t ld = 0;
     if (check_head(tokens, h, vocab, ld)) return 0;
-    const size_t f = head_forward_bytes(tokens, vocab), b = head_space(tokens, h, vocab).total;
+    const size_t f = head_space(tokens, h, vocab, false).total, b = head_space(tokens, h, vocab, true).total;
     return f > b ? f : b;
 }
 
@@ -255,19 +427,35 @@ extern "C" int qg_head_loss_forward(const uint16_t* x_bf16, const uint16_t* W_bf
     for (const void* p : {(const void*)x_bf16, (const void*)W_bf16, (const void*)labels, (const void*)loss, (const void*)lse,
                           (const void*)workspace})
         if (!aligned16(p)) return QG_ERR_ALIGN;
-    if (!workspace || workspace_bytes < head_forward_bytes(tokens, vocab)) return QG_ERR_WORKSPACE;
+    const HeadSpace s = head_space(tokens, h, vocab, false);
+    if (!workspace || workspace_bytes < s.total) return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
-    const int64_t slots = head_slots(tokens, vocab);
-    f32x2* part = static_cast<f32x2*>(workspace);
-    float* label_logit = reinterpret_cast<float*>(part + slots * tokens);
+    char* at = static_cast<char*>(workspace);
+    HeadRows r = {};
     EpiProduct<LinOperand, StatsEpilogue> p;
     p.A = p.A2 = LinOperand{W_bf16, nullptr, ld, 0};
     p.B = p.B2 = LinOperand{x_bf16, nullptr, ld, 0};
-    p.epi = StatsEpilogue{labels, label_logit, part};
     p.M = (int)vocab, p.N = (int)tokens, p.K = (int)h;
-    if (int e = launch_head<kBf16KFast, kBf16KFast>(p, st)) return e;
-    hipLaunchKernelGGL(k_head_join, dim3((unsigned)((tokens + 15) / 16)), dim3(1024), 0, st, part, (int)slots, labels, label_logit,
-                       (int)tokens, vocab, loss, lse);
+    if (head_put_together(tokens, h, vocab)) {
+        r.x = x_bf16, r.labels = labels, r.ld = ld, r.vocab = vocab;
+        r.tokens = (int)tokens, r.padded = (int)s.padded, r.unit = (int)s.unit, r.h = (int)h, r.hp = (int)s.hp;
+        r.xc = reinterpret_cast<uint16_t*>(at + s.x);
+        r.rows = reinterpret_cast<int32_t*>(at + s.rows);
+        r.label32 = reinterpret_cast<int32_t*>(at + s.labels);
+        r.count = reinterpret_cast<int32_t*>(at + s.count);
+        r.loss_out = loss, r.lse_out = lse;
+        if (int e = launch_head_rows(r, st)) return e;
+        p.B = p.B2 = LinOperand{r.xc, nullptr, s.hp, 0};
+        p.N = (int)s.padded;
+        p.count = r.count;
+        p.dim = kDimN;
+    }
+    f32x2* part = reinterpret_cast<f32x2*>(at + s.part);
+    float* label_logit = reinterpret_cast<float*>(at + s.logit);
+    p.epi = StatsEpilogue{r.label32, labels, label_logit, part, s.padded};
+    if (int e = launch_head<kBf16KFast, kBf16KFast>(p, head_tile(vocab, s.padded), st)) return e;
+    hipLaunchKernelGGL(k_head_join, dim3((unsigned)((s.padded + 15) / 16)), dim3(1024), 0, st, part, (int)s.slots, s.padded, labels, vocab,
+                       r.rows, label_logit, r.count, p.N, loss, lse);
     return check_launch();
 }
 
@@ -279,40 +467,56 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
     for (const void* p : {(const void*)x_bf16, (const void*)W_bf16, (const void*)labels, (const void*)lse, (const void*)dloss,
                           (const void*)dx_bf16, (const void*)dW_bf16, (const void*)workspace})
         if (!aligned16(p)) return QG_ERR_ALIGN;
-    const HeadSpace s = head_space(tokens, h, vocab);
+    const HeadSpace s = head_space(tokens, h, vocab, true);
     if (!workspace || workspace_bytes < s.total) return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     char* at = static_cast<char*>(workspace);
-    int32_t* label32 = reinterpret_cast<int32_t*>(at + s.labels);
-    uint16_t *xm = reinterpret_cast<uint16_t*>(at + s.x), *dl = reinterpret_cast<uint16_t*>(at + s.dl);
+    HeadRows r = {};
+    r.x = x_bf16, r.labels = labels, r.lse_in = lse, r.dloss_in = dloss, r.ld = ld, r.vocab = vocab;
+    r.tokens = (int)tokens, r.padded = (int)s.padded, r.unit = (int)s.unit, r.h = (int)h, r.hp = (int)s.hp;
+    r.xc = reinterpret_cast<uint16_t*>(at + s.x);
+    r.rows = reinterpret_cast<int32_t*>(at + s.rows);
+    r.label32 = reinterpret_cast<int32_t*>(at + s.labels);
+    r.count = reinterpret_cast<int32_t*>(at + s.count);
+    r.lse = reinterpret_cast<float*>(at + s.lse);
+    r.dloss = reinterpret_cast<float*>(at + s.dloss);
+    r.dx = dx_bf16;
+    if (int e = launch_head_rows(r, st)) return e;
+    uint16_t* dl = reinterpret_cast<uint16_t*>(at + s.dl);
     float* sum = reinterpret_cast<float*>(at + s.sum);
-    hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((tokens * (s.hp / 8) + 255) / 256)), dim3(256), 0, st, x_bf16, labels, (int)tokens,
-                       (int)h, ld, (int)s.hp, vocab, xm, label32);
-    if (int e = check_launch()) return e;
+    const int64_t stride = s.padded * s.hp;
     for (int64_t v0 = 0; v0 < vocab; v0 += s.piece) {
-        const int64_t width = vocab - v0 < s.piece ? vocab - v0 : s.piece, pitch = up(width, 16);
-        const LinOperand x = {xm, nullptr, s.hp, 0}, W = {W_bf16 + v0 * ld, nullptr, ld, 0}, d = {dl, nullptr, pitch, 0};
+        const int64_t width = vocab - v0 < s.piece ? vocab - v0 : s.piece, pitch = up(width, kLinTM);
+        const LinOperand x = {r.xc, nullptr, s.hp, 0}, W = {W_bf16 + v0 * ld, nullptr, ld, 0}, d = {dl, nullptr, pitch, 0};
         {
             EpiProduct<LinOperand, RunEpilogue<DLogitsRun>> p;
             p.A = p.A2 = x;
             p.B = p.B2 = W;
-            static_cast<DLogitsRun&>(p.epi) = DLogitsRun{label32, lse, dloss, dl, pitch, (int)v0};
-            p.M = (int)tokens, p.N = (int)width, p.K = (int)h;
-            if (int e = launch_head<kBf16KFast, kBf16KFast>(p, st)) return e;
+            static_cast<DLogitsRun&>(p.epi) = DLogitsRun{r.label32, r.lse, r.dloss, dl, pitch, (int)v0};
+            p.M = (int)s.padded, p.N = (int)width, p.K = (int)h;
+            p.count = r.count;
+            p.dim = kDimM;
+            if (int e = launch_head<kBf16KFast, kBf16KFast>(p, head_tile(s.padded, width), st)) return e;
         }
         if (dx_bf16) {
             EpiProduct<LinOperand, RunEpilogue<AddRun>> p;
             p.A = p.A2 = d;
             p.B = p.B2 = W;
-            const bool last = v0 + width == vocab;
-            static_cast<AddRun&>(p.epi) = AddRun{v0 > 0 ? sum : nullptr, last ? nullptr : sum, dx_bf16, s.hp, ld};
-            p.M = (int)tokens, p.N = (int)h, p.K = (int)width;
-            if (int e = launch_head<kBf16KFast, kBf16KSlow>(p, st)) return e;
+            static_cast<AddRun&>(p.epi) = AddRun{sum, dx_bf16, r.rows, s.hp, ld, stride, v0 == 0, v0 + width == vocab && s.splits == 1};
+            p.M = (int)s.padded, p.N = (int)h, p.K = (int)width;
+            p.count = r.count;
+            p.dim = kDimM;
+            p.k_chunk = (int)s.chunk;
+            p.splits = (int)((width + s.chunk - 1) / s.chunk);
+            if (int e = launch_head<kBf16KFast, kBf16KSlow>(p, head_dx_tile(s.padded, h), st)) return e;
         }
         if (dW_bf16)
-            if (int e = launch_tile_gemm<kBf16KSlow, kBf16KSlow, uint16_t>(d, x, nullptr, dW_bf16 + v0 * ld, width, h, tokens, st, nullptr,
-                                                                           1, ld))
-                return e;
+            if (int e = launch_head_dw(dl, pitch, r.xc, s.hp, dW_bf16 + v0 * ld, ld, width, h, s.padded, r.count, st)) return e;
+    }
+    if (dx_bf16 && s.splits > 1) {
+        hipLaunchKernelGGL(k_head_dx, dim3((unsigned)((s.padded * (s.hp / 8) + 255) / 256)), dim3(256), 0, st, sum, stride, (int)s.splits, r.rows,
+                           r.count, (int)h, (int)s.hp, dx_bf16, ld);
+        return check_launch();
     }
     return QG_OK;
 }

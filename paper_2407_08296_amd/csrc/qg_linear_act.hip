@@ -248,7 +248,7 @@ extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* z
     const hipStream_t st = (hipStream_t)stream;
     if (int e = launch_act_backward<true>(dy_bf16, zg_bf16, zu_bf16, dzg_bf16, dzu_bf16, nullptr, tokens, m, ld_m, act, st)) return e;
     const int sg = (int)((n + kGroup - 1) / kGroup);
-    const LinOperand dzg = {dzg_bf16, nullptr, ld_m, 0}, dzu = {dzu_bf16, nullptr, ld_m, 0}, x = {x_bf16, nullptr, ld_n, 0};
+    const LinOperand dzg = {dzg_bf16, nullptr, ld_m, 0}, dzu = {dzu_bf16, nullptr, ld_m, 0};
     if (dx_bf16) {
         EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p;
         p.A = dzg, p.A2 = dzu;

@@ -229,7 +229,7 @@ __device__ __forceinline__ void store_run(uint16_t* dst, int left, const float (
 // `tp`: kTransposeFloats floats of LDS of the wave's own; inside: all blocks lie inside C.
 template <typename OUT>
 struct PlainEpilogue {
-    static constexpr bool kPair = false;
+    static constexpr bool kPair = false, kCounted = false;   // (kCounted: see EpiProduct)
     const uint16_t* bias;
     OUT* C;
     int64_t ldc;
@@ -656,12 +656,19 @@ __global__ __launch_bounds__(256, 2) void k_gemm_pair(LinProduct p0, LinProduct 
 // LLaMA shapes): the staging of the optimizer step's projection kernel for its gradient operand, applied to both -
 // direct global -> LDS loads into unpadded swizzled [k][x] tiles (no staging registers, no LDS write instructions),
 // two stages, the loads of step k+1 issued ahead of the MFMAs of step k, three workgroups per CU.
-template <typename OUT>
+// Rows of A and B are M and N elements apart, multiples of the tile.
+struct KSlowOut {          // RAGGED: C is smaller than the operands, whose columns past it may hold anything
+    int rows, cols;
+    int64_t ldc;
+    const int32_t* device_k;   // the length of the contraction (a multiple of 32), which only the device knows
+};
+template <typename OUT, bool RAGGED = false>
 __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __restrict__ A, const uint16_t* __restrict__ B,
                                                               OUT* __restrict__ C, int M, int N, int K, int tiles_m,
-                                                              int tiles_n) {
+                                                              int tiles_n, KSlowOut out) {
     constexpr int TN = 256, BK = 32;
-    const int64_t ldc = N;   // dense operands and output only
+    if constexpr (RAGGED) K = *out.device_k;
+    const int64_t ldc = RAGGED ? out.ldc : N;
     using AD = KMajorSwizzled<kLinTM, BK, 256>;
     using BD = KMajorSwizzled<TN, BK, 256>;
     __shared__ __attribute__((aligned(16))) uint16_t As[2][AD::STAGE];
@@ -744,6 +751,7 @@ __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __
             for (int v = 0; v < 16; ++v) {
                 const int row = i0 + wm * 64 + a * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
                 const float x = acc[a][b][v];
+                if (RAGGED && (row >= out.rows || col >= out.cols)) continue;
                 if constexpr (sizeof(OUT) == 4) C[(int64_t)row * ldc + col] = x;
                 else C[(int64_t)row * ldc + col] = to_bf16(x);
             }
@@ -1046,7 +1054,7 @@ static int launch_tile_gemm(const LinOperand& A, const LinOperand& B, const uint
             tiles_m * tiles_n >= 512 && K >= 32 && A.ld == M && B.ld == N && (ldc == 0 || ldc == N)) {
             const unsigned grid = (unsigned)((tiles_m * tiles_n + 7) / 8 * 8);
             hipLaunchKernelGGL((k_gemm_kslow_direct<OUT>), dim3(grid), dim3(256), 0, st, static_cast<const uint16_t*>(A.base),
-                               static_cast<const uint16_t*>(B.base), C, (int)M, (int)N, (int)K, (int)tiles_m, (int)tiles_n);
+                               static_cast<const uint16_t*>(B.base), C, (int)M, (int)N, (int)K, (int)tiles_m, (int)tiles_n, KSlowOut{});
             return check_launch();
         }
     }

@@ -17,7 +17,7 @@ U24 = 2.0 ** -24
 
 # (tokens, h, vocab): one of everything, odd everything, around the tiles (64, 128, 256), several pieces (a long batch, a wide vocabulary)
 CASES = [(1, 1, 1), (1, 8, 2), (3, 7, 5), (1, 768, 4001), (33, 65, 130), (64, 64, 64), (65, 72, 257), (130, 521, 1000), (256, 128, 8192),
-         (300, 40, 20001), (2100, 64, 4100), (1100, 24, 16640), (40000, 16, 2600), (33000, 24, 1025)]
+         (300, 40, 20001), (2100, 64, 4100), (1100, 24, 16640), (40000, 16, 2600), (33000, 24, 1025), (20000, 24, 4100)]
 
 
 def f64(t):
@@ -47,10 +47,11 @@ def test_forward(tokens, h, vocab):
     X, WW = f64(x), f64(W)
     want, wlse = O.head_loss_forward(X, WW, labels.cpu().numpy())
     bar = noise_of(X, WW) + (np.log2(vocab) + 40) * U24 * (1 + np.abs(wlse))
-    assert np.all(np.abs(f64(lse) - wlse) <= bar)
-    assert np.all(np.abs(f64(loss) - want) <= 2 * bar + 4 * U24 * np.abs(wlse - want))
     learned = (labels >= 0) & (labels < vocab)
-    assert not loss[~learned].any()
+    on = learned.cpu().numpy()
+    assert np.all((np.abs(f64(lse) - wlse) <= bar)[on])
+    assert np.all(np.abs(f64(loss) - want) <= 2 * bar + 4 * U24 * np.abs(wlse - want))
+    assert not loss[~learned].any() and not lse[~learned].any()
 
 
 @pytest.mark.parametrize("tokens,h,vocab", CASES)
@@ -101,6 +102,29 @@ def test_no_token_with_a_loss():
     loss, lse = qg.head_loss_forward(x, W, labels)
     dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
     assert not loss.any() and not dx.any() and not dW.any()
+
+
+@pytest.mark.parametrize("tokens", [255, 256, 257, 700, 20000])
+@pytest.mark.parametrize("every", [1, 2, 200])
+def test_tokens_put_together(tokens, every):
+    """One token in `every` has a loss: losses and gradients are those of these tokens alone (which are whole rows of products: the
+    same terms; only where a token's row lies in a tile differs)."""
+    x, W, labels, dloss = inputs(tokens, 64, 3000, seed=tokens)
+    labels = torch.where(labels >= 0, labels, 5) % 3000
+    on = torch.arange(tokens, device=DEV) % every == every - 1
+    labels[~on] = -100
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    xs, ls, ds = x[on].contiguous(), labels[on].contiguous(), dloss[on].contiguous()
+    if len(ls) == 0:
+        assert not loss.any() and not dx.any() and not dW.any()
+        return
+    loss2, lse2 = qg.head_loss_forward(xs, W, ls)
+    dx2, dW2 = qg.head_loss_backward(xs, W, ls, lse2, ds)
+    assert not loss[~on].any() and not dx[~on].any()
+    assert torch.allclose(loss[on], loss2, rtol=1e-5, atol=1e-5)
+    close = lambda a, b: float((a.double() - b.double()).norm()) <= 2.0 ** -7 * float(b.double().norm())
+    assert close(dx[on], dx2) and close(dW, dW2)
 
 
 def test_large_logits():
