@@ -378,12 +378,12 @@ int qg_residual_norm_backward(const uint16_t* du_bf16, const void* dh_next, cons
  * qg_int8_linear_act_forward:  z = x W^T + bias (bf16 [m], nullable);  y = act(z) + residual (bf16 [tokens][ld_m], nullable).  The
  *   activation takes the fp32 sum; z (nullable) is what the backward pass wants, rounded to bf16.  y may be residual.
  * qg_int8_linear_act_backward: dz = dy act'(z);  dx = dz W, G = dz^T x, dbias (fp32 [m]) = sum over tokens of dz, each of them
- *   nullable (and then the inputs only it needs are too).  dz (bf16 [tokens][ld_m], may be dy or z) is written where a product is
- *   asked for; QG_ACT_NONE needs neither z nor dz.  The residual's gradient is dy.  workspace (dbias only):
- *   qg_int8_linear_act_workspace_bytes(tokens, m) bytes, 16-byte aligned.
+ *   nullable (and then the inputs only it needs are too).  dz is rounded to bf16 for the products, not for dbias.  QG_ACT_NONE
+ *   needs no z.  The residual's gradient is dy.  workspace: qg_int8_linear_act_workspace_bytes(tokens, m) bytes, 16-byte aligned;
+ *   not needed for dx and G with QG_ACT_NONE.
  * qg_int8_gated_forward:  y = act(x Wg^T) * (x Wu^T), both weights m x n; zg, zu: both (for the backward pass) or neither.
- * qg_int8_gated_backward: dzg = dy zu act'(zg), dzu = dy act(zg) (bf16 [tokens][ld_m], written; may be zg and zu);
- *   dx = dzg Wg + dzu Wu (nullable), Gg = dzg^T x and Gu = dzu^T x (both or neither). */
+ * qg_int8_gated_backward: dzg = dy zu act'(zg), dzu = dy act(zg), rounded to bf16;  dx = dzg Wg + dzu Wu (nullable), Gg = dzg^T x
+ *   and Gu = dzu^T x (both or neither).  workspace: qg_int8_gated_workspace_bytes(tokens, m, n) bytes, 16-byte aligned. */
 enum { QG_ACT_NONE = 0, QG_ACT_RELU = 1, QG_ACT_SILU = 2, QG_ACT_GELU = 3 };
 int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* Wq, const float* Ws, const uint16_t* bias_bf16,
                                const uint16_t* residual_bf16, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n,
@@ -391,15 +391,16 @@ int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* Wq, const f
 size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m);
 int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16_t* z_bf16, const uint16_t* x_bf16, const int8_t* Wq,
                                 const float* Ws, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group,
-                                uint16_t* dz_bf16, uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias, void* workspace,
-                                size_t workspace_bytes, void* stream);
+                                uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias, void* workspace, size_t workspace_bytes,
+                                void* stream);
 int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus, int act,
                           int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* zg_bf16,
                           uint16_t* zu_bf16, uint16_t* y_bf16, void* stream);
+size_t qg_int8_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n);
 int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, const uint16_t* zu_bf16, const uint16_t* x_bf16,
                            const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus, int act, int64_t tokens,
-                           int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* dzg_bf16, uint16_t* dzu_bf16,
-                           uint16_t* dx_bf16, uint16_t* Gg_bf16, uint16_t* Gu_bf16, void* stream);
+                           int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* dx_bf16, uint16_t* Gg_bf16,
+                           uint16_t* Gu_bf16, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Loss of a language model's head: softmax cross entropy over the vocabulary, without the logits in memory.
  * z = x W^T with x bf16 [tokens][h] and W bf16 [vocab][h]; labels int64 [tokens], a label outside [0, vocab) marks a token

@@ -198,11 +198,23 @@ __global__ __launch_bounds__(WM * 128 * KG, KG > 1 ? (MB == 1 ? 4 : 2) : WM == 2
         }
         if (p.splits > 1) {
             const int k0 = (int)blockIdx.y * p.k_chunk;
-            auto at = [&](LinOperand& op, auto slow) {
-                op.base = static_cast<const uint16_t*>(op.base) + (slow.value ? k0 * op.ld : (int64_t)k0);
+            auto at = [&](LinOperand& op, auto layout) {
+                constexpr int L = decltype(layout)::value;
+                static_assert(L == kBf16KFast || L == kBf16KSlow || L == kInt8KSlow, "others: not needed so far");
+                const int64_t off = L == kBf16KFast ? k0 : k0 * op.ld;
+                if constexpr (L == kInt8KSlow) {
+                    op.base = static_cast<const int8_t*>(op.base) + off;
+                    op.scales += (int64_t)k0 * op.sgroups;
+                } else {
+                    op.base = static_cast<const uint16_t*>(op.base) + off;
+                }
             };
-            at(p.A, std::integral_constant<bool, AL == kBf16KSlow>());
-            at(p.B, std::integral_constant<bool, BL == kBf16KSlow>());
+            at(p.A, std::integral_constant<int, AL>());
+            at(p.B, std::integral_constant<int, BL>());
+            if constexpr (TERMS == 2) {
+                at(p.A2, std::integral_constant<int, AL>());
+                at(p.B2, std::integral_constant<int, BL>());
+            }
             p.K = min(p.k_chunk, p.K - k0);
             p.epi.split((int)blockIdx.y);
         }
@@ -219,6 +231,47 @@ __global__ __launch_bounds__(64 * KW) void k_ksplit_epilogue(EpiProduct<OPB, EPI
     const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x);
     if (tile >= (uint32_t)(p.tiles_m * p.tiles_n)) return;
     ksplit_epi<AL, BL, EXACT, KW, TERMS>(p.A, p.B, p.A2, p.B2, p.epi, p.M, p.N, p.K, p.tiles_m, p.tiles_n, tile, smem);
+}
+
+// A part of a split contraction, in fp32: sum[split][row][col], rows `ld` (a multiple of 8) apart.
+struct PartRun {
+    static constexpr bool kPair = false, kCounted = true;
+    float* sum;
+    int64_t ld, stride;
+    __device__ void split(int s) { sum += s * stride; }
+    template <int R>
+    __device__ __forceinline__ void run(int row, int col, int left, float (&v)[R]) const {
+        float* p = sum + (int64_t)row * ld + col;
+#pragma unroll
+        for (int e = 0; e < R; e += 4)
+            if (e < left) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    }
+};
+
+// The parts added in order, rounded once: out[row][col], or out[to[row]][col] where `to` is given and not negative.  rows: *count of
+// them where that is given.
+static __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ sum, int64_t ld, int64_t stride, int splits,
+                                                           const int32_t* __restrict__ to, const int32_t* __restrict__ count, int rows,
+                                                           int cols, uint16_t* __restrict__ out, int64_t ld_out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = (cols + 7) / 8, row = i / chunks;
+    if (row >= (count != nullptr ? *count : rows)) return;
+    const int at = to != nullptr ? to[row] : (int)row, col = (int)(i - row * chunks) * 8;
+    if (at < 0) return;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    const float* p = sum + row * ld + col;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s, p += stride) {
+        a += reinterpret_cast<const f32x4*>(p)[0];
+        b += reinterpret_cast<const f32x4*>(p)[1];
+    }
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    store_run(out + (int64_t)at * ld_out + col, cols - col, v);
+}
+static int launch_join_parts(const float* sum, int64_t ld, int64_t stride, int splits, const int32_t* to, const int32_t* count, int64_t rows,
+                             int64_t cols, uint16_t* out, int64_t ld_out, hipStream_t st) {
+    hipLaunchKernelGGL(k_join_parts, dim3((unsigned)((rows * ((cols + 7) / 8) + 255) / 256)), dim3(256), 0, st, sum, ld, stride, splits, to,
+                       count, (int)rows, (int)cols, out, ld_out);
+    return check_launch();
 }
 
 // One product (TERMS == 2: the sum of two of one shape) by tiles of TM = 32 MB WM rows and TN columns (a pair: TN / 2 of each).

@@ -274,24 +274,6 @@ struct AddRun {
     }
 };
 
-// dx = the splits' sums, added in order.
-__global__ __launch_bounds__(256) void k_head_dx(const float* __restrict__ sum, int64_t stride, int splits, const int32_t* __restrict__ rows,
-                                                 const int32_t* __restrict__ count, int h, int hp, uint16_t* __restrict__ dx, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = hp / 8, row = i / chunks;
-    if (row >= *count) return;
-    const int to = rows[row], col = (int)(i - row * chunks) * 8;
-    if (to < 0) return;
-    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    const float* p = sum + row * hp + col;
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s, p += stride) {
-        a += reinterpret_cast<const f32x4*>(p)[0];
-        b += reinterpret_cast<const f32x4*>(p)[1];
-    }
-    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    store_run(dx + (int64_t)to * ld + col, h - col, v);
-}
-
 // ---- sizes ----
 static int check_head(int64_t tokens, int64_t h, int64_t vocab, int64_t& ld) {
     constexpr int64_t most = int64_t(1) << 24;
@@ -402,7 +384,7 @@ static int launch_head_rows(HeadRows a, hipStream_t st) {
 static int launch_head_dw(const uint16_t* dl, int64_t pitch, const uint16_t* x, int64_t hp, uint16_t* dW, int64_t ldc, int64_t width,
                           int64_t h, int64_t padded, const int32_t* count, hipStream_t st) {
     const int64_t tiles_m = pitch / kLinTM, tiles_n = hp / 256;
-    const KSlowOut out = {(int)width, (int)h, ldc, count};
+    const KSlowOut out = {(int)width, (int)h, ldc, count, nullptr, nullptr};
     hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(256), 0, st, dl, x, dW,
                        (int)pitch, (int)hp, (int)padded, (int)tiles_m, (int)tiles_n, out);
     return check_launch();
@@ -513,10 +495,7 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
         if (dW_bf16)
             if (int e = launch_head_dw(dl, pitch, r.xc, s.hp, dW_bf16 + v0 * ld, ld, width, h, s.padded, r.count, st)) return e;
     }
-    if (dx_bf16 && s.splits > 1) {
-        hipLaunchKernelGGL(k_head_dx, dim3((unsigned)((s.padded * (s.hp / 8) + 255) / 256)), dim3(256), 0, st, sum, stride, (int)s.splits, r.rows,
-                           r.count, (int)h, (int)s.hp, dx_bf16, ld);
-        return check_launch();
-    }
+    if (dx_bf16 && s.splits > 1)
+        return launch_join_parts(sum, s.hp, stride, (int)s.splits, r.rows, r.count, s.padded, h, dx_bf16, ld, st);
     return QG_OK;
 }

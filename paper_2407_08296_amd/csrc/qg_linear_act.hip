@@ -5,8 +5,8 @@
 //     gated forward:   y = act(x Wg^T) * (x Wu^T)
 //     gated backward:  dzg = dy zu act'(zg),  dzu = dy act(zg),  dx = dzg Wg + dzu Wu,  Gg = dzg^T x,  Gu = dzu^T x
 // W is dequantized while it is staged, as in the plain layer.  The forward passes are one launch: the activation is applied to
-// the fp32 sums, and z is rounded only where it is stored for the backward pass.  dz goes through memory as bf16 (it is an
-// operand of two products), made by one pass over dy and z.
+// the fp32 sums, and z is rounded only where it is stored for the backward pass.  dz goes through the workspace as bf16 (it is an
+// operand of two products), made by one pass over dy and z, in rows of whole cache lines whatever m is.
 #include "qg_epilogue.h"
 
 namespace qg {
@@ -32,16 +32,17 @@ static bool all_aligned(std::initializer_list<const void*> ps) {
 // ---- dz: 8 columns of a row per thread, 512 columns and every 4th row of a slab per wave.  Bound by HBM (6 bytes per element, a
 // pair 10).  dbias: the columns' sums over a slab from registers, the four waves added in order, slabs added by k_column_sums.
 template <bool PAIR>
-__global__ __launch_bounds__(256) void k_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg,
-                                                      uint16_t* dzu, float* __restrict__ part, int tokens, int m, int64_t ld, int rows,
-                                                      int kind) {
+__global__ __launch_bounds__(256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
+                                                      const uint16_t* __restrict__ zu, uint16_t* __restrict__ dzg,
+                                                      uint16_t* __restrict__ dzu, float* __restrict__ part, int tokens, int m, int64_t ld,
+                                                      int64_t ld_out, int rows, int kind) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = blockIdx.x * 512 + lane * 8, left = m - col;
     const int first = blockIdx.y * rows, last = min(first + rows, tokens);
     float sum[8] = {};
     if (left > 0) {
         for (int t = first + wave; t < last; t += 4) {
-            const int64_t at = (int64_t)t * ld + col;
+            const int64_t at = (int64_t)t * ld + col, to = (int64_t)t * ld_out + col;
             float d[8], z[8], o[8];
             load_run(dy + at, left, d);
             if constexpr (PAIR) {
@@ -55,8 +56,8 @@ __global__ __launch_bounds__(256) void k_act_backward(const uint16_t* dy, const 
                     o[e] = d[e] * u[e] * g;
                     p[e] = d[e] * a;
                 }
-                store_run(dzg + at, left, o);
-                store_run(dzu + at, left, p);
+                store_run(dzg + to, 8, o);        // (a row's last chunk is whole: zeros past its end)
+                store_run(dzu + to, 8, p);
             } else {
                 if (kind != QG_ACT_NONE) {
                     load_run(zg + at, left, z);
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(256) void k_act_backward(const uint16_t* dy, const 
                         float a;
                         o[e] = d[e] * act_grad(z[e], kind, a);
                     }
-                    if (dzg != nullptr) store_run(dzg + at, left, o);
+                    if (dzg != nullptr) store_run(dzg + to, 8, o);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = d[e];
@@ -117,10 +118,10 @@ static Slabs act_slabs(int64_t tokens, int64_t m) {
 
 template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
-                               int64_t tokens, int64_t m, int64_t ld, int kind, hipStream_t st) {
+                               int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
     const Slabs s = act_slabs(tokens, m);
     hipLaunchKernelGGL((k_act_backward<PAIR>), dim3((unsigned)((m + 511) / 512), (unsigned)s.count), dim3(256), 0, st, dy, zg, zu, dzg, dzu,
-                       part, (int)tokens, (int)m, ld, s.rows, kind);
+                       part, (int)tokens, (int)m, ld, ld_out, s.rows, kind);
     return check_launch();
 }
 
@@ -147,15 +148,55 @@ static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t s
     return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
-// dx = dzg Wg + dzu Wu
-static int launch_gated_dx(EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p, hipStream_t st) {
-    const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32), t128 = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
-    if (t32 <= 512) return launch_epilogue_ksplit<kBf16KFast, kInt8KSlow, 4, 2>(p, st);
+// dx = dzg Wg + dzu Wu, tokens x n.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split over workgroups, parts of
+// 512 at least, in fp32 through the workspace.
+static int64_t gated_dx_chunk(int64_t tokens, int64_t m, int64_t n) {
+    const int64_t t128 = ((tokens + 127) / 128) * ((n + 127) / 128), room = 512 / t128, most = m / 512, splits = room < most ? room : most;
+    return splits <= 1 ? m : ((m + splits - 1) / splits + 63) / 64 * 64;
+}
+static int launch_gated_dx(const LinOperand& dzg, const LinOperand& dzu, const LinOperand& Wg, const LinOperand& Wu, uint16_t* dx, int64_t ld,
+                           int64_t tokens, int64_t m, int64_t n, float* parts, hipStream_t st) {
+    const int64_t chunk = gated_dx_chunk(tokens, m, n);
+    if (chunk < m) {
+        const int64_t ldp = (n + 7) / 8 * 8;
+        EpiProduct<LinOperand, RunEpilogue<PartRun>> p;
+        p.A = dzg, p.A2 = dzu, p.B = Wg, p.B2 = Wu;
+        static_cast<PartRun&>(p.epi) = PartRun{parts, ldp, tokens * ldp};
+        p.M = (int)tokens, p.N = (int)n, p.K = (int)m;
+        p.k_chunk = (int)chunk;
+        p.splits = (int)((m + chunk - 1) / chunk);
+        if (int e = launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 128, 64, 2, true, true, 1, 2>(p, st)) return e;
+        return launch_join_parts(parts, ldp, tokens * ldp, p.splits, nullptr, nullptr, tokens, n, dx, ld, st);
+    }
+    EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p;
+    p.A = dzg, p.A2 = dzu, p.B = Wg, p.B2 = Wu;
+    p.epi = PlainEpilogue<uint16_t>{nullptr, dx, ld};
+    p.M = (int)tokens, p.N = (int)n, p.K = (int)m;
     if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256) >= 256)
         return launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 256, 64, 4, true, true, 1, 2>(p, st);
-    if (t128 < 160) return launch_epilogue_shape<kBf16KFast, kInt8KSlow, 1, 64, 64, 2, true, true, 1, 2>(p, st);
     return launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 128, 64, 2, true, true, 1, 2>(p, st);
 }
+
+// G = dz^T x for one or two dz of rows `ldz` apart: direct loads where x's rows start on 16 bytes and there are tiles for most CUs.
+static int launch_act_grad_w(const uint16_t* dz, const uint16_t* dz2, int64_t ldz, const uint16_t* x, int64_t ld_n, uint16_t* G, uint16_t* G2,
+                             int64_t tokens, int64_t m, int64_t n, hipStream_t st) {
+    const int64_t tiles_m = (m + kLinTM - 1) / kLinTM, tiles_n = (n + 255) / 256, count = dz2 != nullptr ? 2 : 1;
+    if (ld_n % 8 == 0 && tiles_m * tiles_n * count >= 256) {
+        const KSlowOut out = {(int)m, (int)n, ld_n, nullptr, dz2, G2};
+        hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8), (unsigned)count), dim3(256),
+                           0, st, dz, x, G, (int)ldz, (int)ld_n, (int)tokens, (int)tiles_m, (int)tiles_n, out);
+        return check_launch();
+    }
+    const LinOperand xo = {x, nullptr, ld_n, 0};
+    for (int i = 0; i < count; ++i) {
+        const LinOperand d = {i == 0 ? dz : dz2, nullptr, ldz, 0};
+        if (int e = launch_linear_backward<kInt8KSlow>(d, xo, nullptr, tokens, n, m, ld_n, d, xo, i == 0 ? G : G2, m, n, tokens, ld_n, st)) return e;
+    }
+    return QG_OK;
+}
+
+static int64_t dz_pitch(int64_t m) { return (m + 63) / 64 * 64; }
+static size_t whole_lines_of(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace qg
 
@@ -180,37 +221,38 @@ extern "C" int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* 
 
 extern "C" size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m) {
     if (tokens <= 0 || m <= 0 || tokens >= (int64_t(1) << 31) / m) return 0;
-    return (size_t)act_slabs(tokens, m).count * (size_t)m * 4;
+    return whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + (size_t)act_slabs(tokens, m).count * (size_t)m * 4;
 }
 
 extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16_t* z_bf16, const uint16_t* x_bf16, const int8_t* Wq,
                                            const float* Ws, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m,
-                                           int group, uint16_t* dz_bf16, uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias,
-                                           void* workspace, size_t workspace_bytes, void* stream) {
+                                           int group, uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
     if (!dy_bf16 || (!dx_bf16 && !G_bf16 && !dbias)) return QG_ERR_NULL;
     if ((dx_bf16 && (!Wq || !Ws)) || (G_bf16 && !x_bf16)) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
-    const bool products = dx_bf16 || G_bf16;
-    if (act != QG_ACT_NONE && (!z_bf16 || (products && !dz_bf16))) return QG_ERR_NULL;
+    if (act != QG_ACT_NONE && !z_bf16) return QG_ERR_NULL;
     if (int e = check_sizes(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
-    if (!all_aligned({dy_bf16, z_bf16, x_bf16, Wq, Ws, dz_bf16, dx_bf16, G_bf16, dbias, workspace})) return QG_ERR_ALIGN;
-    if (dbias && (!workspace || workspace_bytes < qg_int8_linear_act_workspace_bytes(tokens, m))) return QG_ERR_WORKSPACE;
+    if (!all_aligned({dy_bf16, z_bf16, x_bf16, Wq, Ws, dx_bf16, G_bf16, dbias, workspace})) return QG_ERR_ALIGN;
+    if ((dbias || act != QG_ACT_NONE) && (!workspace || workspace_bytes < qg_int8_linear_act_workspace_bytes(tokens, m)))
+        return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
-    float* part = dbias ? static_cast<float*>(workspace) : nullptr;
-    const uint16_t* dz = dy_bf16;
-    if (act != QG_ACT_NONE || dbias) {
-        uint16_t* out = act != QG_ACT_NONE && products ? dz_bf16 : nullptr;
-        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, out, nullptr, part, tokens, m, ld_m, act, st)) return e;
-        if (out) dz = out;
-    }
+    const bool products = dx_bf16 || G_bf16;
+    const int64_t ldz = dz_pitch(m);
+    uint16_t* dz = act != QG_ACT_NONE && products ? static_cast<uint16_t*>(workspace) : nullptr;
+    float* part = dbias ? reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2)) : nullptr;
+    if (dz || part)
+        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part, tokens, m, ld_m, ldz, act, st)) return e;
     if (dbias) {
         hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, part, act_slabs(tokens, m).count, (int)m, dbias);
         if (int e = check_launch()) return e;
     }
     if (!products) return QG_OK;
-    return qg_int8_linear_backward_ld(dz, x_bf16, Wq, Ws, tokens, m, n, ld_n, ld_m, group, dx_bf16, G_bf16, stream);
+    const LinOperand d = {dz ? dz : dy_bf16, nullptr, dz ? ldz : ld_m, 0}, x = {x_bf16, nullptr, ld_n, 0};
+    const LinOperand W = {Wq, Ws, ld_n, (int)((n + kGroup - 1) / kGroup)};
+    return launch_linear_backward<kInt8KSlow>(d, W, dx_bf16, tokens, n, m, ld_n, d, x, G_bf16, m, n, tokens, ld_n, st);
 }
 
 extern "C" int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus,
@@ -233,32 +275,35 @@ extern "C" int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, 
     return launch_gated_forward(p, (hipStream_t)stream);
 }
 
+extern "C" size_t qg_int8_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
+    if (check_sizes(tokens, m, n, kGroup)) return 0;
+    const int64_t chunk = gated_dx_chunk(tokens, m, n), splits = chunk < m ? (m + chunk - 1) / chunk : 0;
+    return 2 * whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + (size_t)splits * tokens * ((n + 7) / 8 * 8) * 4;
+}
+
 extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, const uint16_t* zu_bf16, const uint16_t* x_bf16,
                                       const int8_t* Wgq, const float* Wgs, const int8_t* Wuq, const float* Wus, int act, int64_t tokens,
-                                      int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* dzg_bf16, uint16_t* dzu_bf16,
-                                      uint16_t* dx_bf16, uint16_t* Gg_bf16, uint16_t* Gu_bf16, void* stream) {
-    if (!dy_bf16 || !zg_bf16 || !zu_bf16 || !dzg_bf16 || !dzu_bf16 || (!Gg_bf16 != !Gu_bf16) || (!dx_bf16 && !Gg_bf16)) return QG_ERR_NULL;
+                                      int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group, uint16_t* dx_bf16, uint16_t* Gg_bf16,
+                                      uint16_t* Gu_bf16, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dy_bf16 || !zg_bf16 || !zu_bf16 || (!Gg_bf16 != !Gu_bf16) || (!dx_bf16 && !Gg_bf16)) return QG_ERR_NULL;
     if ((dx_bf16 && (!Wgq || !Wgs || !Wuq || !Wus)) || (Gg_bf16 && !x_bf16)) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
     if (int e = check_sizes(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
-    if (!all_aligned({dy_bf16, zg_bf16, zu_bf16, x_bf16, Wgq, Wgs, Wuq, Wus, dzg_bf16, dzu_bf16, dx_bf16, Gg_bf16, Gu_bf16}))
-        return QG_ERR_ALIGN;
+    if (!all_aligned({dy_bf16, zg_bf16, zu_bf16, x_bf16, Wgq, Wgs, Wuq, Wus, dx_bf16, Gg_bf16, Gu_bf16, workspace})) return QG_ERR_ALIGN;
+    if (!workspace || workspace_bytes < qg_int8_gated_workspace_bytes(tokens, m, n)) return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
-    if (int e = launch_act_backward<true>(dy_bf16, zg_bf16, zu_bf16, dzg_bf16, dzu_bf16, nullptr, tokens, m, ld_m, act, st)) return e;
+    const int64_t ldz = dz_pitch(m);
+    const size_t dz_bytes = whole_lines_of((size_t)tokens * ldz * 2);
+    uint16_t *dzg = static_cast<uint16_t*>(workspace), *dzu = dzg + dz_bytes / 2;
+    float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * dz_bytes);
+    if (int e = launch_act_backward<true>(dy_bf16, zg_bf16, zu_bf16, dzg, dzu, nullptr, tokens, m, ld_m, ldz, act, st)) return e;
     const int sg = (int)((n + kGroup - 1) / kGroup);
-    const LinOperand dzg = {dzg_bf16, nullptr, ld_m, 0}, dzu = {dzu_bf16, nullptr, ld_m, 0};
-    if (dx_bf16) {
-        EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p;
-        p.A = dzg, p.A2 = dzu;
-        p.B = LinOperand{Wgq, Wgs, ld_n, sg}, p.B2 = LinOperand{Wuq, Wus, ld_n, sg};
-        p.epi = PlainEpilogue<uint16_t>{nullptr, dx_bf16, ld_n};
-        p.M = (int)tokens, p.N = (int)n, p.K = (int)m;
-        if (int e = launch_gated_dx(p, st)) return e;
-    }
+    if (dx_bf16)
+        if (int e = launch_gated_dx({dzg, nullptr, ldz, 0}, {dzu, nullptr, ldz, 0}, {Wgq, Wgs, ld_n, sg}, {Wuq, Wus, ld_n, sg}, dx_bf16, ld_n,
+                                    tokens, m, n, parts, st))
+            return e;
     if (!Gg_bf16) return QG_OK;
-    if (int e = qg_int8_linear_backward_ld(dzg_bf16, x_bf16, nullptr, nullptr, tokens, m, n, ld_n, ld_m, group, nullptr, Gg_bf16, stream))
-        return e;
-    return qg_int8_linear_backward_ld(dzu_bf16, x_bf16, nullptr, nullptr, tokens, m, n, ld_n, ld_m, group, nullptr, Gu_bf16, stream);
+    return launch_act_grad_w(dzg, dzu, ldz, x_bf16, ld_n, Gg_bf16, Gu_bf16, tokens, m, n, st);
 }

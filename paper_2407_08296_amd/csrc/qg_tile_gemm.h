@@ -656,18 +656,28 @@ __global__ __launch_bounds__(256, 2) void k_gemm_pair(LinProduct p0, LinProduct 
 // LLaMA shapes): the staging of the optimizer step's projection kernel for its gradient operand, applied to both -
 // direct global -> LDS loads into unpadded swizzled [k][x] tiles (no staging registers, no LDS write instructions),
 // two stages, the loads of step k+1 issued ahead of the MFMAs of step k, three workgroups per CU.
-// Rows of A and B are M and N elements apart, multiples of the tile.
-struct KSlowOut {          // RAGGED: C is smaller than the operands, whose columns past it may hold anything
+// Rows of A and B are M and N elements apart.  RAGGED: of any multiple of 8; C is out.rows x out.cols.  Loads are bounded by the end
+// of the operand, past which they read zeros: a last step that is not whole adds nothing.  What a tile reads past the end of a row
+// is the next row, and reaches elements only that are not stored.  One or two (gridDim.y) products of one shape with the same B.
+struct KSlowOut {
     int rows, cols;
     int64_t ldc;
-    const int32_t* device_k;   // the length of the contraction (a multiple of 32), which only the device knows
+    const int32_t* device_k;   // NULL, or the length of the contraction where only the device knows it
+    const uint16_t* A2;
+    void* C2;
 };
 template <typename OUT, bool RAGGED = false>
 __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __restrict__ A, const uint16_t* __restrict__ B,
                                                               OUT* __restrict__ C, int M, int N, int K, int tiles_m,
                                                               int tiles_n, KSlowOut out) {
     constexpr int TN = 256, BK = 32;
-    if constexpr (RAGGED) K = *out.device_k;
+    if constexpr (RAGGED) {
+        if (out.device_k != nullptr) K = *out.device_k;
+        if (blockIdx.y != 0) {
+            A = out.A2;
+            C = static_cast<OUT*>(out.C2);
+        }
+    }
     const int64_t ldc = RAGGED ? out.ldc : N;
     using AD = KMajorSwizzled<kLinTM, BK, 256>;
     using BD = KMajorSwizzled<TN, BK, 256>;
@@ -684,8 +694,9 @@ __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __
     const uint32_t a_byte = AD::lane_src_bytes(lane, M, 0);
     const uint32_t b_byte[2] = {BD::lane_src_bytes(lane, N, 0), BD::lane_src_bytes(lane, N, 1)};
     auto gload = [&](int kt, int stage) {
-        const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + (int64_t)kt * BK * M + i0);
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + (int64_t)kt * BK * N + j0);
+        const int64_t rows = K - (int64_t)kt * BK;
+        const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + (int64_t)kt * BK * M + i0, RAGGED ? bound_bytes(2 * ((rows - 1) * M + ((out.rows + 7) & ~7) - i0)) : 0x7FFFFFFF);
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + (int64_t)kt * BK * N + j0, RAGGED ? bound_bytes(2 * ((rows - 1) * N + ((out.cols + 7) & ~7) - j0)) : 0x7FFFFFFF);
 #pragma unroll
         for (int p = 0; p < AD::PER; ++p)
             buffer_load_lds16(ra, As[stage] + AD::load_row0(wave, p) * kLinTM, a_byte, 2u * (uint32_t)(AD::load_row0(wave, p) * M));
@@ -725,7 +736,7 @@ __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __
         __builtin_amdgcn_s_setprio(0);
     };
     auto landed = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };   // direct loads count like any other load
-    const int KT = K / BK;
+    const int KT = RAGGED ? (K + BK - 1) / BK : K / BK;
     // unrolled by two: constant LDS stages; loads past the end re-read the last K slab (in bounds, never consumed)
     gload(0, 0);
     landed();

@@ -36,7 +36,7 @@ EXPORTS = [
     "qg_int8_linear_forward_ld", "qg_int8_linear_backward_ld",
     "qg_residual_norm_forward", "qg_residual_norm_workspace_bytes", "qg_residual_norm_backward",
     "qg_int8_linear_act_forward", "qg_int8_linear_act_workspace_bytes", "qg_int8_linear_act_backward", "qg_int8_gated_forward",
-    "qg_int8_gated_backward", "qg_head_loss_workspace_bytes", "qg_head_loss_forward", "qg_head_loss_backward",
+    "qg_int8_gated_backward", "qg_int8_gated_workspace_bytes", "qg_head_loss_workspace_bytes", "qg_head_loss_forward", "qg_head_loss_backward",
 ]
 
 
@@ -150,9 +150,11 @@ def lib() -> C.CDLL:
         L.qg_int8_linear_act_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp]
         L.qg_int8_linear_act_workspace_bytes.restype = sz
         L.qg_int8_linear_act_workspace_bytes.argtypes = [i64, i64]
-        L.qg_int8_linear_act_backward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.qg_int8_linear_act_backward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, sz, vp]
         L.qg_int8_gated_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp]
-        L.qg_int8_gated_backward.argtypes = [vp] * 8 + [i32, i64, i64, i64, i64, i64, i32] + [vp] * 6
+        L.qg_int8_gated_workspace_bytes.restype = sz
+        L.qg_int8_gated_workspace_bytes.argtypes = [i64, i64, i64]
+        L.qg_int8_gated_backward.argtypes = [vp] * 8 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, sz, vp]
         L.qg_head_loss_workspace_bytes.restype = sz
         L.qg_head_loss_workspace_bytes.argtypes = [i64, i64, i64]
         L.qg_head_loss_forward.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
@@ -582,15 +584,14 @@ def int8_linear_act_backward(dy: torch.Tensor, z: torch.Tensor | None, x: torch.
     w = _weight(Wq, Ws, m, n)
     dx = _bf16_rows(dy, tokens, n) if want_dx else None
     G = _bf16_rows(dy, m, n) if want_G else None
-    dz = _bf16_rows(dy, tokens, m) if kind and (want_dx or want_G) else None
-    dbias = ws = None
+    dbias = dy.new_empty(m, dtype=torch.float32) if want_dbias else None
+    ws = None
     nbytes = 0
-    if want_dbias:
-        dbias = torch.empty(m, dtype=torch.float32, device=dy.device)
+    if want_dbias or kind:
         nbytes = lib().qg_int8_linear_act_workspace_bytes(tokens, m)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device)
+        ws = dy.new_empty(nbytes, dtype=torch.uint8)
     _check(lib().qg_int8_linear_act_backward(_ptr(dy, _BF16), _ptr(z, _BF16), _ptr(x, _BF16), *w, kind, tokens, m, n, n, m, GROUP,
-                                             _ptr(dz), _ptr(dx), _ptr(G), _ptr(dbias), _ptr(ws), nbytes, _stream()))
+                                             _ptr(dx), _ptr(G), _ptr(dbias), _ptr(ws), nbytes, _stream()))
     return dx, G, dbias
 
 
@@ -617,9 +618,10 @@ def int8_gated_backward(dy: torch.Tensor, zg: torch.Tensor, zu: torch.Tensor, x:
     w = _weight(Wgq, Wgs, m, n) + _weight(Wuq, Wus, m, n)
     dx = _bf16_rows(dy, tokens, n) if want_dx else None
     Gg, Gu = (_bf16_rows(dy, m, n), _bf16_rows(dy, m, n)) if want_G else (None, None)
-    dzg, dzu = _bf16_rows(dy, tokens, m), _bf16_rows(dy, tokens, m)
+    nbytes = lib().qg_int8_gated_workspace_bytes(tokens, m, n)
+    ws = dy.new_empty(nbytes, dtype=torch.uint8)
     _check(lib().qg_int8_gated_backward(_ptr(dy, _BF16), _ptr(zg, _BF16), _ptr(zu, _BF16), _ptr(x, _BF16), *w, _act(act), tokens, m, n, n,
-                                        m, GROUP, _ptr(dzg), _ptr(dzu), _ptr(dx), _ptr(Gg), _ptr(Gu), _stream()))
+                                        m, GROUP, _ptr(dx), _ptr(Gg), _ptr(Gu), _ptr(ws), nbytes, _stream()))
     return dx, Gg, Gu
 
 

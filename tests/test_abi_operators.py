@@ -65,15 +65,14 @@ def test_int8_linear_act(L):
         assert call(**{f"a{i}": FAKE + 2}) == 4
     nbytes = L.qg_int8_linear_act_workspace_bytes(16, 512)
     assert nbytes >= 512 * 4 and L.qg_int8_linear_act_workspace_bytes(0, 512) == 0 and L.qg_int8_linear_act_workspace_bytes(1 << 20, 1 << 20) == 0
-    # dy, z, x, Wq, Ws, act, tokens, m, n, ld_n, ld_m, group, dz, dx, G, dbias, ws, bytes, stream
-    call = caller(L.qg_int8_linear_act_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 3, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, FAKE, nbytes,
-                  None)
-    for i in (0, 1, 2, 3, 4, 12):
+    # dy, z, x, Wq, Ws, act, tokens, m, n, ld_n, ld_m, group, dx, G, dbias, ws, bytes, stream
+    call = caller(L.qg_int8_linear_act_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 3, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, nbytes, None)
+    for i in (0, 1, 2, 3, 4):
         assert call(**{f"a{i}": None}) == 1
-    assert call(a13=None, a14=None, a15=None) == 1
+    assert call(a12=None, a13=None, a14=None) == 1
     assert call(a5=9) == 2 and call(a6=0) == 2 and call(a9=8) == 2 and call(a10=500) == 2 and call(a11=64) == 3
-    assert call(a16=None) == 5 and call(a17=nbytes - 1) == 5
-    for i in (0, 1, 2, 3, 4, 12, 13, 14, 15, 16):
+    assert call(a15=None) == 5 and call(a16=nbytes - 1) == 5
+    for i in (0, 1, 2, 3, 4, 12, 13, 14, 15):
         assert call(**{f"a{i}": FAKE + 8}) == 4
 
 
@@ -85,13 +84,16 @@ def test_int8_gated(L):
     assert call(a5=4) == 2 and call(a6=0) == 2 and call(a9=250) == 2 and call(a10=513) == 2 and call(a11=32) == 3
     for i in (0, 1, 2, 3, 4, 12, 13, 14):
         assert call(**{f"a{i}": FAKE + 4}) == 4
-    # dy, zg, zu, x, Wgq, Wgs, Wuq, Wus, act, tokens, m, n, ld_n, ld_m, group, dzg, dzu, dx, Gg, Gu, stream
-    call = caller(L.qg_int8_gated_backward, *[FAKE] * 8, 2, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, FAKE, None)
-    for i in (0, 1, 2, 3, 4, 5, 6, 7, 15, 16, 18, 19):
+    # dy, zg, zu, x, Wgq, Wgs, Wuq, Wus, act, tokens, m, n, ld_n, ld_m, group, dx, Gg, Gu, ws, bytes, stream
+    nbytes = L.qg_int8_gated_workspace_bytes(16, 512, 256)
+    assert nbytes >= 2 * 16 * 512 * 2 and L.qg_int8_gated_workspace_bytes(0, 512, 256) == 0
+    call = caller(L.qg_int8_gated_backward, *[FAKE] * 8, 2, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, nbytes, None)
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 16, 17):
         assert call(**{f"a{i}": None}) == 1
-    assert call(a17=None, a18=None, a19=None) == 1
+    assert call(a15=None, a16=None, a17=None) == 1
     assert call(a8=7) == 2 and call(a10=0) == 2 and call(a12=1) == 2 and call(a13=528 + 1) == 2 and call(a14=1) == 3
-    for i in (0, 1, 2, 3, 4, 5, 6, 7, 15, 16, 17, 18, 19):
+    assert call(a18=None) == 5 and call(a19=nbytes - 1) == 5
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 15, 16, 17, 18):
         assert call(**{f"a{i}": FAKE + 8}) == 4
 
 

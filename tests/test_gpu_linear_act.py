@@ -176,8 +176,8 @@ def test_row_pitch_in_place_and_padding():
     dyp, zp, dxp, Gp, dbp = pad(dy, ld_m), pad(wz, ld_m), pad(x, ld_n), pad(G, ld_n), torch.empty(m, device=DEV)
     nbytes = L.qg_int8_linear_act_workspace_bytes(tokens, m)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
-    assert L.qg_int8_linear_act_backward(at(dyp), at(zp), at(xp), at(wgp), at(wg[1]), 3, tokens, m, n, ld_n, ld_m, 256, at(dyp), at(dxp),
-                                         at(Gp), at(dbp), at(ws), nbytes, st) == 0       # dz on top of dy
+    assert L.qg_int8_linear_act_backward(at(dyp), at(zp), at(xp), at(wgp), at(wg[1]), 3, tokens, m, n, ld_n, ld_m, 256, at(dxp), at(Gp),
+                                         at(dbp), at(ws), nbytes, st) == 0
     assert close(dxp, dx, ld_n) and close(Gp, G, ld_n) and torch.equal(dbp, db)
     want, zg, zu = qg.int8_gated_forward(x, *wg, *wu, want_z=True)
     yp, zgp, zup = pad(res, ld_m), pad(res, ld_m), pad(res, ld_m)
@@ -186,8 +186,10 @@ def test_row_pitch_in_place_and_padding():
     assert close(yp, want, ld_m) and close(zgp, zg, ld_m) and close(zup, zu, ld_m)
     dx, Gg, Gu = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu)
     dyp, zgp, zup, Ggp, Gup = pad(dy, ld_m), pad(zg, ld_m), pad(zu, ld_m), pad(Gg, ld_n), pad(Gu, ld_n)
+    nbytes = L.qg_int8_gated_workspace_bytes(tokens, m, n)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
     assert L.qg_int8_gated_backward(at(dyp), at(zgp), at(zup), at(xp), at(wgp), at(wg[1]), at(wup), at(wu[1]), 2, tokens, m, n, ld_n, ld_m,
-                                    256, at(zgp), at(zup), at(dxp), at(Ggp), at(Gup), st) == 0
+                                    256, at(dxp), at(Ggp), at(Gup), at(ws), nbytes, st) == 0
     assert close(dxp, dx, ld_n) and close(Ggp, Gg, ld_n) and close(Gup, Gu, ld_n)
 
 
