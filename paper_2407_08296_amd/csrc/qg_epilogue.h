@@ -5,7 +5,8 @@
 
 namespace qg {
 
-// R consecutive bf16 elements (R: 4 or 8), of which the first `left` exist; the others read as 0.
+// R consecutive bf16 elements (R: 4 or 8), of which the first `left` exist; the others read as 0.  (At a row's end the last element is
+// read again in the place of those: loads that do not wait for each other.)
 template <int R>
 __device__ __forceinline__ void load_run(const uint16_t* src, int left, float (&v)[R]) {
     uint32_t w[R / 2];
@@ -19,10 +20,12 @@ __device__ __forceinline__ void load_run(const uint16_t* src, int left, float (&
             const u32x4 o = *reinterpret_cast<const u32x4_align2*>(src);
             w[0] = o[0]; w[1] = o[1]; w[2] = o[2]; w[3] = o[3];
         }
-    } else {
+    } else if (left > 0) {
+        uint32_t x[R - 1];
 #pragma unroll
-        for (int e = 0; e < R - 1; ++e)
-            if (e < left) w[e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
+        for (int e = 0; e < R - 1; ++e) x[e] = src[min(e, left - 1)];
+#pragma unroll
+        for (int e = 0; e < R - 1; ++e) w[e >> 1] |= e < left ? x[e] << (16 * (e & 1)) : 0u;
     }
 #pragma unroll
     for (int e = 0; e < R / 2; ++e) {

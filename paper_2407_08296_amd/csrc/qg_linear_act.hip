@@ -29,19 +29,23 @@ static bool all_aligned(std::initializer_list<const void*> ps) {
     return true;
 }
 
-// ---- dz: 8 columns of a row per thread, 512 columns and every 4th row of a slab per wave.  Bound by HBM (6 bytes per element, a
-// pair 10).  dbias: the columns' sums over a slab from registers, the four waves added in order, slabs added by k_column_sums.
-template <bool PAIR>
-__global__ __launch_bounds__(256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
+// ---- dz: 8 columns of a row per thread, LANES threads per row.  Bound by HBM (6 bytes per element, a pair 10).  dbias: the columns'
+// sums over a slab from registers, a wave's rows by lane swaps, the four waves added in order, slabs added by k_column_sums.
+// LANES = 64: 512 columns and every 4th row of a slab per wave.  LANES = 8: 64 columns, all rows over 16 waves, so that dbias takes
+// no second kernel: up to 512 tokens (256 x 2048, gelu and dbias: 8.9 us with two kernels).
+template <bool PAIR, int LANES>
+__global__ __launch_bounds__(LANES == 8 ? 1024 : 256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
                                                       const uint16_t* __restrict__ zu, uint16_t* __restrict__ dzg,
                                                       uint16_t* __restrict__ dzu, float* __restrict__ part, int tokens, int m, int64_t ld,
                                                       int64_t ld_out, int rows, int kind) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * 512 + lane * 8, left = m - col;
+    constexpr int NT = LANES == 8 ? 1024 : 256, WAVES = NT / 64, STEP = NT / LANES;          // rows at a time
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * (8 * LANES) + lane * 8, left = m - col;
     const int first = blockIdx.y * rows, last = min(first + rows, tokens);
     float sum[8] = {};
     if (left > 0) {
-        for (int t = first + wave; t < last; t += 4) {
+#pragma unroll 2
+        for (int t = first + sub; t < last; t += STEP) {
             const int64_t at = (int64_t)t * ld + col, to = (int64_t)t * ld_out + col;
             float d[8], z[8], o[8];
             load_run(dy + at, left, d);
@@ -77,15 +81,22 @@ __global__ __launch_bounds__(256) void k_act_backward(const uint16_t* __restrict
         }
     }
     if (PAIR || part == nullptr) return;
-    __shared__ float sums[4][512];
+    __shared__ float sums[WAVES][8 * LANES];
+    if constexpr (LANES == 8) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = sum[e];
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int off = 8; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
+    }
+    if ((threadIdx.x & 63) < LANES)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[wave][e * LANES + lane] = sum[e];
     __syncthreads();
-    if (wave != 0 || left <= 0) return;
+    if (threadIdx.x >= LANES || left <= 0) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
 #pragma unroll
-        for (int w = 1; w < 4; ++w) sum[e] += sums[w][e * 64 + lane];
+        for (int w = 1; w < WAVES; ++w) sum[e] += sums[w][e * LANES + lane];
         if (e < left) part[(int64_t)blockIdx.y * m + col + e] = sum[e];
     }
 }
@@ -105,7 +116,7 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ 
     out[col] = s;
 }
 
-// Rows of a slab, and slabs: about a thousand workgroups where there are rows for them.
+// Rows of a slab, and slabs: about a thousand workgroups of 64 lanes per row where there are rows for them.
 struct Slabs {
     int rows, count;
 };
@@ -115,26 +126,50 @@ static Slabs act_slabs(int64_t tokens, int64_t m) {
     rows = (rows + 3) / 4 * 4;
     return {(int)rows, (int)((tokens + rows - 1) / rows)};
 }
+constexpr int64_t kActOneSlab = 512;      // tokens up to which dbias is made in one kernel
 
+// part: one row of sums per slab, or dbias itself where there is one slab
 template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
-                               int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
+                               float* dbias, int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
+    if (dbias != nullptr && tokens <= kActOneSlab) {
+        hipLaunchKernelGGL((k_act_backward<PAIR, 8>), dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, dy, zg, zu, dzg, dzu, dbias,
+                           (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
+        return check_launch();
+    }
     const Slabs s = act_slabs(tokens, m);
-    hipLaunchKernelGGL((k_act_backward<PAIR>), dim3((unsigned)((m + 511) / 512), (unsigned)s.count), dim3(256), 0, st, dy, zg, zu, dzg, dzu,
-                       part, (int)tokens, (int)m, ld, ld_out, s.rows, kind);
+    hipLaunchKernelGGL((k_act_backward<PAIR, 64>), dim3((unsigned)((m + 511) / 512), (unsigned)s.count), dim3(256), 0, st, dy, zg, zu, dzg,
+                       dzu, dbias != nullptr ? part : nullptr, (int)tokens, (int)m, ld, ld_out, s.rows, kind);
+    if (dbias != nullptr)
+        hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, part, s.count, (int)m, dbias);
     return check_launch();
 }
 
-// Tiles of the products with an epilogue, x W^T of one weight.
+// Tiles of the products with an epilogue, x W^T of one weight: those of the plain layer's forward pass (see launch_tile_gemm, which
+// has the measurements on both sides of each rule), but for its direct loads of whole 256 x 256 tiles: two register sets are ahead of
+// them here (4096 tokens, 4096 -> 11008, us: 417 / 456, the gated pair 778 / 885).
 template <typename EPI>
 static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
-    const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32), t128 = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
-    if (t32 <= 256) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 8, 1>(p, st);
-    if (t32 <= 768) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 4, 1>(p, st);
-    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256) >= 256)
-        return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
-    if (t128 < 256) return launch_epilogue_shape<kBf16KFast, kInt8KFast, 1, 64, 64, 2, true, true, 1, 1>(p, st);
-    return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 128, 64, 2, true, true, 1, 1>(p, st);
+    constexpr int AL = kBf16KFast, BL = kInt8KFast;
+    if (lin_ksplit<AL, BL>(p.M, p.N, p.K, 0)) {
+        const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32);
+        return t32 <= 256 ? launch_epilogue_ksplit<AL, BL, 8, 1>(p, st) : launch_epilogue_ksplit<AL, BL, 4, 1>(p, st);
+    }
+    auto tiles = [&](int tm, int tn) { return (int64_t)((p.M + tm - 1) / tm) * ((p.N + tn - 1) / tn); };
+    const bool small = lin_small<AL, BL>(p.M, p.N, 1);
+    if (p.K >= 512) {      // two groups of waves per tile while tiles are about a workgroup per CU or fewer
+        if (!small) {
+            if (p.K >= 768 && tiles(128, 128) <= 256) return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 2, 1>(p, st);
+        } else if (tiles(64, 64) <= 256) {
+            return launch_epilogue_shape<AL, BL, 1, 64, 64, 2, true, true, 2, 1>(p, st);
+        } else if (tiles(128, 64) <= 256 && p.K >= (p.K % 16 != 0 ? 4096 : p.K % 64 == 0 ? 640 : 960)) {
+            return launch_epilogue_shape<AL, BL, 2, 64, 64, 2, true, true, 2, 1>(p, st);
+        }
+    }
+    if (p.M >= 1024 && tiles(256, 256) >= 256) return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
+    if (small) return launch_epilogue_shape<AL, BL, 1, 64, 64, 2, true, true, 1, 1>(p, st);
+    if (tiles(128, 128) > 256 && tiles(128, 128) <= 512) return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, false, false, 1, 1>(p, st);
+    return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
 // ... of a pair: N columns of each.
@@ -143,8 +178,7 @@ static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t s
     const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32);
     if (t32 <= 256) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 8, 1>(p, st);
     if (t32 <= 768) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 4, 1>(p, st);
-    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128) >= 256)
-        return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
+    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128) >= 256) return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
     return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
@@ -243,12 +277,8 @@ extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16
     const int64_t ldz = dz_pitch(m);
     uint16_t* dz = act != QG_ACT_NONE && products ? static_cast<uint16_t*>(workspace) : nullptr;
     float* part = dbias ? reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2)) : nullptr;
-    if (dz || part)
-        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part, tokens, m, ld_m, ldz, act, st)) return e;
-    if (dbias) {
-        hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, part, act_slabs(tokens, m).count, (int)m, dbias);
-        if (int e = check_launch()) return e;
-    }
+    if (dz || dbias)
+        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part, dbias, tokens, m, ld_m, ldz, act, st)) return e;
     if (!products) return QG_OK;
     const LinOperand d = {dz ? dz : dy_bf16, nullptr, dz ? ldz : ld_m, 0}, x = {x_bf16, nullptr, ld_n, 0};
     const LinOperand W = {Wq, Ws, ld_n, (int)((n + kGroup - 1) / kGroup)};
@@ -298,7 +328,7 @@ extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* z
     const size_t dz_bytes = whole_lines_of((size_t)tokens * ldz * 2);
     uint16_t *dzg = static_cast<uint16_t*>(workspace), *dzu = dzg + dz_bytes / 2;
     float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * dz_bytes);
-    if (int e = launch_act_backward<true>(dy_bf16, zg_bf16, zu_bf16, dzg, dzu, nullptr, tokens, m, ld_m, ldz, act, st)) return e;
+    if (int e = launch_act_backward<true>(dy_bf16, zg_bf16, zu_bf16, dzg, dzu, nullptr, nullptr, tokens, m, ld_m, ldz, act, st)) return e;
     const int sg = (int)((n + kGroup - 1) / kGroup);
     if (dx_bf16)
         if (int e = launch_gated_dx({dzg, nullptr, ldz, 0}, {dzu, nullptr, ldz, 0}, {Wgq, Wgs, ld_n, sg}, {Wuq, Wus, ld_n, sg}, dx_bf16, ld_n,
