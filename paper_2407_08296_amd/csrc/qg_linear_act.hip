@@ -31,62 +31,64 @@ static bool all_aligned(std::initializer_list<const void*> ps) {
 
 // ---- dz: 8 columns of a row per thread, LANES threads per row.  Bound by HBM (6 bytes per element, a pair 10).  dbias: the columns'
 // sums over a slab from registers, a wave's rows by lane swaps, the four waves added in order, slabs added by k_column_sums.
-// LANES = 64: 512 columns and every 4th row of a slab per wave.  LANES = 8: 64 columns, all rows over 16 waves, so that dbias takes
-// no second kernel: up to 512 tokens (256 x 2048, gelu and dbias: 8.9 us with two kernels).
+// LANES = 64: 512 columns and every 4th row of a slab per wave.  LANES = 2: 16 columns and all rows, so that dbias takes no
+// second kernel and short batches reach all CUs: up to 512 tokens (256 x 2048, gelu and dbias, us: 8.9 with two kernels, 8.5 with 64
+// columns per workgroup).
 template <bool PAIR, int LANES>
-__global__ __launch_bounds__(LANES == 8 ? 1024 : 256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
+__global__ __launch_bounds__(LANES == 2 ? 512 : 256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
                                                       const uint16_t* __restrict__ zu, uint16_t* __restrict__ dzg,
                                                       uint16_t* __restrict__ dzu, float* __restrict__ part, int tokens, int m, int64_t ld,
                                                       int64_t ld_out, int rows, int kind) {
-    constexpr int NT = LANES == 8 ? 1024 : 256, WAVES = NT / 64, STEP = NT / LANES;          // rows at a time
+    constexpr int NT = LANES == 2 ? 512 : 256, WAVES = NT / 64, STEP = NT / LANES;          // rows at a time
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, wave = threadIdx.x >> 6;
     const int col = blockIdx.x * (8 * LANES) + lane * 8, left = m - col;
     const int first = blockIdx.y * rows, last = min(first + rows, tokens);
     float sum[8] = {};
-    if (left > 0) {
-#pragma unroll 2
-        for (int t = first + sub; t < last; t += STEP) {
-            const int64_t at = (int64_t)t * ld + col, to = (int64_t)t * ld_out + col;
-            float d[8], z[8], o[8];
-            load_run(dy + at, left, d);
+    auto fetch = [&](int t, float (&d)[8], float (&z)[8], float (&u)[8]) {
+        const int64_t at = (int64_t)t * ld + col;
+        load_run(dy + at, left, d);
+        if (PAIR || kind != QG_ACT_NONE) load_run(zg + at, left, z);
+        if constexpr (PAIR) load_run(zu + at, left, u);
+    };
+    auto use = [&](int t, const float (&d)[8], const float (&z)[8], const float (&u)[8]) {
+        const int64_t to = (int64_t)t * ld_out + col;
+        float o[8], p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a;
+            const float g = kind == QG_ACT_NONE && !PAIR ? 1.f : act_grad(z[e], kind, a);
             if constexpr (PAIR) {
-                float u[8], p[8];
-                load_run(zg + at, left, z);
-                load_run(zu + at, left, u);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float a;
-                    const float g = act_grad(z[e], kind, a);
-                    o[e] = d[e] * u[e] * g;
-                    p[e] = d[e] * a;
-                }
-                store_run(dzg + to, 8, o);        // (a row's last chunk is whole: zeros past its end)
-                store_run(dzu + to, 8, p);
+                o[e] = d[e] * u[e] * g;
+                p[e] = d[e] * a;
             } else {
-                if (kind != QG_ACT_NONE) {
-                    load_run(zg + at, left, z);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float a;
-                        o[e] = d[e] * act_grad(z[e], kind, a);
-                    }
-                    if (dzg != nullptr) store_run(dzg + to, 8, o);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = d[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += o[e];
+                o[e] = d[e] * g;
+                sum[e] += o[e];
             }
+        }
+        if (PAIR || dzg != nullptr) store_run(dzg + to, 8, o);        // (a row's last chunk is whole: zeros past its end)
+        if constexpr (PAIR) store_run(dzu + to, 8, p);
+    };
+    if (left > 0) {
+        int t = first + sub;
+        float d[2][8], z[2][8], u[2][8];
+        for (; t + STEP < last; t += 2 * STEP) {      // two rows on their way at once
+            fetch(t, d[0], z[0], u[0]);
+            fetch(t + STEP, d[1], z[1], u[1]);
+            use(t, d[0], z[0], u[0]);
+            use(t + STEP, d[1], z[1], u[1]);
+        }
+        if (t < last) {
+            fetch(t, d[0], z[0], u[0]);
+            use(t, d[0], z[0], u[0]);
         }
     }
     if (PAIR || part == nullptr) return;
     __shared__ float sums[WAVES][8 * LANES];
-    if constexpr (LANES == 8) {
+    if constexpr (LANES == 2) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int off = 8; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
+            for (int off = 2; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
     }
     if ((threadIdx.x & 63) < LANES)
 #pragma unroll
@@ -133,7 +135,7 @@ template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
                                float* dbias, int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
     if (dbias != nullptr && tokens <= kActOneSlab) {
-        hipLaunchKernelGGL((k_act_backward<PAIR, 8>), dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, dy, zg, zu, dzg, dzu, dbias,
+        hipLaunchKernelGGL((k_act_backward<PAIR, 2>), dim3((unsigned)((m + 15) / 16)), dim3(512), 0, st, dy, zg, zu, dzg, dzu, dbias,
                            (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
         return check_launch();
     }

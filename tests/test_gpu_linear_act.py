@@ -18,7 +18,8 @@ DEV = "cuda"
 U24 = 2.0 ** -24
 
 # (tokens, m, n): one token, one element, ragged and odd everything, around the tiles and the split contraction, 256 x 256 tiles
-CASES = [(1, 1, 1), (3, 5, 7), (1, 2050, 768), (33, 64, 130), (130, 333, 264), (77, 200, 521), (64, 519, 256), (200, 2112, 65),
+CASES = [(1, 1, 1), (3, 5, 7), (1, 2050, 768), (16, 70, 1300), (15, 33, 1024), (17, 70, 1300), (9, 100, 127), (2, 100, 129),
+         (33, 64, 130), (130, 333, 264), (77, 200, 521), (64, 519, 256), (200, 2112, 65),
          (500, 1100, 600), (2100, 600, 200), (1200, 5000, 72), (4096, 4096, 64), (4100, 4111, 72)]
 
 
