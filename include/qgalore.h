@@ -379,7 +379,7 @@ int qg_residual_norm_backward(const uint16_t* du_bf16, const void* dh_next, cons
  *   activation takes the fp32 sum; z (nullable) is what the backward pass wants, rounded to bf16.  y may be residual.
  * qg_int8_linear_act_backward: dz = dy act'(z);  dx = dz W, G = dz^T x, dbias (fp32 [m]) = sum over tokens of dz, each of them
  *   nullable (and then the inputs only it needs are too).  dz is rounded to bf16 for the products, not for dbias.  QG_ACT_NONE
- *   needs no z.  The residual's gradient is dy.  workspace: qg_int8_linear_act_workspace_bytes(tokens, m) bytes, 16-byte aligned;
+ *   needs no z.  The residual's gradient is dy.  workspace: qg_int8_linear_act_workspace_bytes(tokens, m, n) bytes, 16-byte aligned;
  *   not needed for dx and G with QG_ACT_NONE.
  * qg_int8_gated_forward:  y = act(x Wg^T) * (x Wu^T), both weights m x n; zg, zu: both (for the backward pass) or neither.
  * qg_int8_gated_backward: dzg = dy zu act'(zg), dzu = dy act(zg), rounded to bf16;  dx = dzg Wg + dzu Wu (nullable), Gg = dzg^T x
@@ -388,7 +388,7 @@ enum { QG_ACT_NONE = 0, QG_ACT_RELU = 1, QG_ACT_SILU = 2, QG_ACT_GELU = 3 };
 int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* Wq, const float* Ws, const uint16_t* bias_bf16,
                                const uint16_t* residual_bf16, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n,
                                int64_t ld_m, int group, uint16_t* z_bf16, uint16_t* y_bf16, void* stream);
-size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m);
+size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m, int64_t n);
 int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16_t* z_bf16, const uint16_t* x_bf16, const int8_t* Wq,
                                 const float* Ws, int act, int64_t tokens, int64_t m, int64_t n, int64_t ld_n, int64_t ld_m, int group,
                                 uint16_t* dx_bf16, uint16_t* G_bf16, float* dbias, void* workspace, size_t workspace_bytes,

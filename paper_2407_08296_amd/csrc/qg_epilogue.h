@@ -177,10 +177,11 @@ struct EpiProduct {
     OPB B, B2;
     EPI epi;
     int M, N, K, tiles_m, tiles_n;
-    // An extent that only the device knows: *count elements along `dim`, at most what M, N or K says, and a multiple of 256 (so
-    // that tiles and steps are as whole as the host takes them to be).  The grid is the largest one's; the rest ends at once.
+    // An extent that only the device knows: *count elements along `dim`, at most what M, N or K says, and a multiple of `unit` (at
+    // least 64: a whole number of steps; tiles are taken to be whole if unit is so many of them).  The grid is the largest one's;
+    // the rest ends at once.
     const int32_t* count = nullptr;
-    int dim = kDimM;
+    int dim = kDimM, unit = 0;
     // The contraction over `splits` workgroups per tile (blockIdx.y): `k_chunk` of it each (a multiple of 64), epi.split(s) for the
     // s-th one.
     int splits = 1, k_chunk = 0;
@@ -251,11 +252,12 @@ struct PartRun {
     }
 };
 
-// The parts added in order, rounded once: out[row][col], or out[to[row]][col] where `to` is given and not negative.  rows: *count of
-// them where that is given.
+// The parts added in order (times *scale), rounded once: out[row][col], or out[to[row]][col] where `to` is given and not negative.
+// rows: *count of them where that is given.
 static __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ sum, int64_t ld, int64_t stride, int splits,
-                                                           const int32_t* __restrict__ to, const int32_t* __restrict__ count, int rows,
-                                                           int cols, uint16_t* __restrict__ out, int64_t ld_out) {
+                                                           const int32_t* __restrict__ to, const int32_t* __restrict__ count,
+                                                           const float* __restrict__ scale, int rows, int cols,
+                                                           uint16_t* __restrict__ out, int64_t ld_out) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = (cols + 7) / 8, row = i / chunks;
     if (row >= (count != nullptr ? *count : rows)) return;
     const int at = to != nullptr ? to[row] : (int)row, col = (int)(i - row * chunks) * 8;
@@ -267,13 +269,14 @@ static __global__ __launch_bounds__(256) void k_join_parts(const float* __restri
         a += reinterpret_cast<const f32x4*>(p)[0];
         b += reinterpret_cast<const f32x4*>(p)[1];
     }
-    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    const float f = scale != nullptr ? *scale : 1.f;
+    const float v[8] = {f * a[0], f * a[1], f * a[2], f * a[3], f * b[0], f * b[1], f * b[2], f * b[3]};
     store_run(out + (int64_t)at * ld_out + col, cols - col, v);
 }
-static int launch_join_parts(const float* sum, int64_t ld, int64_t stride, int splits, const int32_t* to, const int32_t* count, int64_t rows,
-                             int64_t cols, uint16_t* out, int64_t ld_out, hipStream_t st) {
+static int launch_join_parts(const float* sum, int64_t ld, int64_t stride, int splits, const int32_t* to, const int32_t* count,
+                             const float* scale, int64_t rows, int64_t cols, uint16_t* out, int64_t ld_out, hipStream_t st) {
     hipLaunchKernelGGL(k_join_parts, dim3((unsigned)((rows * ((cols + 7) / 8) + 255) / 256)), dim3(256), 0, st, sum, ld, stride, splits, to,
-                       count, (int)rows, (int)cols, out, ld_out);
+                       count, scale, (int)rows, (int)cols, out, ld_out);
     return check_launch();
 }
 
@@ -286,7 +289,8 @@ static int launch_epilogue_shape(EpiProduct<OPB, EPI> p, hipStream_t st) {
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
     if (tiles * (WM * 128 * KG) >= (int64_t(1) << 32)) return QG_ERR_SHAPE;   // threads of one launch
     const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
-    const bool exact = p.M % TM == 0 && p.N % TC == 0 && p.K % BK == 0 && p.A.ld % 8 == 0 && p.B.ld % 16 == 0;
+    const int M = p.count != nullptr && p.dim == kDimM ? p.unit : p.M, N = p.count != nullptr && p.dim == kDimN ? p.unit : p.N;
+    const bool exact = M % TM == 0 && N % TC == 0 && p.K % BK == 0 && p.A.ld % 8 == 0 && p.B.ld % 16 == 0;
     if (exact)
         hipLaunchKernelGGL((k_gemm_epilogue<AL, BL, true, MB, TN, BK, WM, DEEP_EXACT, KG, TERMS, OPB, EPI>), dim3(grid, p.splits),
                            dim3(128 * WM * KG), 0, st, p);

@@ -10,6 +10,8 @@
 //           belong to one token and most of the reduction stays in its registers.
 // backward: the vocabulary in pieces.  For each, the logits are computed again with dl in the epilogue (bf16, the operand of the
 //           two products), then dW's rows of the piece, and dx, which is added up over the pieces in fp32.
+// dl is held relative to the largest |dloss|, which dx and dW are multiplied by in fp32: a mean's gradient at a label is then close to -1,
+// which bf16 holds exactly, and not that fraction of 1/T, whose rounding every element of a row would share.
 // Eight T V h flop against six with the logits kept; T x V numbers are never stored, only T x piece.
 #include "qg_epilogue.h"
 
@@ -138,39 +140,49 @@ struct HeadRows {
     int tokens, padded, unit, h, hp, per;   // padded: tokens up to a multiple of unit; per: tokens of a workgroup
     uint16_t* xc;
     int32_t *rows, *label32, *count;
-    float *lse, *dloss;                  // backward only
+    float *lse, *dloss, *scale;          // backward only; dloss: relative to *scale, the largest |dloss|
     float *loss_out, *lse_out;           // forward only
     uint16_t* dx;                        // backward only, may be NULL
 };
 __global__ __launch_bounds__(256) void k_head_rows(HeadRows a) {
     __shared__ int before_s[4], all_s[4];
+    __shared__ float most_s[4];
     const int first = (int)blockIdx.x * a.per, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto learned = [&](int t) {
         const int64_t l = a.labels[t];
         return l >= 0 && l < a.vocab;
     };
     int before = 0, all = 0;
+    float most = 0.f;
 #pragma unroll 4
     for (int t = threadIdx.x; t < a.tokens; t += 256) {
         const int one = learned(t);
         all += one;
         before += t < first ? one : 0;
+        if (a.scale != nullptr) most = fmaxf(most, one ? fabsf(a.dloss_in[t]) : 0.f);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
         all += __shfl_xor(all, off, 64);
         before += __shfl_xor(before, off, 64);
+        most = fmaxf(most, __shfl_xor(most, off, 64));
     }
     if (lane == 0) {
         before_s[wave] = before;
         all_s[wave] = all;
+        most_s[wave] = most;
     }
     __syncthreads();
     all = all_s[0] + all_s[1] + all_s[2] + all_s[3];
     before = before_s[0] + before_s[1] + before_s[2] + before_s[3];
+    most = fmaxf(fmaxf(most_s[0], most_s[1]), fmaxf(most_s[2], most_s[3]));
+    if (!(most > 0.f && most < INFINITY)) most = 1.f;
     // (rows of zeros where no token has a loss: no product is empty)
     const int up = max((all + a.unit - 1) / a.unit, 1) * a.unit;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = up;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *a.count = up;
+        if (a.scale != nullptr) *a.scale = most;
+    }
     const int last = min(first + a.per, a.padded), chunks = a.hp / 8;
     for (int t0 = first; t0 < last; t0 += 64) {
         // where the tokens go: those with a loss in their order, the others behind them while there are rows to fill with zeros
@@ -186,7 +198,7 @@ __global__ __launch_bounds__(256) void k_head_rows(HeadRows a) {
                 a.label32[to] = one ? (int)a.labels[t] : -1;
                 if (a.lse != nullptr) {
                     a.lse[to] = one ? a.lse_in[t] : 0.f;
-                    a.dloss[to] = one ? a.dloss_in[t] : 0.f;
+                    a.dloss[to] = one ? a.dloss_in[t] / most : 0.f;
                 }
             }
             if (a.loss_out != nullptr && here && t < a.tokens && !one) {
@@ -249,6 +261,7 @@ struct AddRun {
     float* sum;              // [splits][padded tokens][ld_sum]
     uint16_t* out;
     const int32_t* rows;
+    const float* scale;
     int64_t ld_sum, ld_out, stride;
     bool begins, ends;       // with this piece; ends only where there is one split
     __device__ void split(int s) { sum += s * stride; }
@@ -269,6 +282,9 @@ struct AddRun {
             for (int e = 0; e < R; e += 4)
                 if (e < left) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
         } else if (const int to = rows[row]; to >= 0) {
+            const float f = *scale;
+#pragma unroll
+            for (int e = 0; e < R; ++e) v[e] *= f;
             store_run(out + (int64_t)to * ld_out + col, left, v);
         }
     }
@@ -333,12 +349,12 @@ static int64_t head_piece(int64_t tokens, int64_t vocab) {
 
 struct HeadSpace {     // a call's workspace, in bytes
     int64_t piece, chunk, splits, hp, unit, padded, slots;     // chunk: contraction of dx per workgroup
-    size_t count, rows, labels, lse, dloss, x, sum, dl, part, logit, total;
+    size_t count, scale, rows, labels, lse, dloss, x, sum, dl, part, logit, total;
 };
 static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab, bool backward) {
     HeadSpace s = {};
     s.hp = up(h, backward ? 256 : 8);
-    s.unit = tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256;
+    s.unit = tokens <= 64 ? 64 : tokens <= 512 ? 128 : 256;
     s.padded = up(tokens, s.unit);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -347,6 +363,7 @@ static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab, bool backw
         return from;
     };
     s.count = take(4);
+    s.scale = take(4);
     s.rows = take((size_t)s.padded * 4);
     s.labels = take((size_t)s.padded * 4);
     s.x = take((size_t)s.padded * s.hp * 2);
@@ -382,9 +399,9 @@ static int launch_head_rows(HeadRows a, hipStream_t st) {
 // dW's rows of a piece, dl^T x: direct loads of whole tiles.  dl's rows are a multiple of 128 elements apart, x's of 256, so that a
 // tile never leaves its row; what stands between their ends and that only reaches elements that are not stored.
 static int launch_head_dw(const uint16_t* dl, int64_t pitch, const uint16_t* x, int64_t hp, uint16_t* dW, int64_t ldc, int64_t width,
-                          int64_t h, int64_t padded, const int32_t* count, hipStream_t st) {
+                          int64_t h, int64_t padded, const int32_t* count, const float* scale, hipStream_t st) {
     const int64_t tiles_m = pitch / kLinTM, tiles_n = hp / 256;
-    const KSlowOut out = {(int)width, (int)h, ldc, count, nullptr, nullptr};
+    const KSlowOut out = {(int)width, (int)h, ldc, count, nullptr, nullptr, scale};
     hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(256), 0, st, dl, x, dW,
                        (int)pitch, (int)hp, (int)padded, (int)tiles_m, (int)tiles_n, out);
     return check_launch();
@@ -431,6 +448,7 @@ extern "C" int qg_head_loss_forward(const uint16_t* x_bf16, const uint16_t* W_bf
         p.N = (int)s.padded;
         p.count = r.count;
         p.dim = kDimN;
+        p.unit = (int)s.unit;
     }
     f32x2* part = reinterpret_cast<f32x2*>(at + s.part);
     float* label_logit = reinterpret_cast<float*>(at + s.logit);
@@ -462,6 +480,7 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
     r.count = reinterpret_cast<int32_t*>(at + s.count);
     r.lse = reinterpret_cast<float*>(at + s.lse);
     r.dloss = reinterpret_cast<float*>(at + s.dloss);
+    r.scale = reinterpret_cast<float*>(at + s.scale);
     r.dx = dx_bf16;
     if (int e = launch_head_rows(r, st)) return e;
     uint16_t* dl = reinterpret_cast<uint16_t*>(at + s.dl);
@@ -478,24 +497,26 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
             p.M = (int)s.padded, p.N = (int)width, p.K = (int)h;
             p.count = r.count;
             p.dim = kDimM;
+            p.unit = (int)s.unit;
             if (int e = launch_head<kBf16KFast, kBf16KFast>(p, head_tile(s.padded, width), st)) return e;
         }
         if (dx_bf16) {
             EpiProduct<LinOperand, RunEpilogue<AddRun>> p;
             p.A = p.A2 = d;
             p.B = p.B2 = W;
-            static_cast<AddRun&>(p.epi) = AddRun{sum, dx_bf16, r.rows, s.hp, ld, stride, v0 == 0, v0 + width == vocab && s.splits == 1};
+            static_cast<AddRun&>(p.epi) = AddRun{sum, dx_bf16, r.rows, r.scale, s.hp, ld, stride, v0 == 0, v0 + width == vocab && s.splits == 1};
             p.M = (int)s.padded, p.N = (int)h, p.K = (int)width;
             p.count = r.count;
             p.dim = kDimM;
+            p.unit = (int)s.unit;
             p.k_chunk = (int)s.chunk;
             p.splits = (int)((width + s.chunk - 1) / s.chunk);
             if (int e = launch_head<kBf16KFast, kBf16KSlow>(p, head_dx_tile(s.padded, h), st)) return e;
         }
         if (dW_bf16)
-            if (int e = launch_head_dw(dl, pitch, r.xc, s.hp, dW_bf16 + v0 * ld, ld, width, h, s.padded, r.count, st)) return e;
+            if (int e = launch_head_dw(dl, pitch, r.xc, s.hp, dW_bf16 + v0 * ld, ld, width, h, s.padded, r.count, r.scale, st)) return e;
     }
     if (dx_bf16 && s.splits > 1)
-        return launch_join_parts(sum, s.hp, stride, (int)s.splits, r.rows, r.count, s.padded, h, dx_bf16, ld, st);
+        return launch_join_parts(sum, s.hp, stride, (int)s.splits, r.rows, r.count, r.scale, s.padded, h, dx_bf16, ld, st);
     return QG_OK;
 }

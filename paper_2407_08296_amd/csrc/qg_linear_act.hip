@@ -202,7 +202,7 @@ static int launch_gated_dx(const LinOperand& dzg, const LinOperand& dzu, const L
         p.k_chunk = (int)chunk;
         p.splits = (int)((m + chunk - 1) / chunk);
         if (int e = launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 128, 64, 2, true, true, 1, 2>(p, st)) return e;
-        return launch_join_parts(parts, ldp, tokens * ldp, p.splits, nullptr, nullptr, tokens, n, dx, ld, st);
+        return launch_join_parts(parts, ldp, tokens * ldp, p.splits, nullptr, nullptr, nullptr, tokens, n, dx, ld, st);
     }
     EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p;
     p.A = dzg, p.A2 = dzu, p.B = Wg, p.B2 = Wu;
@@ -213,14 +213,39 @@ static int launch_gated_dx(const LinOperand& dzg, const LinOperand& dzu, const L
     return launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 128, 64, 2, true, true, 1, 2>(p, st);
 }
 
-// G = dz^T x for one or two dz of rows `ldz` apart: direct loads where x's rows start on 16 bytes and there are tiles for most CUs.
+// Rows of x at a pitch of whole 16-byte chunks, zeros past their ends.
+__global__ __launch_bounds__(256) void k_align_rows(const uint16_t* __restrict__ x, int64_t ld, int rows, int cols, uint16_t* __restrict__ out,
+                                                    int64_t pitch) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = pitch / 8, row = i / chunks;
+    if (row >= rows) return;
+    const int col = (int)(i - row * chunks) * 8;
+    float v[8];
+    load_run(x + row * ld + col, cols - col, v);
+    store_run(out + row * pitch + col, 8, v);
+}
+
+// G = dz^T x for one or two dz of rows `ldz` apart (a multiple of 8).  Direct loads where there are tiles of 128 x 256 for every CU; they
+// want rows that start on 16 bytes, and x is copied to such where it has others (600 tokens, 2997 and 2 x 6869: the products without
+// direct loads 165 us).
+static bool grad_w_direct(int64_t m, int64_t n, int count) { return ((m + kLinTM - 1) / kLinTM) * ((n + 255) / 256) * count >= 256; }
+static size_t grad_w_copy_bytes(int64_t tokens, int64_t m, int64_t n, int count) {   // of x, whatever its pitch turns out to be
+    return grad_w_direct(m, n, count) && n % 8 != 0 ? (size_t)tokens * ((n + 7) / 8 * 8) * 2 : 0;
+}
 static int launch_act_grad_w(const uint16_t* dz, const uint16_t* dz2, int64_t ldz, const uint16_t* x, int64_t ld_n, uint16_t* G, uint16_t* G2,
-                             int64_t tokens, int64_t m, int64_t n, hipStream_t st) {
-    const int64_t tiles_m = (m + kLinTM - 1) / kLinTM, tiles_n = (n + 255) / 256, count = dz2 != nullptr ? 2 : 1;
-    if (ld_n % 8 == 0 && tiles_m * tiles_n * count >= 256) {
-        const KSlowOut out = {(int)m, (int)n, ld_n, nullptr, dz2, G2};
+                             int64_t tokens, int64_t m, int64_t n, uint16_t* copy, hipStream_t st) {
+    const int count = dz2 != nullptr ? 2 : 1;
+    if (grad_w_direct(m, n, count)) {
+        int64_t ldx = ld_n;
+        if (ld_n % 8 != 0) {
+            ldx = (n + 7) / 8 * 8;
+            hipLaunchKernelGGL(k_align_rows, dim3((unsigned)((tokens * (ldx / 8) + 255) / 256)), dim3(256), 0, st, x, ld_n, (int)tokens, (int)n,
+                               copy, ldx);
+            x = copy;
+        }
+        const int64_t tiles_m = (m + kLinTM - 1) / kLinTM, tiles_n = (n + 255) / 256;
+        const KSlowOut out = {(int)m, (int)n, ld_n, nullptr, dz2, G2, nullptr};
         hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8), (unsigned)count), dim3(256),
-                           0, st, dz, x, G, (int)ldz, (int)ld_n, (int)tokens, (int)tiles_m, (int)tiles_n, out);
+                           0, st, dz, x, G, (int)ldz, (int)ldx, (int)tokens, (int)tiles_m, (int)tiles_n, out);
         return check_launch();
     }
     const LinOperand xo = {x, nullptr, ld_n, 0};
@@ -255,9 +280,10 @@ extern "C" int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* 
     return launch_act_forward(p, (hipStream_t)stream);
 }
 
-extern "C" size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m) {
-    if (tokens <= 0 || m <= 0 || tokens >= (int64_t(1) << 31) / m) return 0;
-    return whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + (size_t)act_slabs(tokens, m).count * (size_t)m * 4;
+extern "C" size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
+    if (check_sizes(tokens, m, n, kGroup)) return 0;
+    return whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + whole_lines_of((size_t)act_slabs(tokens, m).count * (size_t)m * 4) +
+           grad_w_copy_bytes(tokens, m, n, 1);
 }
 
 extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16_t* z_bf16, const uint16_t* x_bf16, const int8_t* Wq,
@@ -272,18 +298,24 @@ extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
     if (!all_aligned({dy_bf16, z_bf16, x_bf16, Wq, Ws, dx_bf16, G_bf16, dbias, workspace})) return QG_ERR_ALIGN;
-    if ((dbias || act != QG_ACT_NONE) && (!workspace || workspace_bytes < qg_int8_linear_act_workspace_bytes(tokens, m)))
+    if ((dbias || act != QG_ACT_NONE) && (!workspace || workspace_bytes < qg_int8_linear_act_workspace_bytes(tokens, m, n)))
         return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     const bool products = dx_bf16 || G_bf16;
     const int64_t ldz = dz_pitch(m);
     uint16_t* dz = act != QG_ACT_NONE && products ? static_cast<uint16_t*>(workspace) : nullptr;
-    float* part = dbias ? reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2)) : nullptr;
+    float* part_at = reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2));
     if (dz || dbias)
-        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part, dbias, tokens, m, ld_m, ldz, act, st)) return e;
+        if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part_at, dbias, tokens, m, ld_m, ldz, act, st)) return e;
     if (!products) return QG_OK;
     const LinOperand d = {dz ? dz : dy_bf16, nullptr, dz ? ldz : ld_m, 0}, x = {x_bf16, nullptr, ld_n, 0};
     const LinOperand W = {Wq, Ws, ld_n, (int)((n + kGroup - 1) / kGroup)};
+    if (G_bf16 && dz && grad_w_direct(m, n, 1)) {
+        if (dx_bf16)
+            if (int e = launch_linear_backward<kInt8KSlow>(d, W, dx_bf16, tokens, n, m, ld_n, d, x, nullptr, m, n, tokens, ld_n, st)) return e;
+        char* copy = reinterpret_cast<char*>(part_at) + whole_lines_of((size_t)act_slabs(tokens, m).count * (size_t)m * 4);
+        return launch_act_grad_w(dz, nullptr, ldz, x_bf16, ld_n, G_bf16, nullptr, tokens, m, n, reinterpret_cast<uint16_t*>(copy), st);
+    }
     return launch_linear_backward<kInt8KSlow>(d, W, dx_bf16, tokens, n, m, ld_n, d, x, G_bf16, m, n, tokens, ld_n, st);
 }
 
@@ -310,7 +342,8 @@ extern "C" int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, 
 extern "C" size_t qg_int8_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
     if (check_sizes(tokens, m, n, kGroup)) return 0;
     const int64_t chunk = gated_dx_chunk(tokens, m, n), splits = chunk < m ? (m + chunk - 1) / chunk : 0;
-    return 2 * whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + (size_t)splits * tokens * ((n + 7) / 8 * 8) * 4;
+    return 2 * whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + whole_lines_of((size_t)splits * tokens * ((n + 7) / 8 * 8) * 4) +
+           grad_w_copy_bytes(tokens, m, n, 2);
 }
 
 extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, const uint16_t* zu_bf16, const uint16_t* x_bf16,
@@ -337,5 +370,7 @@ extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* z
                                     tokens, m, n, parts, st))
             return e;
     if (!Gg_bf16) return QG_OK;
-    return launch_act_grad_w(dzg, dzu, ldz, x_bf16, ld_n, Gg_bf16, Gu_bf16, tokens, m, n, st);
+    const int64_t chunk = gated_dx_chunk(tokens, m, n), splits = chunk < m ? (m + chunk - 1) / chunk : 0;
+    char* copy = reinterpret_cast<char*>(parts) + whole_lines_of((size_t)splits * tokens * ((n + 7) / 8 * 8) * 4);
+    return launch_act_grad_w(dzg, dzu, ldz, x_bf16, ld_n, Gg_bf16, Gu_bf16, tokens, m, n, reinterpret_cast<uint16_t*>(copy), st);
 }

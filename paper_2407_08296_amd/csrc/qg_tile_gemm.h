@@ -665,6 +665,7 @@ struct KSlowOut {
     const int32_t* device_k;   // NULL, or the length of the contraction where only the device knows it
     const uint16_t* A2;
     void* C2;
+    const float* scale;        // NULL, or a factor of C
 };
 template <typename OUT, bool RAGGED = false>
 __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __restrict__ A, const uint16_t* __restrict__ B,
@@ -751,22 +752,29 @@ __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __
         landed();
         __syncthreads();
     }
+    const float factor = RAGGED && out.scale != nullptr ? *out.scale : 1.f;
     // Straight from the accumulators: three workgroups per CU cover for each other's stores here (64 tokens, 4096 x 11008:
     // 20.8 us, as 16-byte runs through LDS 23.0; 4096 tokens 329 and 331).
+    auto store = [&](auto whole) {
 #pragma unroll
-    for (int a = 0; a < MB; ++a)
+        for (int a = 0; a < MB; ++a)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int col = j0 + wn * 128 + b * 32 + (lane & 31);
+            for (int b = 0; b < NB; ++b) {
+                const int col = j0 + wn * 128 + b * 32 + (lane & 31);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int row = i0 + wm * 64 + a * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-                const float x = acc[a][b][v];
-                if (RAGGED && (row >= out.rows || col >= out.cols)) continue;
-                if constexpr (sizeof(OUT) == 4) C[(int64_t)row * ldc + col] = x;
-                else C[(int64_t)row * ldc + col] = to_bf16(x);
+                for (int v = 0; v < 16; ++v) {
+                    const int row = i0 + wm * 64 + a * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+                    const float x = RAGGED ? acc[a][b][v] * factor : acc[a][b][v];
+                    if (!whole.value && (row >= out.rows || col >= out.cols)) continue;
+                    if constexpr (sizeof(OUT) == 4) C[(int64_t)row * ldc + col] = x;
+                    else C[(int64_t)row * ldc + col] = to_bf16(x);
+                }
             }
-        }
+    };
+    if constexpr (RAGGED) {
+        if (i0 + kLinTM > out.rows || j0 + TN > out.cols) return store(std::false_type());
+    }
+    store(std::true_type());
 }
 
 // bf16 [X][64] operand tile (rows along the contraction index, 128 bytes each) filled by direct global -> LDS loads:

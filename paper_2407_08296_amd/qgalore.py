@@ -149,7 +149,7 @@ def lib() -> C.CDLL:
                                                 vp, sz, vp]
         L.qg_int8_linear_act_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp]
         L.qg_int8_linear_act_workspace_bytes.restype = sz
-        L.qg_int8_linear_act_workspace_bytes.argtypes = [i64, i64]
+        L.qg_int8_linear_act_workspace_bytes.argtypes = [i64, i64, i64]
         L.qg_int8_linear_act_backward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, sz, vp]
         L.qg_int8_gated_forward.argtypes = [vp] * 5 + [i32, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp]
         L.qg_int8_gated_workspace_bytes.restype = sz
@@ -588,7 +588,7 @@ def int8_linear_act_backward(dy: torch.Tensor, z: torch.Tensor | None, x: torch.
     ws = None
     nbytes = 0
     if want_dbias or kind:
-        nbytes = lib().qg_int8_linear_act_workspace_bytes(tokens, m)
+        nbytes = lib().qg_int8_linear_act_workspace_bytes(tokens, m, n)
         ws = dy.new_empty(nbytes, dtype=torch.uint8)
     _check(lib().qg_int8_linear_act_backward(_ptr(dy, _BF16), _ptr(z, _BF16), _ptr(x, _BF16), *w, kind, tokens, m, n, n, m, GROUP,
                                              _ptr(dx), _ptr(G), _ptr(dbias), _ptr(ws), nbytes, _stream()))

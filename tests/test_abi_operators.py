@@ -63,8 +63,8 @@ def test_int8_linear_act(L):
     assert call(a11=128) == 3
     for i in (0, 1, 2, 3, 4, 12, 13):
         assert call(**{f"a{i}": FAKE + 2}) == 4
-    nbytes = L.qg_int8_linear_act_workspace_bytes(16, 512)
-    assert nbytes >= 512 * 4 and L.qg_int8_linear_act_workspace_bytes(0, 512) == 0 and L.qg_int8_linear_act_workspace_bytes(1 << 20, 1 << 20) == 0
+    nbytes = L.qg_int8_linear_act_workspace_bytes(16, 512, 256)
+    assert nbytes >= 512 * 4 and L.qg_int8_linear_act_workspace_bytes(0, 512, 256) == 0 and L.qg_int8_linear_act_workspace_bytes(1 << 20, 1 << 20, 8) == 0
     # dy, z, x, Wq, Ws, act, tokens, m, n, ld_n, ld_m, group, dx, G, dbias, ws, bytes, stream
     call = caller(L.qg_int8_linear_act_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 3, 16, 512, 256, 0, 0, 256, FAKE, FAKE, FAKE, FAKE, nbytes, None)
     for i in (0, 1, 2, 3, 4):

@@ -1,0 +1,51 @@
+"""The operators together: the feed-forward language model of the example, one step against automatic differentiation in fp64 and a
+short training run."""
+import math
+
+import pytest
+import torch
+
+from oracle import qgalore as Q
+from paper_2407_08296_amd import example_ffn_lm as E
+
+pytestmark = pytest.mark.gpu
+
+
+def test_gradients_of_the_whole_model():
+    """Every tensor that passes between two operators is bf16 (one rounding of 2^-9 on average per element and operator): gradients
+    agree with fp64 to a few times that per operator that they went through, about a dozen here."""
+    model = E.Model(layers=2, seed=3)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for p in model.w_pre + model.w_post + model.gates:
+        p += 0.2 * torch.randn(p.shape, device="cuda", generator=gen)
+    tokens, labels = E.chain(gen, 500, torch.randint(0, E.VOCAB, (E.VOCAB, 8), device="cuda", generator=gen))
+    loss, grads = model.loss_and_gradients(tokens, labels)
+    dense = [p.double().requires_grad_() for p in model.dense]
+    n = len(model.blocks)
+    embed, head, w_pre, w_post, gates = dense[0], dense[1], dense[2:3 + n], dense[3 + n:3 + 2 * n], dense[3 + 2 * n:]
+    W = [[torch.from_numpy(Q.dequant_w_bf16(w.Wq.cpu().numpy(), w.Ws.cpu().numpy())).cuda().requires_grad_() for w in b]
+         for b in model.blocks]
+    rms = lambda v: v / torch.sqrt((v * v).mean(1, keepdim=True) + E.EPS)
+    h = embed[tokens]
+    for i, (wg, wu, wd) in enumerate(W):
+        u = w_pre[i] * rms(h)
+        y = (torch.nn.functional.silu(u @ wg.t()) * (u @ wu.t())) @ wd.t()
+        h = h + E.SCALE * gates[i] * w_post[i] * rms(y)
+    logp = ((w_pre[n] * rms(h)) @ head.t()).log_softmax(1)
+    on = labels >= 0
+    want = -logp[on, labels[on]].mean()
+    want.backward()
+    assert abs(float(loss) - float(want)) <= 1e-3 * float(want)
+    close = lambda a, b: float((a.double() - b).norm()) <= 12 * 2.0 ** -8 * float(b.norm())
+    for got, ref in zip(model.dense, dense):
+        assert close(got.grad, ref.grad), (tuple(got.shape), float((got.grad.double() - ref.grad).norm() / ref.grad.norm()))
+    for gs, ws in zip(grads, W):
+        for G, w in zip(gs, ws):
+            assert close(G, w.grad), float((G.double() - w.grad).norm() / w.grad.norm())
+
+
+def test_training_lowers_the_loss_and_repeats_itself():
+    losses = E.train(60, seed=1)
+    assert all(math.isfinite(v) for v in losses) and abs(losses[0] - math.log(E.VOCAB)) < 0.5
+    assert sum(losses[-5:]) / 5 < losses[0] - 1.0
+    assert E.train(12, seed=1) == losses[:12]          # sums in a fixed order everywhere: the same bits again

@@ -175,7 +175,7 @@ def test_row_pitch_in_place_and_padding():
     assert close(y, want, ld_m) and close(z, wz, ld_m)
     dx, G, db = qg.int8_linear_act_backward(dy, wz, x, *wg, act="gelu", want_dbias=True)
     dyp, zp, dxp, Gp, dbp = pad(dy, ld_m), pad(wz, ld_m), pad(x, ld_n), pad(G, ld_n), torch.empty(m, device=DEV)
-    nbytes = L.qg_int8_linear_act_workspace_bytes(tokens, m)
+    nbytes = L.qg_int8_linear_act_workspace_bytes(tokens, m, n)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
     assert L.qg_int8_linear_act_backward(at(dyp), at(zp), at(xp), at(wgp), at(wg[1]), 3, tokens, m, n, ld_n, ld_m, 256, at(dxp), at(Gp),
                                          at(dbp), at(ws), nbytes, st) == 0
