@@ -299,6 +299,8 @@ static int check_head(int64_t tokens, int64_t h, int64_t vocab, int64_t& ld) {
     if (ld != h && (ld < h || (ld & 15) || ld >= 65536 + 16)) return QG_ERR_SHAPE;
     return QG_OK;
 }
+// (labels and the numbers per token are read one by one: a shifted view of a longer array will do)
+static bool aligned_to(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 static int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Tiles of a product of M x N elements: 256 x 256 with a workgroup per CU at least, 128 x 128, or 64 x 64 where those would leave
@@ -423,9 +425,9 @@ extern "C" int qg_head_loss_forward(const uint16_t* x_bf16, const uint16_t* W_bf
                                     void* stream) {
     if (!x_bf16 || !W_bf16 || !labels || !loss || !lse) return QG_ERR_NULL;
     if (int e = check_head(tokens, h, vocab, ld)) return e;
-    for (const void* p : {(const void*)x_bf16, (const void*)W_bf16, (const void*)labels, (const void*)loss, (const void*)lse,
-                          (const void*)workspace})
-        if (!aligned16(p)) return QG_ERR_ALIGN;
+    if (!aligned16(x_bf16) || !aligned16(W_bf16) || !aligned16(workspace) || !aligned_to(labels, 8) || !aligned_to(loss, 4) ||
+        !aligned_to(lse, 4))
+        return QG_ERR_ALIGN;
     const HeadSpace s = head_space(tokens, h, vocab, false);
     if (!workspace || workspace_bytes < s.total) return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
@@ -464,9 +466,9 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
                                      uint16_t* dW_bf16, void* workspace, size_t workspace_bytes, void* stream) {
     if (!x_bf16 || !W_bf16 || !labels || !lse || !dloss || (!dx_bf16 && !dW_bf16)) return QG_ERR_NULL;
     if (int e = check_head(tokens, h, vocab, ld)) return e;
-    for (const void* p : {(const void*)x_bf16, (const void*)W_bf16, (const void*)labels, (const void*)lse, (const void*)dloss,
-                          (const void*)dx_bf16, (const void*)dW_bf16, (const void*)workspace})
-        if (!aligned16(p)) return QG_ERR_ALIGN;
+    if (!aligned16(x_bf16) || !aligned16(W_bf16) || !aligned16(dx_bf16) || !aligned16(dW_bf16) || !aligned16(workspace) ||
+        !aligned_to(labels, 8) || !aligned_to(lse, 4) || !aligned_to(dloss, 4))
+        return QG_ERR_ALIGN;
     const HeadSpace s = head_space(tokens, h, vocab, true);
     if (!workspace || workspace_bytes < s.total) return QG_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;

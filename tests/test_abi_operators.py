@@ -110,8 +110,10 @@ def test_head_loss(L):
     for i in (0, 1, 2, 7, 8):
         assert call(**{f"a{i}": None}) == 1
     assert call(a3=0) == 2 and call(a4=0) == 2 and call(a5=0) == 2 and call(a6=63) == 2 and call(a6=72) == 2
-    for i in (0, 1, 2, 7, 8, 9):
+    for i in (0, 1, 9):
         assert call(**{f"a{i}": FAKE + 8}) == 4
+    assert call(a2=FAKE + 4) == 4 and call(a7=FAKE + 2) == 4 and call(a8=FAKE + 1) == 4
+    assert call(a2=FAKE + 8, a7=FAKE + 4, a8=FAKE + 4, a10=64) == 5      # labels by 8, numbers by 4: on to the next check
     assert call(a9=None) == 5 and call(a10=64) == 5
     # x, W, labels, lse, dloss, tokens, h, vocab, ld, dx, dW, ws, bytes, stream
     call = caller(L.qg_head_loss_backward, FAKE, FAKE, FAKE, FAKE, FAKE, 16, 64, 1000, 0, FAKE, FAKE, FAKE, nbytes, None)
@@ -119,6 +121,8 @@ def test_head_loss(L):
         assert call(**{f"a{i}": None}) == 1
     assert call(a9=None, a10=None) == 1
     assert call(a5=-4) == 2 and call(a8=65) == 2
-    for i in (0, 1, 2, 3, 4, 9, 10, 11):
+    for i in (0, 1, 2, 9, 10, 11):
         assert call(**{f"a{i}": FAKE + 4}) == 4
+    assert call(a3=FAKE + 2) == 4 and call(a4=FAKE + 2) == 4
+    assert call(a2=FAKE + 8, a3=FAKE + 4, a4=FAKE + 12, a12=64) == 5
     assert call(a11=None) == 5 and call(a12=64) == 5

@@ -35,7 +35,7 @@ def test_gradients_of_the_whole_model():
     on = labels >= 0
     want = -logp[on, labels[on]].mean()
     want.backward()
-    assert abs(float(loss) - float(want)) <= 1e-3 * float(want)
+    assert abs(float(loss) - want.item()) <= 1e-3 * want.item()
     close = lambda a, b: float((a.double() - b).norm()) <= 12 * 2.0 ** -8 * float(b.norm())
     for got, ref in zip(model.dense, dense):
         assert close(got.grad, ref.grad), (tuple(got.shape), float((got.grad.double() - ref.grad).norm() / ref.grad.norm()))

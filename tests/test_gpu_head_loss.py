@@ -191,6 +191,47 @@ def test_row_pitch():
         assert torch.equal(p[:, :h], t) and torch.isnan(p[:, h:].float()).all()
 
 
+def test_views_shifted_by_a_token():
+    """labels of a sequence are its tokens one further on; numbers per token may start anywhere too."""
+    x, W, labels, dloss = inputs(71, 64, 300, seed=11)
+    labels, dloss = labels.clamp(0, 299), dloss
+    want = qg.head_loss_forward(x[:70], W, labels[1:].clone())
+    got = qg.head_loss_forward(x[:70], W, labels[1:])
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    lse = torch.cat([got[1][:1], got[1]])[1:]
+    a = qg.head_loss_backward(x[:70], W, labels[1:], lse, dloss[1:])
+    b = qg.head_loss_backward(x[:70], W, labels[1:].clone(), got[1], dloss[1:].clone())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_a_head_of_more_than_2_to_the_31_elements():
+    tokens, h, vocab = 9, 8192, 262150
+    g = torch.Generator(device=DEV).manual_seed(12)
+    x = torch.randn(tokens, h, device=DEV, generator=g).bfloat16()
+    W = torch.empty(vocab, h, dtype=torch.bfloat16, device=DEV)
+    for v in range(0, vocab, 65536):
+        W[v:v + 65536] = torch.randn(min(65536, vocab - v), h, device=DEV, generator=g) * 0.02
+    labels = torch.tensor([0, vocab - 1, -1, 262143, 262144, 5, vocab, 131072, vocab - 2], device=DEV)
+    loss, lse = qg.head_loss_forward(x, W, labels)
+    dloss = torch.linspace(0.5, 2, tokens, device=DEV)
+    dx, dW = qg.head_loss_backward(x, W, labels, lse, dloss)
+    z = torch.cat([x.double() @ W[v:v + 32768].double().t().contiguous() for v in range(0, vocab, 32768)], 1)
+    on = (labels >= 0) & (labels < vocab)
+    wlse = torch.logsumexp(z, 1)
+    at = torch.where(on, labels, 0)[:, None]
+    want = torch.where(on, wlse - z.gather(1, at)[:, 0], 0)
+    bar = 4 * h * U24 * float((x.double().norm(dim=1).max() * W[:1000].double().norm(dim=1).max())) + 64 * U24 * 20
+    assert float((loss.double() - want).abs().max()) <= 2 * bar
+    dl = (z - wlse[:, None]).exp_()
+    dl.scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
+    dl *= torch.where(on, dloss, 0).double()[:, None]
+    want_dx = sum(dl[:, v:v + 32768].contiguous() @ W[v:v + 32768].double() for v in range(0, vocab, 32768))
+    assert float((dx.double() - want_dx).norm() / want_dx.norm()) <= 2.0 ** -7
+    for rows in (slice(0, 300), slice(131000, 131200), slice(262000, vocab)):     # before and behind 2^31 elements
+        ref = dl[:, rows].t().contiguous() @ x.double()
+        assert float((dW[rows].double() - ref).norm() / ref.norm()) <= 2.0 ** -7
+
+
 def test_refusals():
     x, W, labels, dloss = inputs(8, 16, 32, seed=9)
     lse = torch.zeros(8, device=DEV)

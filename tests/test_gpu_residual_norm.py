@@ -193,6 +193,23 @@ def test_gradient_against_differences_of_the_forward_kernel():
         assert abs(diff - want) <= noise + 1e-5 * float((grad.double() * e.double()).abs().sum())
 
 
+def test_rows_past_2_to_the_31_elements():
+    tokens, d = 540000, 4096
+    s = {k: torch.zeros(tokens, d, dtype=torch.bfloat16, device=DEV) for k in ("h", "y", "du")}
+    at = [0, 1, 524287, 524288, 524289, tokens - 1]
+    small = inputs(len(at), d, False, "channel", seed=9)
+    for k in s:
+        s[k][at] = small[k]
+    want = qg.residual_norm_forward(small["h"], small["y"], small["w_post"], small["gate"], small["w_pre"], scale=0.7, eps=EPS)
+    got = qg.residual_norm_forward(s["h"], s["y"], small["w_post"], small["gate"], small["w_pre"], scale=0.7, eps=EPS)
+    assert torch.equal(got[0][at], want[0]) and torch.equal(got[1][at], want[1])
+    want = qg.residual_norm_backward(small["du"], None, small["h"], small["y"], small["w_post"], small["gate"], small["w_pre"], eps=EPS)
+    got = qg.residual_norm_backward(s["du"], None, s["h"], s["y"], small["w_post"], small["gate"], small["w_pre"], eps=EPS)
+    assert torch.equal(got[0][at], want[0]) and torch.equal(got[1][at], want[1])
+    for a, b in zip(got[2:], want[2:]):          # sums over rows of which all others are zero, in another order
+        assert torch.allclose(a, b, rtol=1e-5, atol=1e-9)
+
+
 def test_refusals():
     s = inputs(4, 64, False, "channel")
     with pytest.raises(qg.QGError):
