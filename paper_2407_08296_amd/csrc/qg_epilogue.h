@@ -170,14 +170,14 @@ struct GatedRun {
 };
 
 // ---- kernels ----
-enum : int { kDimM = 0, kDimN = 1, kDimK = 2 };
+enum : int { kDimM = 0, kDimN = 1 };
 template <typename OPB, typename EPI>
 struct EpiProduct {
     LinOperand A, A2;
     OPB B, B2;
     EPI epi;
     int M, N, K, tiles_m, tiles_n;
-    // An extent that only the device knows: *count elements along `dim`, at most what M, N or K says, and a multiple of `unit` (at
+    // An extent that only the device knows: *count rows or columns, at most M or N, and a multiple of `unit` (at
     // least 64: a whole number of steps; tiles are taken to be whole if unit is so many of them).  The grid is the largest one's;
     // the rest ends at once.
     const int32_t* count = nullptr;
@@ -195,8 +195,7 @@ __global__ __launch_bounds__(WM * 128 * KG, KG > 1 ? (MB == 1 ? 4 : 2) : WM == 2
         if (p.count != nullptr) {
             const int n = *p.count;
             if (p.dim == kDimM) p.tiles_m = ((p.M = n) + 32 * MB * WM - 1) / (32 * MB * WM);
-            else if (p.dim == kDimN) p.tiles_n = ((p.N = n) + TN - 1) / TN;
-            else p.K = n;
+            else p.tiles_n = ((p.N = n) + TN - 1) / TN;
             grid = (uint32_t)(p.tiles_m * p.tiles_n + 7) / 8 * 8;      // the XCDs share what there is
             if (blockIdx.x >= grid) return;
         }
@@ -229,12 +228,12 @@ __global__ __launch_bounds__(WM * 128 * KG, KG > 1 ? (MB == 1 ? 4 : 2) : WM == 2
                                                                   smem);
 }
 
-template <int AL, int BL, bool EXACT, int KW, int TERMS, typename OPB, typename EPI>
+template <int AL, int BL, bool EXACT, int KW, typename OPB, typename EPI>
 __global__ __launch_bounds__(64 * KW) void k_ksplit_epilogue(EpiProduct<OPB, EPI> p) {
     __shared__ __attribute__((aligned(16))) uint16_t smem[KSplit<AL, BL, KW, EPI::kPair ? 2 : 1>::SMEM];
     const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x);
     if (tile >= (uint32_t)(p.tiles_m * p.tiles_n)) return;
-    ksplit_epi<AL, BL, EXACT, KW, TERMS>(p.A, p.B, p.A2, p.B2, p.epi, p.M, p.N, p.K, p.tiles_m, p.tiles_n, tile, smem);
+    ksplit_epi<AL, BL, EXACT, KW>(p.A, p.B, p.epi, p.M, p.N, p.K, p.tiles_m, p.tiles_n, tile, smem);
 }
 
 // A part of a split contraction, in fp32: sum[split][row][col], rows `ld` (a multiple of 8) apart.
@@ -301,14 +300,14 @@ static int launch_epilogue_shape(EpiProduct<OPB, EPI> p, hipStream_t st) {
 }
 
 // 32 x 32 output elements per workgroup, the contraction over KW waves (see KSplit).
-template <int AL, int BL, int KW, int TERMS, typename OPB, typename EPI>
+template <int AL, int BL, int KW, typename OPB, typename EPI>
 static int launch_epilogue_ksplit(EpiProduct<OPB, EPI> p, hipStream_t st) {
     p.tiles_m = (p.M + 31) / 32;
     p.tiles_n = (p.N + 31) / 32;
     const unsigned grid = (unsigned)((p.tiles_m * p.tiles_n + 7) / 8 * 8);
     const bool exact = p.M % 32 == 0 && p.N % 32 == 0 && p.K % 64 == 0 && p.A.ld % 8 == 0 && p.B.ld % 16 == 0;
-    if (exact) hipLaunchKernelGGL((k_ksplit_epilogue<AL, BL, true, KW, TERMS, OPB, EPI>), dim3(grid), dim3(64 * KW), 0, st, p);
-    else hipLaunchKernelGGL((k_ksplit_epilogue<AL, BL, false, KW, TERMS, OPB, EPI>), dim3(grid), dim3(64 * KW), 0, st, p);
+    if (exact) hipLaunchKernelGGL((k_ksplit_epilogue<AL, BL, true, KW, OPB, EPI>), dim3(grid), dim3(64 * KW), 0, st, p);
+    else hipLaunchKernelGGL((k_ksplit_epilogue<AL, BL, false, KW, OPB, EPI>), dim3(grid), dim3(64 * KW), 0, st, p);
     return check_launch();
 }
 

@@ -20,6 +20,8 @@ namespace qg {
 constexpr float kLog2e = 1.44269504f;
 
 // ---- forward ----
+// 4096 tokens, 4096 x 32000: 930 us (1155 TFLOP/s, the matrix pipe busy 54 % of the time at 2.0 GHz); 256 tokens, 768 x 32000: 20.5 us,
+// of which W's bytes take 10; one token, 4096 x 32000: 51 us (5.1 TB/s).
 // Rows of the product are vocabulary entries, columns tokens.  A lane has 16 entries of each block of its column's token, the lane 32
 // further the other 16.
 struct StatsEpilogue {
@@ -75,7 +77,7 @@ struct StatsEpilogue {
     }
 };
 
-// 16 tokens per workgroup, 64 slices of the slots: maxima first, then the sums below the token's maximum, in a fixed order.
+// 16 tokens per workgroup, 64 slices of the slots: maxima first, then the sums below the token's maximum, in a fixed order.  4 to 6.5 us.
 __global__ __launch_bounds__(1024) void k_head_join(const f32x2* __restrict__ part, int slots, int64_t stride,
                                                     const int64_t* __restrict__ labels, int64_t vocab,
                                                     const int32_t* __restrict__ rows, const float* __restrict__ label_logit,
@@ -131,7 +133,8 @@ __global__ __launch_bounds__(1024) void k_head_join(const f32x2* __restrict__ pa
 // ---- the tokens that have a loss ----
 // Of each such token: its row of x, its number, its label in 32 bits and (backward) its lse and dloss; then rows of zeros up to a
 // multiple of `unit`.  The others' loss and lse, or row of dx, become zero here.  A workgroup counts the labels for itself
-// (they are few bytes and stay in the cache): one launch, and an order that does not depend on timing.
+// (they are few bytes and stay in the cache): one launch, and an order that does not depend on timing.  5 us and up: 1000 tokens of 2048
+// 8 to 10, 4096 of 4096 27 (a copy of that size 14).
 struct HeadRows {
     const uint16_t* x;
     const int64_t* labels;
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(256) void k_head_rows(HeadRows a) {
     }
 }
 
-// dl of the entries from v0 on
+// dl of the entries from v0 on.  4096 tokens, 4096 x 16128: 484 us (1118 TFLOP/s).
 struct DLogitsRun {
     static constexpr bool kPair = false, kCounted = true;
     const int32_t* label32;
@@ -255,7 +258,8 @@ struct DLogitsRun {
     }
 };
 
-// dx over the pieces and the parts of a split contraction: in fp32 up to the last one, which rounds.
+// dx over the pieces and the parts of a split contraction: in fp32 up to the last one, which rounds.  4096 tokens, 16128 x 4096: 462 us
+// (1171 TFLOP/s); 512 tokens with a loss, 32003 x 2048 in eight parts 92 us and 9 for their sum, in 64 x 64 tiles that take all of it 224.
 struct AddRun {
     static constexpr bool kPair = false, kCounted = true;
     float* sum;              // [splits][padded tokens][ld_sum]
@@ -398,7 +402,8 @@ static int launch_head_rows(HeadRows a, hipStream_t st) {
     return check_launch();
 }
 
-// dW's rows of a piece, dl^T x: direct loads of whole tiles.  dl's rows are a multiple of 128 elements apart, x's of 256, so that a
+// dW's rows of a piece, dl^T x: direct loads of whole tiles (4096 tokens, 16128 x 4096: 488 us, 1109 TFLOP/s; 512, 32003 x 2048: 87 to 95,
+// through registers 113).  dl's rows are a multiple of 128 elements apart, x's of 256, so that a
 // tile never leaves its row; what stands between their ends and that only reaches elements that are not stored.
 static int launch_head_dw(const uint16_t* dl, int64_t pitch, const uint16_t* x, int64_t hp, uint16_t* dW, int64_t ldc, int64_t width,
                           int64_t h, int64_t padded, const int32_t* count, const float* scale, hipStream_t st) {

@@ -11,26 +11,6 @@
 // W in the forward pass, of dy only in grad_input, of neither in grad_W.
 #include "qg_tile_gemm.h"
 
-namespace qg {
-
-static int check_linear(int64_t tokens, int64_t m, int64_t n, int group) {
-    const int64_t lim = int64_t(1) << 31;
-    if (tokens <= 0 || m <= 0 || n <= 0 || tokens >= lim / m || tokens >= lim / n || m >= lim / n) return QG_ERR_SHAPE;
-    if (group != kGroup) return QG_ERR_GROUP;
-    return QG_OK;
-}
-
-// Row pitches of the pitched entry points: ld_n for the arrays with n elements per row (x, dx, Wq, G), ld_m for those
-// with m (y, dy).  Each is the row length itself, or at least it and a multiple of 16 elements.
-static int check_pitch(int64_t rows_limit, int64_t len, int64_t& ld) {
-    if (ld == 0) ld = len;
-    if (ld != len && (ld < len || (ld & 15))) return QG_ERR_SHAPE;
-    if (rows_limit >= (int64_t(1) << 31) / ld) return QG_ERR_SHAPE;
-    return QG_OK;
-}
-
-}  // namespace qg
-
 using namespace qg;
 
 extern "C" int qg_int8_linear_forward_ld(const uint16_t* x_bf16, const int8_t* Wq, const float* Ws,

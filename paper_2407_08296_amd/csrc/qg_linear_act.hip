@@ -11,18 +11,6 @@
 
 namespace qg {
 
-static int check_sizes(int64_t tokens, int64_t m, int64_t n, int group) {
-    const int64_t lim = int64_t(1) << 31;
-    if (tokens <= 0 || m <= 0 || n <= 0 || tokens >= lim / m || tokens >= lim / n || m >= lim / n) return QG_ERR_SHAPE;
-    if (group != kGroup) return QG_ERR_GROUP;
-    return QG_OK;
-}
-static int check_pitch(int64_t rows, int64_t len, int64_t& ld) {
-    if (ld == 0) ld = len;
-    if (ld != len && (ld < len || (ld & 15))) return QG_ERR_SHAPE;
-    if (rows >= (int64_t(1) << 31) / ld) return QG_ERR_SHAPE;
-    return QG_OK;
-}
 static bool all_aligned(std::initializer_list<const void*> ps) {
     for (const void* p : ps)
         if (!aligned16(p)) return false;
@@ -32,8 +20,8 @@ static bool all_aligned(std::initializer_list<const void*> ps) {
 // ---- dz: 8 columns of a row per thread, LANES threads per row.  Bound by HBM (6 bytes per element, a pair 10).  dbias: the columns'
 // sums over a slab from registers, a wave's rows by lane swaps, the four waves added in order, slabs added by k_column_sums.
 // LANES = 64: 512 columns and every 4th row of a slab per wave.  LANES = 2: 16 columns and all rows, so that dbias takes no
-// second kernel and short batches reach all CUs: up to 512 tokens (256 x 2048, gelu and dbias, us: 8.9 with two kernels, 8.5 with 64
-// columns per workgroup).
+// second kernel and short batches reach all CUs: up to 512 tokens (256 x 2048, gelu and dbias, us: 7.1, 8.9 with two kernels, 8.5 with
+// 64 columns per workgroup).  A pair of 4096 x 11008: 83 us (5.4 TB/s), of 1000 x 5461 (unaligned rows) 15 (3.6 TB/s).
 template <bool PAIR, int LANES>
 __global__ __launch_bounds__(LANES == 2 ? 512 : 256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
                                                       const uint16_t* __restrict__ zu, uint16_t* __restrict__ dzg,
@@ -155,7 +143,7 @@ static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
     constexpr int AL = kBf16KFast, BL = kInt8KFast;
     if (lin_ksplit<AL, BL>(p.M, p.N, p.K, 0)) {
         const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32);
-        return t32 <= 256 ? launch_epilogue_ksplit<AL, BL, 8, 1>(p, st) : launch_epilogue_ksplit<AL, BL, 4, 1>(p, st);
+        return t32 <= 256 ? launch_epilogue_ksplit<AL, BL, 8>(p, st) : launch_epilogue_ksplit<AL, BL, 4>(p, st);
     }
     auto tiles = [&](int tm, int tn) { return (int64_t)((p.M + tm - 1) / tm) * ((p.N + tn - 1) / tn); };
     const bool small = lin_small<AL, BL>(p.M, p.N, 1);
@@ -174,18 +162,23 @@ static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
     return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
-// ... of a pair: N columns of each.
+// ... of a pair: N columns of each, the tile's columns shared between the two so that x is staged once for both.  4096 tokens, 4096 ->
+// 2 x 11008: 727 us (1016 TFLOP/s; without zg and zu 9 % less: their stores come at the end of a tile, when the CU's matrix pipe is
+// idle); 256 tokens 80 us; one token 26.6 us (3.4 TB/s of codes; a kernel that loads them straight into matrix operands, without LDS,
+// took 25.9 to 30).
 template <typename EPI>
 static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t st) {
     const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32);
-    if (t32 <= 256) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 8, 1>(p, st);
-    if (t32 <= 768) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 4, 1>(p, st);
-    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128) >= 256) return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
+    if (t32 <= 256) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 8>(p, st);
+    if (t32 <= 768) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 4>(p, st);
+    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128) >= 256)
+        return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
     return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
-// dx = dzg Wg + dzu Wu, tokens x n.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split over workgroups, parts of
-// 512 at least, in fp32 through the workspace.
+// dx = dzg Wg + dzu Wu, tokens x n, one accumulator for both.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split
+// over workgroups, parts of 512 at least, in fp32 through the workspace.  1000 tokens, 2 x 5461 -> 2048, us: 68 and 7 for the sum of
+// four parts, 110 in 64 x 64 tiles that take the whole contraction; 4096 tokens, 2 x 11008 -> 4096 700 (1055 TFLOP/s).
 static int64_t gated_dx_chunk(int64_t tokens, int64_t m, int64_t n) {
     const int64_t t128 = ((tokens + 127) / 128) * ((n + 127) / 128), room = 512 / t128, most = m / 512, splits = room < most ? room : most;
     return splits <= 1 ? m : ((m + splits - 1) / splits + 63) / 64 * 64;
@@ -225,8 +218,9 @@ __global__ __launch_bounds__(256) void k_align_rows(const uint16_t* __restrict__
 }
 
 // G = dz^T x for one or two dz of rows `ldz` apart (a multiple of 8).  Direct loads where there are tiles of 128 x 256 for every CU; they
-// want rows that start on 16 bytes, and x is copied to such where it has others (600 tokens, 2997 and 2 x 6869: the products without
-// direct loads 165 us).
+// want rows that start on 16 bytes, and x is copied to such where it has others (600 tokens, 2997 and 2 x 6869, us: 97 and 5 for the
+// copy; without direct loads 130).  1000 tokens, 2 x 5461 x 2048: both in one launch 54 us, in two of other tiles 91; 4096 tokens, 2 x 11008
+// x 4096 683 (1080 TFLOP/s).
 static bool grad_w_direct(int64_t m, int64_t n, int count) { return ((m + kLinTM - 1) / kLinTM) * ((n + 255) / 256) * count >= 256; }
 static size_t grad_w_copy_bytes(int64_t tokens, int64_t m, int64_t n, int count) {   // of x, whatever its pitch turns out to be
     return grad_w_direct(m, n, count) && n % 8 != 0 ? (size_t)tokens * ((n + 7) / 8 * 8) * 2 : 0;
@@ -243,9 +237,10 @@ static int launch_act_grad_w(const uint16_t* dz, const uint16_t* dz2, int64_t ld
             x = copy;
         }
         const int64_t tiles_m = (m + kLinTM - 1) / kLinTM, tiles_n = (n + 255) / 256;
+        const dim3 grid((unsigned)((tiles_m * tiles_n + 7) / 8 * 8), (unsigned)count);
         const KSlowOut out = {(int)m, (int)n, ld_n, nullptr, dz2, G2, nullptr};
-        hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8), (unsigned)count), dim3(256),
-                           0, st, dz, x, G, (int)ldz, (int)ldx, (int)tokens, (int)tiles_m, (int)tiles_n, out);
+        hipLaunchKernelGGL((k_gemm_kslow_direct<uint16_t, true>), grid, dim3(256), 0, st, dz, x, G, (int)ldz, (int)ldx, (int)tokens, (int)tiles_m,
+                           (int)tiles_n, out);
         return check_launch();
     }
     const LinOperand xo = {x, nullptr, ld_n, 0};
@@ -268,7 +263,7 @@ extern "C" int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* 
                                           int64_t ld_m, int group, uint16_t* z_bf16, uint16_t* y_bf16, void* stream) {
     if (!x_bf16 || !Wq || !Ws || !y_bf16) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
-    if (int e = check_sizes(tokens, m, n, group)) return e;
+    if (int e = check_linear(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
     if (!all_aligned({x_bf16, Wq, Ws, bias_bf16, residual_bf16, z_bf16, y_bf16})) return QG_ERR_ALIGN;
@@ -281,7 +276,7 @@ extern "C" int qg_int8_linear_act_forward(const uint16_t* x_bf16, const int8_t* 
 }
 
 extern "C" size_t qg_int8_linear_act_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
-    if (check_sizes(tokens, m, n, kGroup)) return 0;
+    if (check_linear(tokens, m, n, kGroup)) return 0;
     return whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + whole_lines_of((size_t)act_slabs(tokens, m).count * (size_t)m * 4) +
            grad_w_copy_bytes(tokens, m, n, 1);
 }
@@ -294,7 +289,7 @@ extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16
     if ((dx_bf16 && (!Wq || !Ws)) || (G_bf16 && !x_bf16)) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
     if (act != QG_ACT_NONE && !z_bf16) return QG_ERR_NULL;
-    if (int e = check_sizes(tokens, m, n, group)) return e;
+    if (int e = check_linear(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
     if (!all_aligned({dy_bf16, z_bf16, x_bf16, Wq, Ws, dx_bf16, G_bf16, dbias, workspace})) return QG_ERR_ALIGN;
@@ -324,7 +319,7 @@ extern "C" int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, 
                                      uint16_t* zg_bf16, uint16_t* zu_bf16, uint16_t* y_bf16, void* stream) {
     if (!x_bf16 || !Wgq || !Wgs || !Wuq || !Wus || !y_bf16 || (!zg_bf16 != !zu_bf16)) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
-    if (int e = check_sizes(tokens, m, n, group)) return e;
+    if (int e = check_linear(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
     if (!all_aligned({x_bf16, Wgq, Wgs, Wuq, Wus, zg_bf16, zu_bf16, y_bf16})) return QG_ERR_ALIGN;
@@ -340,7 +335,7 @@ extern "C" int qg_int8_gated_forward(const uint16_t* x_bf16, const int8_t* Wgq, 
 }
 
 extern "C" size_t qg_int8_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
-    if (check_sizes(tokens, m, n, kGroup)) return 0;
+    if (check_linear(tokens, m, n, kGroup)) return 0;
     const int64_t chunk = gated_dx_chunk(tokens, m, n), splits = chunk < m ? (m + chunk - 1) / chunk : 0;
     return 2 * whole_lines_of((size_t)tokens * dz_pitch(m) * 2) + whole_lines_of((size_t)splits * tokens * ((n + 7) / 8 * 8) * 4) +
            grad_w_copy_bytes(tokens, m, n, 2);
@@ -353,7 +348,7 @@ extern "C" int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* z
     if (!dy_bf16 || !zg_bf16 || !zu_bf16 || (!Gg_bf16 != !Gu_bf16) || (!dx_bf16 && !Gg_bf16)) return QG_ERR_NULL;
     if ((dx_bf16 && (!Wgq || !Wgs || !Wuq || !Wus)) || (Gg_bf16 && !x_bf16)) return QG_ERR_NULL;
     if (act < QG_ACT_NONE || act > QG_ACT_GELU) return QG_ERR_SHAPE;
-    if (int e = check_sizes(tokens, m, n, group)) return e;
+    if (int e = check_linear(tokens, m, n, group)) return e;
     if (int e = check_pitch(tokens > m ? tokens : m, n, ld_n)) return e;
     if (int e = check_pitch(tokens, m, ld_m)) return e;
     if (!all_aligned({dy_bf16, zg_bf16, zu_bf16, x_bf16, Wgq, Wgs, Wuq, Wus, dx_bf16, Gg_bf16, Gu_bf16, workspace})) return QG_ERR_ALIGN;

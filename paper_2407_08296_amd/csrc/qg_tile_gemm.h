@@ -509,9 +509,9 @@ struct KSplit {
     static constexpr int SMEM = KW * WAVE;
 };
 
-template <int AL, int BL, bool EXACT, int KW, int TERMS, typename OPB, typename EPI>
-__device__ __forceinline__ void ksplit_epi(const LinOperand& A1, const OPB& B1, const LinOperand& A2, const OPB& B2, const EPI& epi, int M,
-                                           int N, int K, int tiles_m, int tiles_n, uint32_t tile, uint16_t* smem) {
+template <int AL, int BL, bool EXACT, int KW, typename OPB, typename EPI>
+__device__ __forceinline__ void ksplit_epi(const LinOperand& A, const OPB& B, const EPI& epi, int M, int N, int K, int tiles_m, int tiles_n,
+                                           uint32_t tile, uint16_t* smem) {
     constexpr int NB = EPI::kPair ? 2 : 1;
     using T = KSplit<AL, BL, KW, NB>;
     using SA = typename T::SA;
@@ -556,7 +556,6 @@ __device__ __forceinline__ void ksplit_epi(const LinOperand& A1, const OPB& B1, 
 #pragma unroll
             for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[kk], bf[b][kk], acc[b], 0, 0, 0);
     };
-    auto contraction = [&](const LinOperand& A, const OPB& B) {
     // this wave's steps first, first + KW, ... (`count` of them), fetched two ahead under FETCH's terms
     auto run = [&](auto fetch_mode, int first, int count) {
         constexpr int FETCH = decltype(fetch_mode)::value;
@@ -585,9 +584,6 @@ __device__ __forceinline__ void ksplit_epi(const LinOperand& A1, const OPB& B1, 
     } else {
         run(Guarded(), wave, steps_below(total));
     }
-    };
-    contraction(A1, B1);
-    if constexpr (TERMS == 2) contraction(A2, B2);
     float* tp = reinterpret_cast<float*>(At);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -617,7 +613,7 @@ template <int AL, int BL, bool EXACT, int KW>
 __device__ __forceinline__ void ksplit_gemm(const LinOperand& A, const LinOperand& B, const uint16_t* __restrict__ bias,
                                             uint16_t* __restrict__ C, int64_t ldc, int M, int N, int K, int tiles_m, int tiles_n,
                                             uint32_t tile, uint16_t* smem) {
-    ksplit_epi<AL, BL, EXACT, KW, 1>(A, B, A, B, PlainEpilogue<uint16_t>{bias, C, ldc}, M, N, K, tiles_m, tiles_n, tile, smem);
+    ksplit_epi<AL, BL, EXACT, KW>(A, B, PlainEpilogue<uint16_t>{bias, C, ldc}, M, N, K, tiles_m, tiles_n, tile, smem);
 }
 
 template <int BL, bool EXACT, int KW>
@@ -696,8 +692,9 @@ __global__ __launch_bounds__(256, 3) void k_gemm_kslow_direct(const uint16_t* __
     const uint32_t b_byte[2] = {BD::lane_src_bytes(lane, N, 0), BD::lane_src_bytes(lane, N, 1)};
     auto gload = [&](int kt, int stage) {
         const int64_t rows = K - (int64_t)kt * BK;
-        const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + (int64_t)kt * BK * M + i0, RAGGED ? bound_bytes(2 * ((rows - 1) * M + ((out.rows + 7) & ~7) - i0)) : 0x7FFFFFFF);
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + (int64_t)kt * BK * N + j0, RAGGED ? bound_bytes(2 * ((rows - 1) * N + ((out.cols + 7) & ~7) - j0)) : 0x7FFFFFFF);
+        auto bound = [&](int ld, int x, int x0) { return RAGGED ? bound_bytes(2 * ((rows - 1) * ld + ((x + 7) & ~7) - x0)) : 0x7FFFFFFF; };
+        const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + (int64_t)kt * BK * M + i0, bound(M, out.rows, i0));
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + (int64_t)kt * BK * N + j0, bound(N, out.cols, j0));
 #pragma unroll
         for (int p = 0; p < AD::PER; ++p)
             buffer_load_lds16(ra, As[stage] + AD::load_row0(wave, p) * kLinTM, a_byte, 2u * (uint32_t)(AD::load_row0(wave, p) * M));
@@ -920,6 +917,21 @@ static void launch_tile_gemm_shape(const LinOperand& A, const LinOperand& B, con
     else
         hipLaunchKernelGGL((k_tile_gemm<AL, BL, false, OUT, MB, TN, BK, WM, DEEP_RAGGED, KG>), grid, dim3(128 * WM * KG), 0, st, A, B, bias,
                            C, (int)M, (int)N, (int)K, (int)tiles_m, (int)tiles_n, batch);
+}
+
+// Sizes of the linear layer, and the row pitches of its arrays: ld_n for those with n elements per row (x, dx, Wq, G), ld_m for those
+// with m (y, dy).  Each is the row length itself, or at least it and a multiple of 16 elements.
+static inline int check_linear(int64_t tokens, int64_t m, int64_t n, int group) {
+    const int64_t lim = int64_t(1) << 31;
+    if (tokens <= 0 || m <= 0 || n <= 0 || tokens >= lim / m || tokens >= lim / n || m >= lim / n) return QG_ERR_SHAPE;
+    if (group != kGroup) return QG_ERR_GROUP;
+    return QG_OK;
+}
+static inline int check_pitch(int64_t rows_limit, int64_t len, int64_t& ld) {
+    if (ld == 0) ld = len;
+    if (ld != len && (ld < len || (ld & 15))) return QG_ERR_SHAPE;
+    if (rows_limit >= (int64_t(1) << 31) / ld) return QG_ERR_SHAPE;
+    return QG_OK;
 }
 
 // Whether a product runs 64 x 64 tiles (see launch_tile_gemm).
