@@ -411,7 +411,7 @@ int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, con
  *   dz = dloss (exp(z - lse) - onehot), rounded to bf16;  dx = dz W, dW = dz^T x, either may be NULL.  The vocabulary is
  *   taken in pieces: the logits of a piece are computed again, and only tokens x piece numbers are stored.
  * ld: row pitch of x, W, dx and dW: h (or 0), or more and a multiple of 16.  tokens and vocab below 2^24, h below 2^16,
- * tokens * vocab below 2^38, tokens * h below 2^34.  workspace: qg_head_loss_workspace_bytes(tokens, h, vocab) bytes, 16-byte
+ * tokens * vocab below 2^38, tokens * h below 2^34, vocab * h below 2^37.  workspace: qg_head_loss_workspace_bytes(tokens, h, vocab) bytes, 16-byte
  * aligned, enough for either call.  labels need 8-byte alignment only, loss, lse and dloss 4-byte (views shifted by a token). */
 size_t qg_head_loss_workspace_bytes(int64_t tokens, int64_t h, int64_t vocab);
 int qg_head_loss_forward(const uint16_t* x_bf16, const uint16_t* W_bf16, const int64_t* labels, int64_t tokens, int64_t h,

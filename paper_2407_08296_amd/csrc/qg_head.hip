@@ -298,7 +298,8 @@ struct AddRun {
 static int check_head(int64_t tokens, int64_t h, int64_t vocab, int64_t& ld) {
     constexpr int64_t most = int64_t(1) << 24;
     if (tokens <= 0 || h <= 0 || vocab <= 0 || tokens >= most || vocab >= most || h >= 65536) return QG_ERR_SHAPE;
-    if (tokens * vocab >= (int64_t(1) << 38) || tokens * h >= (int64_t(1) << 34)) return QG_ERR_SHAPE;   // threads of one launch
+    // threads of one launch: tiles of dz, rows of x, tiles of dW
+    if (tokens * vocab >= (int64_t(1) << 38) || tokens * h >= (int64_t(1) << 34) || vocab * h >= (int64_t(1) << 37)) return QG_ERR_SHAPE;
     if (ld == 0) ld = h;
     if (ld != h && (ld < h || (ld & 15) || ld >= 65536 + 16)) return QG_ERR_SHAPE;
     return QG_OK;

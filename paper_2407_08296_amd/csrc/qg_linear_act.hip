@@ -116,13 +116,13 @@ static Slabs act_slabs(int64_t tokens, int64_t m) {
     rows = (rows + 3) / 4 * 4;
     return {(int)rows, (int)((tokens + rows - 1) / rows)};
 }
-constexpr int64_t kActOneSlab = 512;      // tokens up to which dbias is made in one kernel
+constexpr int64_t kActOneSlab = 512, kActOneSlabCols = 65536;   // tokens (and columns) up to which dbias is made in one kernel
 
 // part: one row of sums per slab, or dbias itself where there is one slab
 template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
                                float* dbias, int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
-    if (dbias != nullptr && tokens <= kActOneSlab) {
+    if (dbias != nullptr && tokens <= kActOneSlab && m <= kActOneSlabCols) {
         hipLaunchKernelGGL((k_act_backward<PAIR, 2>), dim3((unsigned)((m + 15) / 16)), dim3(512), 0, st, dy, zg, zu, dzg, dzu, dbias,
                            (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
         return check_launch();

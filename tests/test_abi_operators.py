@@ -101,7 +101,7 @@ def test_head_loss(L):
     nbytes = L.qg_head_loss_workspace_bytes(16, 64, 1000)
     assert nbytes >= 16 * 64 * 2 + 16 * 1000 * 2
     for bad in ((0, 64, 1000), (16, 0, 1000), (16, 64, -1), (1 << 24, 64, 1000), (16, 65536, 1000), (16, 64, 1 << 24), (1 << 20, 64, 1 << 18),
-                (1 << 23, 2048, 1000)):
+                (1 << 23, 2048, 1000), (16, 8192, 1 << 24), (16, 65535, 1 << 22)):
         assert L.qg_head_loss_workspace_bytes(*bad) == 0
     # a long batch over a wide vocabulary: far below its logits in 16 bits
     assert L.qg_head_loss_workspace_bytes(65536, 4096, 128000) < 65536 * 128000 * 2 // 8
