@@ -166,14 +166,28 @@ static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
 // 2 x 11008: 727 us (1016 TFLOP/s; without zg and zu 9 % less: their stores come at the end of a tile, when the CU's matrix pipe is
 // idle); 256 tokens 80 us; one token 26.6 us (3.4 TB/s of codes; a kernel that loads them straight into matrix operands, without LDS,
 // took 25.9 to 30).
+// Tiles, us, by what the rule takes / the next one (T32: blocks of 32 x 32 columns of each; T64, T128: tiles of 64 or 128 tokens by 64):
+//  * the contraction over waves up to T32 = 512: 64 tokens, 4096 -> 8192 (512) 26.8 / 28.5, 64 tokens, 1024 -> 5461 (342) 8.7 / 10.3, but
+//    150 tokens, 2047 -> 4095 (640) 38.5 / 24.0, 64 tokens, 4096 -> 11008 (688) 40 / 30.
+//  * 64 tokens in two groups of waves up to T64 = 256: 128 tokens, 4096 -> 8192 (256) 30.7, 128 tokens a tile 42.7 to 47; one
+//    group below K = 1024: 500 tokens, 768 -> 2048 11.5 / 12.2, at 1024 (300 tokens, 2736 columns) 12.3 / 12.2, at 1536 16.4 / 14.2.
+//  * 128 tokens in two groups up to T128 = 256: 500 tokens, 2048 -> 4096 (256) 28.0, one group 29.6, 150 tokens, 4096 -> 8192 49.4 / 52.5;
+//    one group below K = 768: 500 tokens, 512 -> 4096 12.8 / 12.5.
+//  * 64 tokens, one group, up to T64 = 512: 700 tokens, 2048 -> 2736 (473) 31.1, 128 tokens a tile 40.0; 700 tokens, 1024 -> 2736 18.4 / 24.2;
+//    not beyond: 256 tokens, 4096 -> 11008 (688) 91 / 75, 1000 tokens, 2048 -> 5461 (1376) 87 / 68.
+//  * 256 tokens from a workgroup per CU on, as for one weight.
 template <typename EPI>
 static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t st) {
-    const int64_t t32 = (int64_t)((p.M + 31) / 32) * ((p.N + 31) / 32);
-    if (t32 <= 256) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 8>(p, st);
-    if (t32 <= 768) return launch_epilogue_ksplit<kBf16KFast, kInt8KFast, 4>(p, st);
-    if (p.M >= 1024 && (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128) >= 256)
-        return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 256, 64, 4, true, true, 1, 1>(p, st);
-    return launch_epilogue_shape<kBf16KFast, kInt8KFast, 2, 128, 64, 2, true, true, 1, 1>(p, st);
+    constexpr int AL = kBf16KFast, BL = kInt8KFast;
+    auto tiles = [&](int tm, int tn) { return (int64_t)((p.M + tm - 1) / tm) * ((p.N + tn - 1) / tn); };
+    const int64_t t32 = tiles(32, 32), t64 = tiles(64, 64), t128 = tiles(128, 64);
+    if (t32 <= 256) return launch_epilogue_ksplit<AL, BL, 8>(p, st);
+    if (t32 <= 512) return launch_epilogue_ksplit<AL, BL, 4>(p, st);
+    if (t64 <= 256 && p.K >= 1024) return launch_epilogue_shape<AL, BL, 1, 128, 64, 2, true, true, 2, 1>(p, st);
+    if (t64 > 256 && t128 <= 256 && p.K >= 768) return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 2, 1>(p, st);
+    if (t64 <= 256 || (t128 > 256 && t64 <= 512)) return launch_epilogue_shape<AL, BL, 1, 128, 64, 2, true, true, 1, 1>(p, st);
+    if (p.M >= 1024 && tiles(256, 128) >= 256) return launch_epilogue_shape<AL, BL, 2, 256, 64, 4, true, true, 1, 1>(p, st);
+    return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
 // dx = dzg Wg + dzu Wu, tokens x n, one accumulator for both.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split

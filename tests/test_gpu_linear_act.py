@@ -85,8 +85,13 @@ def test_act_backward(tokens, m, n, act):
     assert torch.equal(qg.int8_linear_act_backward(dy, zz, x, *w, act=act, want_dx=False, want_G=False, want_dbias=True)[2], db)
 
 
+# (tokens, m, n) of the gated pair's tiles, whole and ragged: 64 tokens in two groups of waves and in one, 128 in two groups and in one
+GATED = [(256, 2048, 1024), (250, 2050, 1025), (512, 2048, 512), (500, 2040, 600), (512, 4096, 768), (500, 4100, 800), (512, 4096, 448),
+         (700, 2736, 320), (690, 2731, 300), (1000, 5461, 128)]
+
+
 @pytest.mark.parametrize("act", ["none", "silu", "gelu"])
-@pytest.mark.parametrize("tokens,m,n", CASES)
+@pytest.mark.parametrize("tokens,m,n", CASES + GATED)
 def test_gated_forward(tokens, m, n, act):
     g = torch.Generator().manual_seed(tokens + m + n + 2)
     (wg, Wg), (wu, Wu) = weight(g, m, n), weight(g, m, n)

@@ -73,3 +73,14 @@ def test_dbias_of_short_batches_takes_no_second_kernel(driver, tokens, kernels):
     assert len(driver("act_backward", tokens, 768, 256)) in (kernels, kernels + 1)
     first = driver("act_backward", tokens, 768, 256)[0]
     assert first == ((48, 1, 512) if tokens == 512 else (2, up(513, 4), 256))
+
+
+@pytest.mark.parametrize("tokens,m,n,want", [
+    (1, 8192, 4096, (256, 512)), (64, 8192, 4096, (512, 256)),                       # contraction over eight waves, over four
+    (150, 4095, 2047, (192, 512)), (500, 2048, 768, (256, 256)),                     # tiles of 64 tokens in two groups, in one
+    (500, 4096, 2048, (256, 512)), (500, 4096, 512, (256, 256)),                     # of 128 tokens in two groups, in one
+    (700, 2736, 2048, (480, 256)), (1000, 5461, 2048, (688, 256)),                   # 473 tiles of 64 tokens; 688 of 128
+    (4096, 11008, 4096, (1376, 512)),                                                # 256 tokens, eight waves
+])
+def test_tiles_of_the_gated_pair(driver, tokens, m, n, want):
+    assert driver("gated_forward", tokens, m, n) == [(want[0], 1, want[1])]
