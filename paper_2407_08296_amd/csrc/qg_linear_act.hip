@@ -20,8 +20,8 @@ static bool all_aligned(std::initializer_list<const void*> ps) {
 // ---- dz: 8 columns of a row per thread, LANES threads per row.  Bound by HBM (6 bytes per element, a pair 10).  dbias: the columns'
 // sums over a slab from registers, a wave's rows by lane swaps, the four waves added in order, slabs added by k_column_sums.
 // LANES = 64: 512 columns and every 4th row of a slab per wave.  LANES = 2: 16 columns and all rows, so that dbias takes no
-// second kernel and short batches reach all CUs: up to 512 tokens (256 x 2048, gelu and dbias, us: 7.1, 8.9 with two kernels, 8.5 with
-// 64 columns per workgroup).  A pair of 4096 x 11008: 83 us (5.4 TB/s), of 1000 x 5461 (unaligned rows) 15 (3.6 TB/s).
+// second kernel and short batches reach all CUs (256 x 2048, gelu and dbias, us: 7.1, 8.9 with two kernels, 8.5 with 64 columns
+// per workgroup).  A pair of 4096 x 11008: 83 us (5.4 TB/s), of 1000 x 5461 (unaligned rows) 15 (3.6 TB/s).
 template <bool PAIR, int LANES>
 __global__ __launch_bounds__(LANES == 2 ? 512 : 256) void k_act_backward(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ zg,
                                                       const uint16_t* __restrict__ zu, uint16_t* __restrict__ dzg,
@@ -116,13 +116,17 @@ static Slabs act_slabs(int64_t tokens, int64_t m) {
     rows = (rows + 3) / 4 * 4;
     return {(int)rows, (int)((tokens + rows - 1) / rows)};
 }
-constexpr int64_t kActOneSlab = 512, kActOneSlabCols = 65536;   // tokens (and columns) up to which dbias is made in one kernel
+// dbias in one kernel: up to 2048 tokens (a workgroup takes all of them) and 2^21 elements (beyond, 16 columns of a row per workgroup
+// read worse than the second kernel costs).  The whole backward pass, us, one / two kernels: 32 x 768 columns 17.0 / 19.3, 1024 x 256
+// 16.7 / 19.4, 768 x 2048 30.1 / 32.2, 1024 x 2048 32.7 / 34.2, 2048 x 1024 39.6 / 40.2; but 4096 x 64 35.3 / 34.2, 512 x 8192
+// 84 / 81, 1024 x 4096 51.9 / 48.8, 1024 x 8192 147 / 133.
+static bool act_one_slab(int64_t tokens, int64_t m) { return tokens <= 2048 && tokens * m <= (int64_t(1) << 21); }
 
 // part: one row of sums per slab, or dbias itself where there is one slab
 template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
                                float* dbias, int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
-    if (dbias != nullptr && tokens <= kActOneSlab && m <= kActOneSlabCols) {
+    if (dbias != nullptr && act_one_slab(tokens, m)) {
         hipLaunchKernelGGL((k_act_backward<PAIR, 2>), dim3((unsigned)((m + 15) / 16)), dim3(512), 0, st, dy, zg, zu, dzg, dzu, dbias,
                            (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
         return check_launch();
@@ -192,7 +196,8 @@ static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t s
 
 // dx = dzg Wg + dzu Wu, tokens x n, one accumulator for both.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split
 // over workgroups, parts of 512 at least, in fp32 through the workspace.  1000 tokens, 2 x 5461 -> 2048, us: 68 and 7 for the sum of
-// four parts, 110 in 64 x 64 tiles that take the whole contraction; 4096 tokens, 2 x 11008 -> 4096 700 (1055 TFLOP/s).
+// four parts, 110 in 64 x 64 tiles that take the whole contraction (the pass: 149, 155 and 161 with parts for one and for four workgroups per CU; 256
+// tokens, 2 x 11008 -> 4096 170, 172, 180; 1400 tokens, 2 x 5461 -> 2048 200, 210, 197); 4096 tokens, 2 x 11008 -> 4096 700 (1055 TFLOP/s).
 static int64_t gated_dx_chunk(int64_t tokens, int64_t m, int64_t n) {
     const int64_t t128 = ((tokens + 127) / 128) * ((n + 127) / 128), room = 512 / t128, most = m / 512, splits = room < most ? room : most;
     return splits <= 1 ? m : ((m + splits - 1) / splits + 63) / 64 * 64;

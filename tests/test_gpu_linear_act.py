@@ -22,6 +22,9 @@ CASES = [(1, 1, 1), (3, 5, 7), (1, 2050, 768), (16, 70, 1300), (15, 33, 1024), (
          (33, 64, 130), (130, 333, 264), (77, 200, 521), (64, 519, 256), (200, 2112, 65),
          (500, 1100, 600), (2100, 600, 200), (1200, 5000, 72), (4096, 4096, 64), (4100, 4111, 72)]
 
+# dbias in one kernel, up to its largest batch and product of tokens and columns, and just past them
+SLABS = [(2048, 1024, 40), (2048, 33, 70), (2049, 33, 70), (700, 2990, 48), (700, 3001, 48)]
+
 
 def f64(t):
     return None if t is None else t.double().cpu().numpy()
@@ -65,7 +68,7 @@ def test_act_forward(tokens, m, n, act):
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
-@pytest.mark.parametrize("tokens,m,n", CASES)
+@pytest.mark.parametrize("tokens,m,n", CASES + SLABS)
 def test_act_backward(tokens, m, n, act):
     g = torch.Generator().manual_seed(tokens + m + n + 1)
     w, W = weight(g, m, n)

@@ -68,11 +68,11 @@ def test_two_weight_gradients_in_one_launch(driver):
     assert len(driver("gated_backward", 64, 2736, 1024)) == 5                       # few tiles: each in a launch of its own
 
 
-@pytest.mark.parametrize("tokens,kernels", [(512, 2), (513, 3)])
+@pytest.mark.parametrize("tokens,kernels", [(512, 2), (2048, 2), (2049, 3)])
 def test_dbias_of_short_batches_takes_no_second_kernel(driver, tokens, kernels):
     assert len(driver("act_backward", tokens, 768, 256)) in (kernels, kernels + 1)
     first = driver("act_backward", tokens, 768, 256)[0]
-    assert first == ((48, 1, 512) if tokens == 512 else (2, up(513, 4), 256))
+    assert first == ((48, 1, 512) if tokens <= 2048 else (2, (2049 + 7) // 8, 256))
 
 
 @pytest.mark.parametrize("tokens,m,n,want", [
