@@ -171,6 +171,12 @@ struct GatedRun {
 
 // ---- kernels ----
 enum : int { kDimM = 0, kDimN = 1 };
+// Contraction of a part where the number of tiles is known to the device only: about two workgroups per CU for `live` tiles of a
+// contraction of k, parts of `least` (a multiple of 64) and more.
+__device__ __forceinline__ int live_chunk(int least, int k, int live) {
+    const int splits = max(512 / live, 1);
+    return max(least, ((k + splits - 1) / splits + 63) / 64 * 64);
+}
 template <typename OPB, typename EPI>
 struct EpiProduct {
     LinOperand A, A2;
@@ -185,6 +191,7 @@ struct EpiProduct {
     // The contraction over `splits` workgroups per tile (blockIdx.y): `k_chunk` of it each (a multiple of 64), epi.split(s) for the
     // s-th one.
     int splits = 1, k_chunk = 0;
+    int live_k = 0;      // > 0: the parts are live_chunk(k_chunk, live_k, tiles there are), the workgroups of further ones end at once
 };
 
 template <int AL, int BL, bool EXACT, int MB, int TN, int BK, int WM, bool DEEP, int KG, int TERMS, typename OPB, typename EPI>
@@ -200,7 +207,9 @@ __global__ __launch_bounds__(WM * 128 * KG, KG > 1 ? (MB == 1 ? 4 : 2) : WM == 2
             if (blockIdx.x >= grid) return;
         }
         if (p.splits > 1) {
+            if (p.live_k > 0) p.k_chunk = live_chunk(p.k_chunk, p.live_k, p.tiles_m * p.tiles_n);
             const int k0 = (int)blockIdx.y * p.k_chunk;
+            if (k0 >= p.K) return;
             auto at = [&](LinOperand& op, auto layout) {
                 constexpr int L = decltype(layout)::value;
                 static_assert(L == kBf16KFast || L == kBf16KSlow || L == kInt8KSlow, "others: not needed so far");
@@ -252,13 +261,21 @@ struct PartRun {
 };
 
 // The parts added in order (times *scale), rounded once: out[row][col], or out[to[row]][col] where `to` is given and not negative.
-// rows: *count of them where that is given.
+// rows: *count of them where that is given.  live.k > 0: as many parts as live_chunk made of that many rows.
+struct LiveParts {
+    int k = 0, chunk = 0, side = 0, across = 0;      // side: of a tile; across: tiles per row of tiles
+};
 static __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ sum, int64_t ld, int64_t stride, int splits,
-                                                           const int32_t* __restrict__ to, const int32_t* __restrict__ count,
+                                                           LiveParts live, const int32_t* __restrict__ to, const int32_t* __restrict__ count,
                                                            const float* __restrict__ scale, int rows, int cols,
                                                            uint16_t* __restrict__ out, int64_t ld_out) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = (cols + 7) / 8, row = i / chunks;
-    if (row >= (count != nullptr ? *count : rows)) return;
+    const int there = count != nullptr ? *count : rows;
+    if (row >= there) return;
+    if (live.k > 0) {
+        const int chunk = live_chunk(live.chunk, live.k, (there + live.side - 1) / live.side * live.across);
+        splits = (live.k + chunk - 1) / chunk;
+    }
     const int at = to != nullptr ? to[row] : (int)row, col = (int)(i - row * chunks) * 8;
     if (at < 0) return;
     f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
@@ -272,9 +289,9 @@ static __global__ __launch_bounds__(256) void k_join_parts(const float* __restri
     const float v[8] = {f * a[0], f * a[1], f * a[2], f * a[3], f * b[0], f * b[1], f * b[2], f * b[3]};
     store_run(out + (int64_t)at * ld_out + col, cols - col, v);
 }
-static int launch_join_parts(const float* sum, int64_t ld, int64_t stride, int splits, const int32_t* to, const int32_t* count,
+static int launch_join_parts(const float* sum, int64_t ld, int64_t stride, int splits, LiveParts live, const int32_t* to, const int32_t* count,
                              const float* scale, int64_t rows, int64_t cols, uint16_t* out, int64_t ld_out, hipStream_t st) {
-    hipLaunchKernelGGL(k_join_parts, dim3((unsigned)((rows * ((cols + 7) / 8) + 255) / 256)), dim3(256), 0, st, sum, ld, stride, splits, to,
+    hipLaunchKernelGGL(k_join_parts, dim3((unsigned)((rows * ((cols + 7) / 8) + 255) / 256)), dim3(256), 0, st, sum, ld, stride, splits, live, to,
                        count, scale, (int)rows, (int)cols, out, ld_out);
     return check_launch();
 }

@@ -259,7 +259,8 @@ struct DLogitsRun {
 };
 
 // dx over the pieces and the parts of a split contraction: in fp32 up to the last one, which rounds.  4096 tokens, 16128 x 4096: 462 us
-// (1171 TFLOP/s); 512 tokens with a loss, 32003 x 2048 in eight parts 92 us and 9 for their sum, in 64 x 64 tiles that take all of it 224.
+// (1171 TFLOP/s); 512 tokens with a loss, 32003 x 2048 in eight parts 92 us and 9 for their sum, in 64 x 64 tiles that take
+// all of it 224.
 struct AddRun {
     static constexpr bool kPair = false, kCounted = true;
     float* sum;              // [splits][padded tokens][ld_sum]
@@ -332,9 +333,12 @@ static int64_t head_slots(int64_t tokens, int64_t vocab) {
 }
 
 // dx has tokens x h elements and a contraction as long as the vocabulary: where its tiles would leave CUs idle, the contraction of a
-// piece is split over workgroups, 1024 of it each at least, up to two workgroups of 128 x 128 (or 64 x 64) tiles per CU.  Backward
-// pass, us, up to two / up to four: 500 tokens, 32003 x 2048 284 / 294, 700, 32000 x 1024 222 / 244, 1000, 32000 x 768 216 / 237,
-// 100, 32000 x 4096 282 / 289, 2048, 50304 x 768 645 / 669; 1500, 32000 x 2048 690 / 679; up to eight: 500, 32003 x 2048 320.
+// piece is split over workgroups, 1024 of it each at least, up to two workgroups of 128 x 128 (or 64 x 64) tiles per CU.  The device
+// knows how many tokens have a loss, and so how many tiles there are: the grid and the workspace have room for twice the parts that
+// all tokens would get, and live_chunk decides.  Backward pass, us, parts for two / for four workgroups per CU: 500 tokens, 32003 x
+// 2048 268 / 282 (eight: 320), 700, 32000 x 1024 214 / 232, 1000, 32000 x 768 216 / 237, 100, 32000 x 4096 271 / 277, 2048, 50304 x
+// 768 620 / 640; but 1500, 32000 x 2048 690 / 679.  1000 tokens of which half have a loss, 32003 x 2048: two workgroups per CU for the
+// tiles that there are 279, for those of all tokens 310.
 static int head_dx_tile(int64_t tokens, int64_t h) {
     const int tile = head_tile(tokens, h);
     return tile == kTile64 && tokens > 64 && h > 64 ? kTile128 : tile;
@@ -343,7 +347,7 @@ static int64_t head_chunk(int64_t tokens, int64_t h, int64_t piece) {
     const int tile = head_dx_tile(tokens, h);
     if (tile == kTile256) return piece;
     const int64_t side = tile == kTile64 ? 64 : 128, tiles = ((tokens + side - 1) / side) * ((h + side - 1) / side);
-    const int64_t room = 512 / tiles, most = piece / 1024, splits = room < most ? room : most;
+    const int64_t room = 1024 / tiles, most = piece / 1024, splits = room < most ? room : most;
     return splits <= 1 ? piece : up((piece + splits - 1) / splits, 64);
 }
 
@@ -359,7 +363,7 @@ static int64_t head_piece(int64_t tokens, int64_t vocab) {
 }
 
 struct HeadSpace {     // a call's workspace, in bytes
-    int64_t piece, chunk, splits, hp, unit, padded, slots;     // chunk: contraction of dx per workgroup
+    int64_t piece, chunk, splits, hp, unit, padded, slots;     // chunk: least contraction of dx per workgroup; splits: most parts
     size_t count, scale, rows, labels, lse, dloss, x, sum, dl, part, logit, total;
 };
 static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab, bool backward) {
@@ -499,6 +503,10 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
     uint16_t* dl = reinterpret_cast<uint16_t*>(at + s.dl);
     float* sum = reinterpret_cast<float*>(at + s.sum);
     const int64_t stride = s.padded * s.hp;
+    LiveParts live;
+    live.k = (int)s.piece, live.chunk = (int)s.chunk;
+    live.side = head_dx_tile(s.padded, h) == kTile64 ? 64 : 128;
+    live.across = (int)((h + live.side - 1) / live.side);
     for (int64_t v0 = 0; v0 < vocab; v0 += s.piece) {
         const int64_t width = vocab - v0 < s.piece ? vocab - v0 : s.piece, pitch = up(width, kLinTM);
         const LinOperand x = {r.xc, nullptr, s.hp, 0}, W = {W_bf16 + v0 * ld, nullptr, ld, 0}, d = {dl, nullptr, pitch, 0};
@@ -523,6 +531,7 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
             p.dim = kDimM;
             p.unit = (int)s.unit;
             p.k_chunk = (int)s.chunk;
+            p.live_k = live.k;
             p.splits = (int)((width + s.chunk - 1) / s.chunk);
             if (int e = launch_head<kBf16KFast, kBf16KSlow>(p, head_dx_tile(s.padded, h), st)) return e;
         }
@@ -530,6 +539,6 @@ extern "C" int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_b
             if (int e = launch_head_dw(dl, pitch, r.xc, s.hp, dW_bf16 + v0 * ld, ld, width, h, s.padded, r.count, r.scale, st)) return e;
     }
     if (dx_bf16 && s.splits > 1)
-        return launch_join_parts(sum, s.hp, stride, (int)s.splits, r.rows, r.count, r.scale, s.padded, h, dx_bf16, ld, st);
+        return launch_join_parts(sum, s.hp, stride, (int)s.splits, live, r.rows, r.count, r.scale, s.padded, h, dx_bf16, ld, st);
     return QG_OK;
 }

@@ -214,7 +214,7 @@ static int launch_gated_dx(const LinOperand& dzg, const LinOperand& dzu, const L
         p.k_chunk = (int)chunk;
         p.splits = (int)((m + chunk - 1) / chunk);
         if (int e = launch_epilogue_shape<kBf16KFast, kInt8KSlow, 2, 128, 64, 2, true, true, 1, 2>(p, st)) return e;
-        return launch_join_parts(parts, ldp, tokens * ldp, p.splits, nullptr, nullptr, nullptr, tokens, n, dx, ld, st);
+        return launch_join_parts(parts, ldp, tokens * ldp, p.splits, {}, nullptr, nullptr, nullptr, tokens, n, dx, ld, st);
     }
     EpiProduct<LinOperand, PlainEpilogue<uint16_t>> p;
     p.A = dzg, p.A2 = dzu, p.B = Wg, p.B2 = Wu;

@@ -18,6 +18,8 @@ U24 = 2.0 ** -24
 # (tokens, h, vocab): one of everything, odd everything, around the tiles (64, 128, 256), several pieces (a long batch, a wide vocabulary)
 CASES = [(1, 1, 1), (1, 8, 2), (3, 7, 5), (1, 768, 4001), (33, 65, 130), (64, 64, 64), (65, 72, 257), (130, 521, 1000), (256, 128, 8192),
          (300, 40, 20001), (2100, 64, 4100), (1100, 24, 16640), (40000, 16, 2600), (33000, 24, 1025), (20000, 24, 4100)]
+# more tiles of dx than a quarter of the CUs: the parts of its contraction depend on how many tokens have a loss
+PARTS = [(1000, 1100, 12300), (300, 4100, 10000), (1500, 1024, 9001)]
 
 
 def f64(t):
@@ -54,7 +56,7 @@ def test_forward(tokens, h, vocab):
     assert not loss[~learned].any() and not lse[~learned].any()
 
 
-@pytest.mark.parametrize("tokens,h,vocab", CASES)
+@pytest.mark.parametrize("tokens,h,vocab", CASES + PARTS)
 def test_backward(tokens, h, vocab):
     x, W, labels, dloss = inputs(tokens, h, vocab, seed=1)
     _, lse = qg.head_loss_forward(x, W, labels)
