@@ -177,8 +177,8 @@ static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
 //    group below K = 1024: 500 tokens, 768 -> 2048 11.5 / 12.2, at 1024 (300 tokens, 2736 columns) 12.3 / 12.2, at 1536 16.4 / 14.2.
 //  * 128 tokens in two groups up to T128 = 256: 500 tokens, 2048 -> 4096 (256) 28.0, one group 29.6, 150 tokens, 4096 -> 8192 49.4 / 52.5;
 //    one group below K = 768: 500 tokens, 512 -> 4096 12.8 / 12.5.
-//  * 64 tokens, one group, up to T64 = 512: 700 tokens, 2048 -> 2736 (473) 31.1, 128 tokens a tile 40.0; 700 tokens, 1024 -> 2736 18.4 / 24.2;
-//    not beyond: 256 tokens, 4096 -> 11008 (688) 91 / 75, 1000 tokens, 2048 -> 5461 (1376) 87 / 68.
+//  * 64 tokens, one group, up to T64 = 512: 700 tokens, 2048 -> 2736 (473) 31.1, 128 tokens a tile 40.0; 700 tokens, 1024 -> 2736
+//    18.4 / 24.2; not beyond: 256 tokens, 4096 -> 11008 (688) 91 / 75, 1000 tokens, 2048 -> 5461 (1376) 87 / 68.
 //  * 256 tokens from a workgroup per CU on, as for one weight.
 template <typename EPI>
 static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t st) {
@@ -196,8 +196,9 @@ static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t s
 
 // dx = dzg Wg + dzu Wu, tokens x n, one accumulator for both.  Fewer than 512 tiles of 128 x 128 (two per CU): both contractions split
 // over workgroups, parts of 512 at least, in fp32 through the workspace.  1000 tokens, 2 x 5461 -> 2048, us: 68 and 7 for the sum of
-// four parts, 110 in 64 x 64 tiles that take the whole contraction (the pass: 149, 155 and 161 with parts for one and for four workgroups per CU; 256
-// tokens, 2 x 11008 -> 4096 170, 172, 180; 1400 tokens, 2 x 5461 -> 2048 200, 210, 197); 4096 tokens, 2 x 11008 -> 4096 700 (1055 TFLOP/s).
+// four parts, 110 in 64 x 64 tiles that take the whole contraction (the pass: 149, 155 and 161 with parts for one and for four
+// workgroups per CU; 256 tokens, 2 x 11008 -> 4096 170, 172, 180; 1400 tokens, 2 x 5461 -> 2048 200, 210, 197); 4096 tokens, 2 x 11008
+// -> 4096 700 (1055 TFLOP/s).
 static int64_t gated_dx_chunk(int64_t tokens, int64_t m, int64_t n) {
     const int64_t t128 = ((tokens + 127) / 128) * ((n + 127) / 128), room = 512 / t128, most = m / 512, splits = room < most ? room : most;
     return splits <= 1 ? m : ((m + splits - 1) / splits + 63) / 64 * 64;
