@@ -333,9 +333,13 @@ __global__ __launch_bounds__(64 * WPR * ROWS, 4) void k_residual_norm_bwd(
             w.y[q].again();
             if constexpr (TOKEN_GATE) w.g[q].again();
         }
-        const float r = has_u ? 1.f / sqrtf(s[0] * rd + a.eps) : 0.f, qi = post ? 1.f / sqrtf(s[2] * rd + a.eps) : 1.f;
-        const float c1 = r * r * s[1] * rd;                                             // dh = dh' + r (a - c1 h')
-        const float c2 = post ? qi * qi * rd * (s[3] + r * (s[4] - c1 * s[5])) : 0.f;   // dy = q (k dh - c2 y)
+        // (past the end: r = q = 0, so that zeros add nothing with eps = 0 either; r and q are multiplied into the sums one by one, since
+        // the square of one overflows where eps is tiny and the row zero)
+        const bool row_is = t < a.tokens;
+        const float r = has_u && row_is ? 1.f / sqrtf(s[0] * rd + a.eps) : 0.f;
+        const float qi = !post ? 1.f : row_is ? 1.f / sqrtf(s[2] * rd + a.eps) : 0.f;
+        const float c1 = r * (r * s[1]) * rd;                                             // dh = dh' + r (a - c1 h')
+        const float c2 = post ? qi * (qi * (s[3] + r * (s[4] - c1 * s[5]))) * rd : 0.f;   // dy = q (k dh - c2 y)
 #pragma unroll
         for (int q = 0; q < CH; ++q) {
             const int c = 8 * (tid + NT * q), valid = t < a.tokens ? a.d - c : 0;

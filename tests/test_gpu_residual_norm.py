@@ -251,3 +251,37 @@ def test_another_stream_and_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("gate", [None, "channel", "token"])
+@pytest.mark.parametrize("tokens,d", [(3, 96), (5, 768), (9, 2047), (7, 4096), (1, 33), (300, 700), (1030, 2000)])
+def test_backward_without_eps_where_the_last_workgroup_has_rows_to_spare(tokens, d, gate, fp32):
+    """eps = 0 and no row of zeros: every rms is positive, but that of the rows past the last token, which must add nothing."""
+    s = inputs(tokens, d, fp32, gate, seed=11)
+    got = qg.residual_norm_backward(s["du"], s["dh"], s["h"], s["y"], s["w_post"], s["gate"], s["w_pre"], scale=0.7, eps=0.0)
+    f = {k: f64(v) for k, v in s.items()}
+    want = O.residual_norm_backward(f["du"], f["dh"], f["h"], f["y"], f["w_post"], f["gate"], f["w_pre"], 0.7, 0.0)
+    mh, my, q = sums_noise(f, d)      # (its eps of 1e-6 beside a mean square of 1 and more changes these magnitudes by 1e-6)
+    check(got[0], want[0], mh)
+    check(got[1], want[1], my)
+    check_sum(got[2], f["du"] * f["h"] / np.sqrt(np.mean(f["h"] ** 2, axis=1, keepdims=True)))
+    gv = 1.0 if f["gate"] is None else f["gate"]
+    assert np.all(np.abs(f64(got[3]) - want[3]) <= 8 * (1 + np.sqrt(tokens)) * U24 * np.sum(0.7 * np.abs(gv * f["y"]) * q * mh, axis=0))
+    if gate == "channel":
+        assert np.all(np.abs(f64(got[4]) - want[4]) <= 8 * (1 + np.sqrt(tokens)) * U24 * np.sum(0.7 * np.abs(f["w_post"] * f["y"]) * q * mh, axis=0))
+    elif gate == "token":
+        check(got[4], want[4], 0.7 * np.abs(f["w_post"] * f["y"]) * q * mh)
+
+
+@pytest.mark.parametrize("tokens,d", [(3, 96), (5, 2047)])
+def test_backward_of_rows_of_zeros_with_a_tiny_eps(tokens, d):
+    """A row of zeros under eps = 1e-40: r = 1e20, whose square is beyond fp32, while r (a - h' r^2 mean(a h')) = r a."""
+    s = inputs(tokens, d, True, None, seed=12)
+    s["h"][1], s["y"][1] = 0, 0
+    s["dh"][1] = 0
+    got = qg.residual_norm_backward(s["du"], s["dh"], s["h"], s["y"], s["w_post"], None, s["w_pre"], eps=1e-40)
+    a = f64(s["w_pre"]) * f64(s["du"][1])
+    eps = float(torch.tensor(1e-40, dtype=torch.float32))
+    assert np.all(np.abs(f64(got[0])[1] - a / np.sqrt(eps)) <= 16 * U24 * np.abs(a) / np.sqrt(eps))
+    assert all(bool(torch.isfinite(t[[0, 2]]).all()) for t in got[:2]) and bool(torch.isfinite(got[2]).all())
