@@ -414,7 +414,8 @@ static int launch_head_rows(HeadRows a, hipStream_t st) {
 
 // dW's rows of a piece, dl^T x: direct loads of whole tiles (4096 tokens, 16128 x 4096: 488 us, 1109 TFLOP/s; 512, 32003 x 2048: 87 to 95,
 // through registers 113).  dl's rows are a multiple of 128 elements apart, x's of 256, so that a
-// tile never leaves its row; what stands between their ends and that only reaches elements that are not stored.
+// tile never leaves its row; what stands between their ends and that only reaches elements that are not stored.  (The sizes' limits keep
+// both below kKSlowPitch.)
 static int launch_head_dw(const uint16_t* dl, int64_t pitch, const uint16_t* x, int64_t hp, uint16_t* dW, int64_t ldc, int64_t width,
                           int64_t h, int64_t padded, const int32_t* count, const float* scale, hipStream_t st) {
     const int64_t tiles_m = pitch / kLinTM, tiles_n = hp / 256;

@@ -241,14 +241,18 @@ __global__ __launch_bounds__(256) void k_align_rows(const uint16_t* __restrict__
 // want rows that start on 16 bytes, and x is copied to such where it has others (600 tokens, 2997 and 2 x 6869, us: 97 and 5 for the
 // copy; without direct loads 130).  1000 tokens, 2 x 5461 x 2048: both in one launch 54 us, in two of other tiles 91; 4096 tokens, 2 x 11008
 // x 4096 683 (1080 TFLOP/s).
-static bool grad_w_direct(int64_t m, int64_t n, int count) { return ((m + kLinTM - 1) / kLinTM) * ((n + 255) / 256) * count >= 256; }
+// (Rows longer than that kernel addresses: the other tiles.)
+static int64_t dz_pitch(int64_t m) { return (m + 63) / 64 * 64; }
+static bool grad_w_direct(int64_t m, int64_t n, int64_t ld_n, int count) {
+    return ((m + kLinTM - 1) / kLinTM) * ((n + 255) / 256) * count >= 256 && dz_pitch(m) <= kKSlowPitch && (ld_n + 7) / 8 * 8 <= kKSlowPitch;
+}
 static size_t grad_w_copy_bytes(int64_t tokens, int64_t m, int64_t n, int count) {   // of x, whatever its pitch turns out to be
-    return grad_w_direct(m, n, count) && n % 8 != 0 ? (size_t)tokens * ((n + 7) / 8 * 8) * 2 : 0;
+    return grad_w_direct(m, n, n, count) && n % 8 != 0 ? (size_t)tokens * ((n + 7) / 8 * 8) * 2 : 0;
 }
 static int launch_act_grad_w(const uint16_t* dz, const uint16_t* dz2, int64_t ldz, const uint16_t* x, int64_t ld_n, uint16_t* G, uint16_t* G2,
                              int64_t tokens, int64_t m, int64_t n, uint16_t* copy, hipStream_t st) {
     const int count = dz2 != nullptr ? 2 : 1;
-    if (grad_w_direct(m, n, count)) {
+    if (grad_w_direct(m, n, ld_n, count)) {
         int64_t ldx = ld_n;
         if (ld_n % 8 != 0) {
             ldx = (n + 7) / 8 * 8;
@@ -271,7 +275,6 @@ static int launch_act_grad_w(const uint16_t* dz, const uint16_t* dz2, int64_t ld
     return QG_OK;
 }
 
-static int64_t dz_pitch(int64_t m) { return (m + 63) / 64 * 64; }
 static size_t whole_lines_of(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace qg
@@ -325,7 +328,7 @@ extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16
     if (!products) return QG_OK;
     const LinOperand d = {dz ? dz : dy_bf16, nullptr, dz ? ldz : ld_m, 0}, x = {x_bf16, nullptr, ld_n, 0};
     const LinOperand W = {Wq, Ws, ld_n, (int)((n + kGroup - 1) / kGroup)};
-    if (G_bf16 && dz && grad_w_direct(m, n, 1)) {
+    if (G_bf16 && dz && grad_w_direct(m, n, ld_n, 1)) {
         if (dx_bf16)
             if (int e = launch_linear_backward<kInt8KSlow>(d, W, dx_bf16, tokens, n, m, ld_n, d, x, nullptr, m, n, tokens, ld_n, st)) return e;
         char* copy = reinterpret_cast<char*>(part_at) + whole_lines_of((size_t)act_slabs(tokens, m).count * (size_t)m * 4);

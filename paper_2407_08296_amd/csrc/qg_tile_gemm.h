@@ -655,6 +655,10 @@ __global__ __launch_bounds__(256, 2) void k_gemm_pair(LinProduct p0, LinProduct 
 // Rows of A and B are M and N elements apart.  RAGGED: of any multiple of 8; C is out.rows x out.cols.  Loads are bounded by the end
 // of the operand, past which they read zeros: a last step that is not whole adds nothing.  What a tile reads past the end of a row
 // is the next row, and reaches elements only that are not stored.  One or two (gridDim.y) products of one shape with the same B.
+// A step's 32 rows are addressed from one base, in 31 bits: M and N up to kKSlowPitch.  (Dense and whole, in 512 tiles and more, they
+// are below 2^23 by the limits of the layer's sizes.)
+constexpr int64_t kKSlowPitch = int64_t(1) << 25;
+static_assert(2 * 31 * kKSlowPitch + 512 < 0x7FFFFFFC, "the last row of a step, a tile's columns");
 struct KSlowOut {
     int rows, cols;
     int64_t ldc;

@@ -272,3 +272,18 @@ def test_another_stream_and_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("m,n", [(40000000, 32), (32, 40000000)])
+def test_weight_gradient_of_rows_whose_step_passes_31_bits(m, n):
+    """32 tokens whose rows of dz or x are 80 MB: the last of them lie 2^31 bytes and more behind the first.  relu: dz is exact."""
+    tokens = 32
+    g = torch.Generator(device=DEV).manual_seed(14)
+    x = torch.randn(tokens, n, device=DEV, generator=g, dtype=torch.bfloat16)
+    dy, z = (torch.randn(tokens, m, device=DEV, generator=g, dtype=torch.bfloat16) for _ in range(2))
+    w = torch.zeros(m, n, dtype=torch.int8, device=DEV), torch.zeros(m, -(-n // 256), device=DEV)
+    G = qg.int8_linear_act_backward(dy, z, x, *w, act="relu", want_dx=False)[1]
+    for at in (0, 12345677, 1 << 25, max(m, n) - 500):
+        rows, cols = (slice(at, at + 500), slice(None)) if m > n else (slice(None), slice(at, at + 500))
+        dz, X = f64(dy[:, rows] * (z[:, rows] > 0)), f64(x[:, cols])
+        check(G[rows, cols], dz.T @ X, 4 * tokens * U24 * rss(dz.T, X))
