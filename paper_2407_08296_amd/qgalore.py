@@ -650,17 +650,20 @@ def residual_norm_forward(h: torch.Tensor, y: torch.Tensor | None = None, w_post
                           gate: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, scale: float = 1.0,
                           eps: float = 1e-6, out: torch.Tensor | None = None):
     """Returns (h', u): h' = h + scale * gate * norm(y; w_post), u = norm(h'; w_pre).  h: bf16 or fp32 [tokens][d], gate: None, fp32
-    [d] or bf16 [tokens][d].  Without y, h' is h itself; without w_pre, u is None.  out: where h' is written (h itself: in place)."""
+    [d] or bf16 [tokens][d].  Without y, h' is h itself; without w_pre, u is None.  out: where h' is written (h itself: in place);
+    without y nothing is, and another out than h is refused."""
     tokens, d = h.shape
     stype, fp32 = _stream_type(h)
     for v in (w_post, w_pre):
         _expect(v, d)
     _expect(y, tokens, d)
     g, kind = _gate(gate if y is not None else None, tokens, d)
-    if out is None and y is not None:
-        out = torch.empty_like(h)
-    elif y is None:
+    if y is None:
+        if out is not None and out.data_ptr() != h.data_ptr():
+            raise QGError("out without y: h' is h itself, and is not written anywhere else")
         out = None
+    elif out is None:
+        out = torch.empty_like(h)
     _expect(out, tokens, d)
     u = _bf16_rows(h if y is None else y, tokens, d) if w_pre is not None else None
     _check(lib().qg_residual_norm_forward(_ptr(h, stype), _ptr(y, _BF16), _ptr(w_post, _F32), g, kind, _ptr(w_pre, _F32), scale, eps,

@@ -285,3 +285,13 @@ def test_backward_of_rows_of_zeros_with_a_tiny_eps(tokens, d):
     eps = float(torch.tensor(1e-40, dtype=torch.float32))
     assert np.all(np.abs(f64(got[0])[1] - a / np.sqrt(eps)) <= 16 * U24 * np.abs(a) / np.sqrt(eps))
     assert all(bool(torch.isfinite(t[[0, 2]]).all()) for t in got[:2]) and bool(torch.isfinite(got[2]).all())
+
+
+def test_out_without_a_block_output():
+    """A norm alone leaves the stream where it is: another place for it would stay unwritten, so it is refused."""
+    s = inputs(5, 96, True, None, seed=13)
+    keep, elsewhere = s["h"].clone(), torch.full_like(s["h"], 7.0)
+    with pytest.raises(qg.QGError):
+        qg.residual_norm_forward(s["h"], w_pre=s["w_pre"], out=elsewhere)
+    h, u = qg.residual_norm_forward(s["h"], w_pre=s["w_pre"], out=s["h"])
+    assert h is s["h"] and torch.equal(h, keep) and torch.equal(u, qg.residual_norm_forward(keep, w_pre=s["w_pre"])[1])
