@@ -573,11 +573,18 @@ def int8_linear_act_forward(x: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor,
     return y, z
 
 
-def int8_linear_act_backward(dy: torch.Tensor, z: torch.Tensor | None, x: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor,
-                             act: str = "none", want_dx: bool = True, want_G: bool = True, want_dbias: bool = False):
-    """Returns (dx, G, dbias) of int8_linear_act_forward (None where not wanted); the residual's gradient is dy itself."""
+def _inputs_of(x: torch.Tensor | None, Wq: torch.Tensor | None) -> int:
+    """n, from what a backward pass was given: x may be missing where no G is wanted, the weight where no dx is."""
+    return x.shape[1] if x is not None else Wq.shape[1] if Wq is not None else 1
+
+
+def int8_linear_act_backward(dy: torch.Tensor, z: torch.Tensor | None, x: torch.Tensor | None, Wq: torch.Tensor | None,
+                             Ws: torch.Tensor | None, act: str = "none", want_dx: bool = True, want_G: bool = True,
+                             want_dbias: bool = False):
+    """Returns (dx, G, dbias) of int8_linear_act_forward (None where not wanted); the residual's gradient is dy itself.  z is not
+    needed without an activation, x not without G, the weight not without dx."""
     tokens, m = dy.shape
-    n = x.shape[1]
+    n = _inputs_of(x, Wq)
     kind = _act(act)
     _expect(x, tokens, n)
     _expect(z, tokens, m)
@@ -607,11 +614,13 @@ def int8_gated_forward(x: torch.Tensor, Wgq: torch.Tensor, Wgs: torch.Tensor, Wu
     return y, zg, zu
 
 
-def int8_gated_backward(dy: torch.Tensor, zg: torch.Tensor, zu: torch.Tensor, x: torch.Tensor, Wgq: torch.Tensor, Wgs: torch.Tensor,
-                        Wuq: torch.Tensor, Wus: torch.Tensor, act: str = "silu", want_dx: bool = True, want_G: bool = True):
-    """Returns (dx, Gg, Gu) of int8_gated_forward (None where not wanted)."""
+def int8_gated_backward(dy: torch.Tensor, zg: torch.Tensor, zu: torch.Tensor, x: torch.Tensor | None, Wgq: torch.Tensor | None,
+                        Wgs: torch.Tensor | None, Wuq: torch.Tensor | None, Wus: torch.Tensor | None, act: str = "silu",
+                        want_dx: bool = True, want_G: bool = True):
+    """Returns (dx, Gg, Gu) of int8_gated_forward (None where not wanted).  x is not needed without Gg and Gu, the weights not
+    without dx."""
     tokens, m = dy.shape
-    n = x.shape[1]
+    n = _inputs_of(x, Wgq)
     _expect(x, tokens, n)
     for v in (zg, zu):
         _expect(v, tokens, m)

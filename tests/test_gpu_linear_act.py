@@ -287,3 +287,24 @@ def test_weight_gradient_of_rows_whose_step_passes_31_bits(m, n):
         rows, cols = (slice(at, at + 500), slice(None)) if m > n else (slice(None), slice(at, at + 500))
         dz, X = f64(dy[:, rows] * (z[:, rows] > 0)), f64(x[:, cols])
         check(G[rows, cols], dz.T @ X, 4 * tokens * U24 * rss(dz.T, X))
+
+
+def test_backward_passes_without_what_they_do_not_need():
+    """x where only dx is wanted, the weights where only their gradients are, either where only dbias is: the same bits as with them."""
+    g = torch.Generator().manual_seed(15)
+    (wg, _), (wu, _) = weight(g, 130, 70), weight(g, 130, 70)
+    x, dy, z, zu = normal(g, 33, 70), normal(g, 33, 130), normal(g, 33, 130), normal(g, 33, 130)
+    none = (None, None)
+    for act in ("none", "gelu"):
+        dx, G, db = qg.int8_linear_act_backward(dy, z, x, *wg, act=act, want_dbias=True)
+        assert torch.equal(qg.int8_linear_act_backward(dy, z, None, *wg, act=act, want_G=False)[0], dx)
+        assert torch.equal(qg.int8_linear_act_backward(dy, z, x, *none, act=act, want_dx=False)[1], G)
+        assert torch.equal(qg.int8_linear_act_backward(dy, z, None, *none, act=act, want_dx=False, want_G=False, want_dbias=True)[2], db)
+    dx, Gg, Gu = qg.int8_gated_backward(dy, z, zu, x, *wg, *wu)
+    assert torch.equal(qg.int8_gated_backward(dy, z, zu, None, *wg, *wu, want_G=False)[0], dx)
+    alone = qg.int8_gated_backward(dy, z, zu, x, *none, *none, want_dx=False)
+    assert torch.equal(alone[1], Gg) and torch.equal(alone[2], Gu)
+    for bad in (lambda: qg.int8_linear_act_backward(dy, z, None, *wg, act="gelu"), lambda: qg.int8_linear_act_backward(dy, z, x, *none, act="gelu"),
+                lambda: qg.int8_gated_backward(dy, z, zu, None, *wg, *wu), lambda: qg.int8_gated_backward(dy, z, zu, x, *wg, *none)):
+        with pytest.raises(qg.QGError):
+            bad()
