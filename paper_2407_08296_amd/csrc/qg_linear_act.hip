@@ -122,20 +122,24 @@ static Slabs act_slabs(int64_t tokens, int64_t m) {
 // 84 / 81, 1024 x 4096 51.9 / 48.8, 1024 x 8192 147 / 133.
 static bool act_one_slab(int64_t tokens, int64_t m) { return tokens <= 2048 && tokens * m <= (int64_t(1) << 21); }
 
-// part: one row of sums per slab, or dbias itself where there is one slab
+// part: one row of sums per slab, or dbias itself where there is one slab (a pair has no dbias)
 template <bool PAIR>
 static int launch_act_backward(const uint16_t* dy, const uint16_t* zg, const uint16_t* zu, uint16_t* dzg, uint16_t* dzu, float* part,
                                float* dbias, int64_t tokens, int64_t m, int64_t ld, int64_t ld_out, int kind, hipStream_t st) {
-    if (dbias != nullptr && act_one_slab(tokens, m)) {
-        hipLaunchKernelGGL((k_act_backward<PAIR, 2>), dim3((unsigned)((m + 15) / 16)), dim3(512), 0, st, dy, zg, zu, dzg, dzu, dbias,
-                           (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
-        return check_launch();
+    if constexpr (!PAIR) {
+        if (dbias != nullptr && act_one_slab(tokens, m)) {
+            hipLaunchKernelGGL((k_act_backward<false, 2>), dim3((unsigned)((m + 15) / 16)), dim3(512), 0, st, dy, zg, zu, dzg, dzu, dbias,
+                               (int)tokens, (int)m, ld, ld_out, (int)tokens, kind);
+            return check_launch();
+        }
     }
     const Slabs s = act_slabs(tokens, m);
     hipLaunchKernelGGL((k_act_backward<PAIR, 64>), dim3((unsigned)((m + 511) / 512), (unsigned)s.count), dim3(256), 0, st, dy, zg, zu, dzg,
                        dzu, dbias != nullptr ? part : nullptr, (int)tokens, (int)m, ld, ld_out, s.rows, kind);
-    if (dbias != nullptr)
-        hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, part, s.count, (int)m, dbias);
+    if constexpr (!PAIR) {
+        if (dbias != nullptr)
+            hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, st, part, s.count, (int)m, dbias);
+    }
     return check_launch();
 }
 

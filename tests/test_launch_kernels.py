@@ -1,4 +1,7 @@
 """Which kernels the operators around the linear layer launch, as the host decides on it (tests/launch_kernels_driver.cpp)."""
+import math
+import random
+
 import pytest
 
 import launch_kernels
@@ -22,3 +25,28 @@ def test_direct_loads_of_long_rows(launches):
         assert any(k[0].startswith("k_gemm_kslow_direct<unsigned short, true>") for k in got), call
     for call, got in zip(long, launches(long)):
         assert not any(k[0].startswith(("k_gemm_kslow_direct", "k_align_rows")) for k in got), call
+
+
+# kernels of the operators around the linear layer (the weight gradient's by direct loads is theirs in its ragged form)
+OWN = ("k_residual_norm", "k_act_backward", "k_column_sums", "k_gemm_epilogue", "k_ksplit_epilogue", "k_join_parts", "k_align_rows", "k_head",
+       "k_gemm_kslow_direct<unsigned short, true>")
+
+
+def test_every_kernel_is_launched_by_some_call(launches):
+    """Sizes spread over their range, a third of them whatever comes, the rest multiples of 64 and of 256."""
+    rng = random.Random(1)
+
+    def size(most):
+        v, r = int(round(math.exp(rng.uniform(0, math.log(most))))), rng.random()
+        return max(1, v if r < 1 / 3 else v // 64 * 64 if r < 2 / 3 else v // 256 * 256)
+    calls = [("kernels",), ("act_forward", 1024, 4096, 1024, 0), ("act_forward", 1000, 4090, 1024, 0)]   # (256 tiles of 128 x 128: the only
+    # number of them that is taken in two groups of waves)
+    for _ in range(12000):
+        tokens, m, n = size(9000), size(12000), size(12000)
+        calls += [("act_forward", tokens, m, n, 0), ("act_backward", tokens, m, n, 0, rng.randrange(4), rng.randrange(1, 8)),
+                  ("gated_forward", tokens, m, n, 0), ("gated_backward", tokens, m, n, 0, 2, rng.randrange(1, 4))]
+        calls += [("head_forward", tokens, n, size(130000), 0), ("head_backward", tokens, n, size(130000), 0, 0, rng.randrange(1, 4))]
+        calls += [(w, tokens, size(16384), rng.randrange(2), rng.randrange(3)) for w in ("norm_forward", "norm_backward")]
+    held, *got = launches(calls)
+    launched = {k[0] for one in got for k in one}
+    assert len(held) > 50 and [k[0] for k in held if k[0].startswith(OWN) and k[0] not in launched] == []
