@@ -351,11 +351,11 @@ static int64_t head_chunk(int64_t tokens, int64_t h, int64_t piece) {
     return splits <= 1 ? piece : up((piece + splits - 1) / splits, 64);
 }
 
-// Entries of a piece: dl of one piece stays below 128 MiB (so that both products find it in the 256 MB cache behind the L2s), 1024
-// entries at least, pieces of about one size.  4096 tokens, us, pieces of 128 / 64 MiB: 32000 x 768 1002 / 1171, 32000 x 4096
-// 3895 / 4006.
-static int64_t head_piece(int64_t tokens, int64_t vocab) {
-    const int64_t most = (int64_t(1) << 26) / tokens;
+// Entries of a piece: dl of one piece, of all rows that the tokens are padded to, takes 128 MiB at most (so that both products find it in
+// the 256 MB cache behind the L2s), but 1024 entries at least (beyond 65536 tokens that is more); pieces of about one size, multiples of
+// 256.  4096 tokens, us, pieces of 128 / 64 MiB: 32000 x 768 1002 / 1171, 32000 x 4096 3895 / 4006.
+static int64_t head_piece(int64_t padded, int64_t vocab) {
+    const int64_t most = (int64_t(1) << 26) / padded / 256 * 256;
     const int64_t piece = most < 1024 ? 1024 : most;
     const int64_t pieces = (vocab + piece - 1) / piece;
     const int64_t even = up((vocab + pieces - 1) / pieces, 256);
@@ -384,7 +384,7 @@ static HeadSpace head_space(int64_t tokens, int64_t h, int64_t vocab, bool backw
     s.labels = take((size_t)s.padded * 4);
     s.x = take((size_t)s.padded * s.hp * 2);
     if (backward) {
-        s.piece = head_piece(tokens, vocab);
+        s.piece = head_piece(s.padded, vocab);
         s.chunk = head_chunk(s.padded, h, s.piece);
         s.splits = (s.piece + s.chunk - 1) / s.chunk;
         s.lse = take((size_t)s.padded * 4);

@@ -50,3 +50,20 @@ def test_every_kernel_is_launched_by_some_call(launches):
     held, *got = launches(calls)
     launched = {k[0] for one in got for k in one}
     assert len(held) > 50 and [k[0] for k in held if k[0].startswith(OWN) and k[0] not in launched] == []
+
+
+@pytest.mark.parametrize("tokens,vocab", [(1, (1 << 24) - 1), (64, 2000000), (65, 600000), (129, 520000), (513, 130000), (1000, 66000), (4096, 32000),
+                                          (5000, 50304), (30000, 128256), (65536, 4100)])
+def test_pieces_of_the_vocabulary(launches, tokens, vocab):
+    """dz of a piece, of the rows that the tokens are padded to, takes 128 MiB at most, and the pieces cover the vocabulary."""
+    got, = launches([("head_backward", tokens, 64, vocab, 0, 0, 2)])
+    unit = 64 if tokens <= 64 else 128 if tokens <= 512 else 256
+    padded = -(-tokens // unit) * unit
+    covered = 0
+    for name, grid, _, _ in (k for k in got if "DLogitsRun" in k[0]):
+        a = [v.strip() for v in name[name.index("<") + 1:].split(",")]
+        rows, cols = 32 * int(a[3]) * int(a[6]), int(a[4])
+        down = -(-padded // rows)                                    # tiles; the grid is the next multiple of 8
+        covered += grid // down * cols
+        assert padded * max((grid - 7) // down, 1) * cols * 2 <= 1 << 27, (name, grid)
+    assert covered >= vocab
