@@ -1,6 +1,7 @@
 """Builds libqgalore.so (HIP, gfx950 only) in-tree with hipcc: one object per source, compiled in parallel, then linked."""
 from __future__ import annotations
 
+import functools
 import os
 import subprocess
 from concurrent.futures import ThreadPoolExecutor
@@ -46,19 +47,24 @@ def build(verbose: bool = False, extra_flags: list[str] | None = None, lib: str 
     return lib
 
 
-def build_sanitized(driver_src: str, verbose: bool = False) -> str:
-    """Host-side AddressSanitizer + UBSan build: the library with its HOST code instrumented (the sanitizer flags sit
-    behind -Xarch_host; device code is compiled as usual) as _build/libqgalore_san.so, and `driver_src` (a host
-    program that walks the ABI's validation paths) linked against it as _build/abi_sanitizer_driver.  Returns the
-    driver's path; run it with LD_LIBRARY_PATH pointing at _build/."""
+@functools.lru_cache(maxsize=1)
+def _sanitized_library(verbose: bool) -> str:
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
-    lib = build(verbose=verbose, extra_flags=san, lib=os.path.join(OBJ, "libqgalore_san.so"),
-                link_flags=["-fsanitize=address", "-fsanitize=undefined"])
+    return build(verbose=verbose, extra_flags=san, lib=os.path.join(OBJ, "libqgalore_san.so"),
+                 link_flags=["-fsanitize=address", "-fsanitize=undefined"])
+
+
+def build_sanitized(driver_src: str, verbose: bool = False) -> str:
+    """Host-side AddressSanitizer + UBSan build: the library with its HOST code instrumented (the sanitizer flags sit
+    behind -Xarch_host; device code is compiled as usual) as _build/libqgalore_san.so, once per process, and `driver_src`
+    (a host program that walks the ABI's validation paths) linked against it as _build/<its name>.  Returns the
+    driver's path; run it with LD_LIBRARY_PATH pointing at _build/."""
+    _sanitized_library(verbose)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    exe = os.path.join(OBJ, "abi_sanitizer_driver")
+    exe = os.path.join(OBJ, os.path.splitext(os.path.basename(driver_src))[0])
     cmd = [hipcc, "-x", "c++", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined",
-           "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"), driver_src,
+           "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"), driver_src, "-rdynamic",
            "-L", OBJ, "-lqgalore_san", "-Wl,-rpath," + OBJ, "-o", exe]
     if verbose:
         print(" ".join(cmd), flush=True)

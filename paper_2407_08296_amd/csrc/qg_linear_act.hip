@@ -326,7 +326,7 @@ extern "C" int qg_int8_linear_act_backward(const uint16_t* dy_bf16, const uint16
     const bool products = dx_bf16 || G_bf16;
     const int64_t ldz = dz_pitch(m);
     uint16_t* dz = act != QG_ACT_NONE && products ? static_cast<uint16_t*>(workspace) : nullptr;
-    float* part_at = reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2));
+    float* part_at = dz || dbias ? reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_lines_of((size_t)tokens * ldz * 2)) : nullptr;
     if (dz || dbias)
         if (int e = launch_act_backward<false>(dy_bf16, z_bf16, nullptr, dz, nullptr, part_at, dbias, tokens, m, ld_m, ldz, act, st)) return e;
     if (!products) return QG_OK;

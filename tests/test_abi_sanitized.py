@@ -20,3 +20,15 @@ def test_abi_validation_paths_under_asan_ubsan():
     assert p.returncode == 0, out[-4000:]
     assert "sanitizer driver ok" in p.stdout
     assert "ERROR: AddressSanitizer" not in out and "runtime error:" not in out, out[-4000:]
+
+
+def test_host_code_of_the_operators_around_the_linear_layer_under_asan_ubsan():
+    exe = qg_build.build_sanitized(os.path.join(HERE, "abi_operators_sanitizer_driver.cpp"))
+    env = dict(os.environ)
+    env["ASAN_OPTIONS"] = "detect_leaks=0:abort_on_error=0:halt_on_error=1"
+    env["UBSAN_OPTIONS"] = "print_stacktrace=1:halt_on_error=1"
+    p = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    out = p.stdout + p.stderr
+    assert p.returncode == 0, out[-4000:]
+    assert "sanitizer driver ok" in p.stdout
+    assert "ERROR: AddressSanitizer" not in out and "runtime error:" not in out, out[-4000:]
