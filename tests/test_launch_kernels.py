@@ -67,3 +67,31 @@ def test_pieces_of_the_vocabulary(launches, tokens, vocab):
         covered += grid // down * cols
         assert padded * max((grid - 7) // down, 1) * cols * 2 <= 1 << 27, (name, grid)
     assert covered >= vocab
+
+
+def test_every_kernel_is_launched_by_a_test(launches):
+    """The sizes of the tests on the GPU, by what the host makes of them."""
+    import test_gpu_head_loss as head
+    import test_gpu_linear_act as layer
+    import test_gpu_operator_kernels as more
+    import test_gpu_residual_norm as norm
+    calls = [("kernels",)]
+    calls += [("act_forward", *s, 0) for s in layer.CASES + more.ACT_FORWARD]
+    calls += [("act_backward", *s, 0, act, out) for s in layer.CASES + layer.SLABS + more.ACT_DIRECT for act, out in ((0, 7), (3, 1), (3, 2), (3, 4), (3, 7))]
+    calls += [("gated_forward", *s, 0) for s in layer.CASES + layer.GATED + more.GATED_FORWARD]
+    calls += [("gated_backward", *s, 0, 2, out) for s in layer.CASES + more.GATED_DX + more.GATED_DIRECT for out in (1, 2, 3)]
+    calls += [("head_forward", *s, 0) for s in head.CASES + more.TOGETHER + more.HEAD]
+    calls += [("head_backward", *s, 0, 0, 3) for s in head.CASES + head.PARTS + more.HEAD]
+    calls += [(w, *s, fp32, gate) for w in ("norm_forward", "norm_backward") for s in norm.SHAPES for fp32 in (0, 1) for gate in (0, 1, 2)]
+    held, *got = launches(calls)
+    launched = {k[0] for one in got for k in one}
+    assert [k[0] for k in held if k[0].startswith(OWN) and k[0] not in launched] == []
+    # ... and the forms of one kernel that its name does not tell apart
+    of = dict(zip(calls[1:], got))
+    names = lambda *call: [k[0] for k in of[call]]
+    assert all("k_head_rows" in names("head_forward", *s, 0) for s in more.TOGETHER)
+    for s in more.ACT_DIRECT:
+        assert any(k.startswith("k_gemm_kslow_direct") for k in names("act_backward", *s, 0, 3, 2))
+    for s in more.GATED_DIRECT:                                       # both weights' gradients in one launch
+        assert [k[2] for k in of[("gated_backward", *s, 0, 2, 2)] if k[0].startswith("k_gemm_kslow_direct")] == [2]
+    assert "k_align_rows" in names("act_backward", 65, 5463, 2051, 0, 3, 2) and "k_align_rows" in names("gated_backward", 33, 5461, 1027, 0, 2, 2)
