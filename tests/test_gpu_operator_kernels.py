@@ -196,3 +196,31 @@ def test_tokens_put_together_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_long_batch_whose_dz_passes_2_to_the_31_elements():
+    """Rows of dz are 64 elements apart in the workspace whatever m is: 40000003 tokens reach past 2^31 of them.  dy is zero but for some
+    hundred rows at both ends and around 2^31 / 64, so that G has few terms and dx few rows."""
+    tokens, m, n = 40000003, 5, 8
+    gen = torch.Generator().manual_seed(16)
+    (wg, Wg), (wu, Wu) = layer.weight(gen, m, n), layer.weight(gen, m, n)
+    g = torch.Generator(device=DEV).manual_seed(17)
+    x, zg, zu = (torch.randn(tokens, k, device=DEV, generator=g, dtype=torch.bfloat16) for k in (n, m, m))
+    at = torch.cat([torch.arange(v, v + 200, device=DEV) for v in (0, (1 << 25) - 100, tokens - 200)])
+    dy = torch.zeros(tokens, m, dtype=torch.bfloat16, device=DEV)
+    dy[at] = torch.randn(len(at), m, device=DEV, generator=g).bfloat16()
+    X, DY, ZG, ZU = (layer.f64(t[at]) for t in (x, dy, zg, zu))
+    r, rss, k = 4 * 2.0 ** -8, layer.rss, len(at)
+    dz = DY * O.act(ZG, "silu")[1]
+    dx, G, db = qg.int8_linear_act_backward(dy, zg, x, *wg, act="silu", want_dbias=True)
+    layer.check(dx[at], dz @ Wg, (r + 4 * m * U24) * rss(dz, Wg) + 1e-6 * rss(DY, Wg))
+    layer.check(G, dz.T @ X, (r + 4 * k * U24) * rss(dz.T, X) + 1e-6 * rss(DY.T, X))
+    assert np.all(np.abs(layer.f64(db) - dz.sum(0)) <= 8 * (1 + np.sqrt(k)) * U24 * np.abs(dz).sum(0) + 5e-7 * np.abs(DY).sum(0))
+    assert int((dx != 0).any(1).sum()) <= k
+    dx, Gg, Gu = qg.int8_gated_backward(dy, zg, zu, x, *wg, *wu)
+    a, da = O.act(ZG, "silu")
+    dzg, dzu = DY * ZU * da, DY * a
+    layer.check(dx[at], dzg @ Wg + dzu @ Wu, (r + 4 * m * U24) * (rss(dzg, Wg) + rss(dzu, Wu)) + 1e-6 * (rss(DY * ZU, Wg) + rss(DY * ZG, Wu)))
+    layer.check(Gg, dzg.T @ X, (r + 4 * k * U24) * rss(dzg.T, X) + 1e-6 * rss((DY * ZU).T, X))
+    layer.check(Gu, dzu.T @ X, (r + 4 * k * U24) * rss(dzu.T, X) + 1e-6 * rss((DY * ZG).T, X))
+    assert int((dx != 0).any(1).sum()) <= k
