@@ -350,7 +350,7 @@ int qg_int8_linear_t_zp_backward(const uint16_t* dy_bf16, const uint16_t* x_bf16
  *     h' = h + scale * gate * n           gate_kind: none (1), fp32 [d], or bf16 [tokens][ld]
  *     u  = w_pre * h' / rms(h')           bf16; from h' as it is before it is rounded to the stream's type
  * h and h' (h_out) are bf16, or fp32 with stream_fp32 != 0.  y NULL: h' = h, h_out is not written (a norm alone).
- * u NULL: not computed.  h_out may be h.  w_post, w_pre: fp32 [d].
+ * u NULL: not computed.  h_out may be h.  w_post, w_pre: fp32 [d].  eps: 0 or more (with 0, a row of zeros has no rms).
  *
  * qg_residual_norm_backward: the gradients at h_next = h' as stored, given du and dh_next (the stream's own gradient at
  * h', in the stream's type; either may be NULL: 0): dh of h and, in the sum, of h' alike (may be dh_next), dy (bf16),
@@ -405,7 +405,8 @@ int qg_int8_gated_backward(const uint16_t* dy_bf16, const uint16_t* zg_bf16, con
 /* ---- Loss of a language model's head: softmax cross entropy over the vocabulary, without the logits in memory.
  * z = x W^T with x bf16 [tokens][h] and W bf16 [vocab][h]; labels int64 [tokens], a label outside [0, vocab) marks a token
  * without a loss (padding, a prompt): its loss, lse and row of dx are 0, and it adds nothing to dW whatever its row of x holds.
- * Such tokens take no part in the products and cost next to nothing.
+ * Such tokens take no part in the products; what that saves comes in steps of 64 to 256 tokens, and is least in dx of a batch of
+ * thousands with few labels.
  * qg_head_loss_forward:  lse = log sum_v exp z_v, loss = lse - z_label, fp32 [tokens].
  * qg_head_loss_backward: from lse and dloss (fp32 [tokens], the gradient of each token's loss: a mean's 1/count, a weight),
  *   dz = dloss (exp(z - lse) - onehot), rounded to bf16;  dx = dz W, dW = dz^T x, either may be NULL.  The vocabulary is

@@ -5,8 +5,9 @@
 //     gated forward:   y = act(x Wg^T) * (x Wu^T)
 //     gated backward:  dzg = dy zu act'(zg),  dzu = dy act(zg),  dx = dzg Wg + dzu Wu,  Gg = dzg^T x,  Gu = dzu^T x
 // W is dequantized while it is staged, as in the plain layer.  The forward passes are one launch: the activation is applied to
-// the fp32 sums, and z is rounded only where it is stored for the backward pass.  dz goes through the workspace as bf16 (it is an
-// operand of two products), made by one pass over dy and z, in rows of whole cache lines whatever m is.
+// the fp32 sums, and z is rounded only where it is stored for the backward pass.  dz goes through the workspace, made by one pass over dy
+// and z, in rows of whole cache lines whatever m is.  It is rounded to bf16 there, as an operand of two bf16 products: dx and G are then
+// off by 0.0023 of their norm where their own rounding alone gives 0.0017.  dbias takes dz in fp32.
 #include "qg_epilogue.h"
 
 namespace qg {
@@ -170,10 +171,10 @@ static int launch_act_forward(EpiProduct<LinOperand, EPI> p, hipStream_t st) {
     return launch_epilogue_shape<AL, BL, 2, 128, 64, 2, true, true, 1, 1>(p, st);
 }
 
-// ... of a pair: N columns of each, the tile's columns shared between the two so that x is staged once for both.  4096 tokens, 4096 ->
-// 2 x 11008: 727 us (1016 TFLOP/s; without zg and zu 9 % less: their stores come at the end of a tile, when the CU's matrix pipe is
-// idle); 256 tokens 80 us; one token 26.6 us (3.4 TB/s of codes; a kernel that loads them straight into matrix operands, without LDS,
-// took 25.9 to 30).
+// ... of a pair: N columns of each, the tile's columns shared between the two so that x is staged once for both.  4096 tokens, 4096 -> 2 x
+// 11008: 727 to 755 us from card to card (1016 to 978 TFLOP/s; without zg and zu 9 % less: their stores come at the end of a tile, when the
+// CU's matrix pipe is idle); 256 tokens 80 us; one token 26.6 us (3.4 TB/s of codes; a kernel that loads them straight into matrix operands,
+// without LDS, took 25.9 to 30).
 // Tiles, us, by what the rule takes / the next one (T32: blocks of 32 x 32 columns of each; T64, T128: tiles of 64 or 128 tokens by 64):
 //  * the contraction over waves up to T32 = 512: 64 tokens, 4096 -> 8192 (512) 26.8 / 28.5, 64 tokens, 1024 -> 5461 (342) 8.7 / 10.3, but
 //    150 tokens, 2047 -> 4095 (640) 38.5 / 24.0, 64 tokens, 4096 -> 11008 (688) 40 / 30.
@@ -202,7 +203,8 @@ static int launch_gated_forward(EpiProduct<LinPairOperand, EPI> p, hipStream_t s
 // over workgroups, parts of 512 at least, in fp32 through the workspace.  1000 tokens, 2 x 5461 -> 2048, us: 68 and 7 for the sum of
 // four parts, 110 in 64 x 64 tiles that take the whole contraction (the pass: 149, 155 and 161 with parts for one and for four
 // workgroups per CU; 256 tokens, 2 x 11008 -> 4096 170, 172, 180; 1400 tokens, 2 x 5461 -> 2048 200, 210, 197); 4096 tokens, 2 x 11008
-// -> 4096 700 (1055 TFLOP/s).
+// -> 4096 700 (1055 TFLOP/s).  Ragged 256 x 256 tiles hold 233 registers of a lane in scratch for the checks of two products beside two
+// register sets; with dz, 4000 tokens take 763 us like 4096 with 781 (3840, which are 240 of these tiles and go by 128 x 128, 898).
 static int64_t gated_dx_chunk(int64_t tokens, int64_t m, int64_t n) {
     const int64_t t128 = ((tokens + 127) / 128) * ((n + 127) / 128), room = 512 / t128, most = m / 512, splits = room < most ? room : most;
     return splits <= 1 ? m : ((m + splits - 1) / splits + 63) / 64 * 64;

@@ -6,7 +6,8 @@
 //     dh = dh' + r (a - h' r^2 mean(a h'))        of h and h' alike
 //     dy = q (k dh - y q^2 mean(k dh y))
 //     dw_pre = sum_t du h' r,   dw_post = sum_t scale gate dh y q,   dgate = scale dh w_post y q (summed over t if per channel)
-// Every array is read or written once; a row stays in the registers of one workgroup (or wave).  All of it is bound by HBM.
+// Every array is read or written once; a row stays in the registers of one workgroup (or wave), and HBM is the bound.  Not so the backward
+// pass of rows beyond 8192 elements: it spills, and is bound by that (see there).
 #include "qg_common.h"
 #include "qg_gemm_kernels.h"
 
@@ -235,11 +236,12 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void k_residual_norm_fwd
 // one reduction of six sums serves both norms.  A workgroup has ROWS rows at a time, `per` times, and keeps the columns' sums over
 // them in registers: dw_pre's, and E = sum_t dh y q (times the gate where that is per token), of which dw_post and a channel's dgate
 // are multiples.  At its end the ROWS sums are added in order.
-// CH == 1 (rows of up to 8192): the vectors stay in registers; with two chunks per lane there are none left for them.  (Fetching the
-// next rows ahead of the present ones' sums as well: 8192 x 4096 the same, 4096 x 2048 with a gate per token 65 us against 38, for the
-// registers that it spills.)  8 elements per lane and 16 waves per workgroup instead of 16 and 4, which took twice the registers and
-// twice the partial sums: 8192 x 4096, bf16, 112 us -> 88 (4.6 TB/s); 4096 x 2048, fp32 stream, gate per token 38 us (4.8 TB/s); 1000 x
-// 2047 of the same 16 us, one row per wave group: latency.
+// CH == 1 (rows of up to 8192): the vectors stay in registers; with two chunks per lane there are none left for them.  (Fetching the next
+// rows ahead of the present ones' sums as well: 8192 x 4096 the same, 4096 x 2048 with a gate per token 65 us against 38, for the registers
+// that it spills.)  Two chunks per lane and their columns' sums do not fit either: 116 to 190 registers of a lane live in scratch, and 8192
+// x 16384, bf16, takes 831 us (1.9 TB/s), 4096 x 9216 371, where 4096 x 8192 takes 96 (4.2 TB/s).  8 elements per lane and 16 waves per
+// workgroup instead of 16 and 4, which took twice the registers and twice the partial sums: 8192 x 4096, bf16, 112 us -> 88 (4.6 TB/s); 4096
+// x 2048, fp32 stream, gate per token 38 us (4.8 TB/s); 1000 x 2047 of the same 16 us, one row per wave group: latency.
 template <typename S, int WPR, int CH, int ROWS, bool TOKEN_GATE>
 __global__ __launch_bounds__(64 * WPR * ROWS, 4) void k_residual_norm_bwd(
     NormArgs a, const uint16_t* __restrict__ du, const S* dh_next, const S* __restrict__ h, const uint16_t* __restrict__ y, S* dh,
