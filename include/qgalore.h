@@ -422,6 +422,87 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
                           const float* dloss, int64_t tokens, int64_t h, int64_t vocab, int64_t ld, uint16_t* dx_bf16,
                           uint16_t* dW_bf16, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Attention half of a decoder layer: rotary positions, attention over packed sequences, and a cache of keys and values in pages with
+ * the attention of one new token over it.
+ *
+ * qg_heads: a bf16 array [tokens][heads][d] with the strides given, in elements, both multiples of 8, token_stride below 2^23
+ *   (so that q, k and v may be slices of one linear layer's output, or heads may be the outer index).  Elements of a head are consecutive.
+ *
+ * qg_rope_forward: the pairs (a, b) of the first `rot` elements of every head of q and k (k may be NULL, with heads_k = 0) become
+ *     amplitude * (a cos t - b sin t, a sin t + b cos t),   t = positions[token] * freqs[pair];
+ *   QG_ROPE_HALF: pair i is elements (i, i + rot/2), QG_ROPE_INTERLEAVED: (2i, 2i + 1); elements from rot on are copied.  rot is even, 2 <= rot <= d;
+ *   1 <= d <= 1024; positions int64, freqs double [rot/2] (device).  Angles are formed in 64 bits.  An output may be its input.
+ * qg_rope_backward: its gradients, turned back: dq and dk from those of the outputs (the same call with -t).
+ * qg_rope_frequencies (HOST ONLY, `out` is a host pointer to rot/2 doubles): base^(-2i/rot); with a factor other than 1 stretched to longer
+ *   contexts: frequencies that turn at most `low` times over `context` positions are divided by factor, those that turn at least `high`
+ *   times are kept, those between go from one to the other linearly in their turns; context 0: all are divided.
+ *
+ * qg_attention_forward: for each query of a sequence, over the keys of the same sequence that are visible to it,
+ *     x = scale q.k;  cap > 0: x = cap tanh(x / cap);  slopes: x -= slopes[head] |distance|;  o = softmax(x) v, lse = log sum exp x.
+ *   Tokens are packed: sequence i has queries cu_q[i] .. cu_q[i+1] - 1 and keys cu_k[i] .. cu_k[i+1] - 1 (int32 [sequences + 1] on the device,
+ *   ascending, the first is 0; cu_k NULL: the queries' (tokens_q = tokens_k then); both NULL: one sequence of all tokens).  Query i of a
+ *   sequence stands at position i + n_keys - n_queries, the distance to key j is that minus j.  Visible: with causal, keys that are not
+ *   behind the query and, with window > 0, nearer than window, or, with prefix (int32 [sequences]), among the first prefix keys of the
+ *   sequence; window and prefix exclude each other and need causal; without causal all keys.  Query head h reads key head
+ *   h / (heads_q / heads_k).  lse: fp32 [heads_q][tokens_q], may be NULL.  A query without a visible key, and tokens behind
+ *   the last sequence: o = 0, lse = -inf.  Those tokens' q, k and v are not read; inside a sequence a value that is not finite can
+ *   reach every query of its sequence.
+ * qg_attention_backward: dq, dk, dv from do, the forward pass's inputs and its o and lse (as stored: delta = sum do o).  Sums of the heads that
+ *   share k and v, and over tokens, are added in a fixed order.  Slopes have no gradient.
+ *   d: a multiple of 8 up to 128.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
+ *   workspace: qg_attention_workspace_bytes(a) bytes, 16-byte aligned, for either call.
+ *
+ * qg_cache: keys and values of `sequences` sequences in pages: position p of sequence s is row p % page_size of page
+ *   table[s][p / page_size].  An entry outside [0, pages) has no page: nothing is written there, and its keys are not visible.
+ *   pages * page_size below 2^31, sequences * width below 2^31.
+ * qg_cache_append: k and v of `tokens` tokens to their place: token t belongs to sequence[t] (NULL: t) and stands at positions[t]; one without
+ *   a place is left out.  k is turned as by qg_rope_forward on its way, and so is q (NULL, with heads_q = 0: none) to q_out (may be q); rot 0:
+ *   nothing is turned (freqs NULL).  Of two tokens with one place either may win.
+ * qg_attention_paged: one new token per sequence: o = softmax over positions 0 .. lengths[s] - 1 of the cache, the query standing
+ *   at lengths[s] - 1; scores, cap, slopes and window as above, d a multiple of 8 up to 128.  No length (or no page): o = 0.  What the
+ *   cache holds outside the visible positions is not looked at.  workspace: qg_attention_paged_workspace_bytes(c, heads_q) bytes, 16-byte
+ *   aligned; calls that may run at the same time need one each. */
+typedef struct {
+    uint16_t* data;
+    int64_t token_stride, head_stride;
+} qg_heads;
+enum { QG_ROPE_HALF = 0, QG_ROPE_INTERLEAVED = 1 };
+int qg_rope_frequencies(int rot, double base, double factor, double context, double low, double high, double* out);
+int qg_rope_forward(const qg_heads* q, int heads_q, const qg_heads* k, int heads_k, const int64_t* positions, const double* freqs,
+                    int64_t tokens, int d, int rot, int layout, float amplitude, const qg_heads* q_out, const qg_heads* k_out, void* stream);
+int qg_rope_backward(const qg_heads* dq_out, int heads_q, const qg_heads* dk_out, int heads_k, const int64_t* positions, const double* freqs,
+                     int64_t tokens, int d, int rot, int layout, float amplitude, const qg_heads* dq, const qg_heads* dk, void* stream);
+
+typedef struct {
+    int64_t tokens_q, tokens_k;         /* rows of q and o, of k and v */
+    int heads_q, heads_k, d, sequences;
+    const int32_t *cu_q, *cu_k;
+    const int32_t* prefix;
+    const float* slopes;
+    float scale, cap;
+    int causal;
+    int64_t window;
+} qg_attention;
+size_t qg_attention_workspace_bytes(const qg_attention* a);
+int qg_attention_forward(const qg_attention* a, const qg_heads* q, const qg_heads* k, const qg_heads* v, const qg_heads* o, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
+int qg_attention_backward(const qg_attention* a, const qg_heads* dO, const qg_heads* q, const qg_heads* k, const qg_heads* v,
+                          const qg_heads* o, const float* lse, const qg_heads* dq, const qg_heads* dk, const qg_heads* dv, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+typedef struct {
+    uint16_t *k, *v;                    /* [pages][page_size][heads][d] each, 16-byte aligned */
+    const int32_t* table;               /* [sequences][width] */
+    int64_t pages;
+    int page_size, heads, d, sequences, width;
+} qg_cache;
+int qg_cache_append(const qg_cache* c, const qg_heads* q, int heads_q, const qg_heads* k, const qg_heads* v, const int64_t* positions,
+                    const int32_t* sequence, int64_t tokens, const double* freqs, int rot, int layout, float amplitude,
+                    const qg_heads* q_out, void* stream);
+size_t qg_attention_paged_workspace_bytes(const qg_cache* c, int heads_q);
+int qg_attention_paged(const qg_cache* c, const int32_t* lengths, const qg_heads* q, int heads_q, float scale, float cap, int64_t window,
+                       const float* slopes, const qg_heads* o, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Adaptive lazy update policy (Sec. 3.2), HOST ONLY (p is a host pointer):
  * streak counts consecutive checks with cos >= threshold; at k in a row the
  * interval doubles and the streak restarts; next_refresh advances by the

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqgalore.so")
 SOURCES = ["qg_api.hip", "qg_quant.hip", "qg_adam.hip", "qg_gemm.hip", "qg_cossim.hip", "qg_diag.hip", "qg_refresh.hip", "qg_linear.hip", "qg_adam8.hip",
-           "qg_norm.hip", "qg_linear_act.hip", "qg_head.hip"]
+           "qg_norm.hip", "qg_linear_act.hip", "qg_head.hip", "qg_attention.hip", "qg_rope.hip", "qg_paged.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off",                                   # fused multiply-adds only where written

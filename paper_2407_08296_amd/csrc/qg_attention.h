@@ -1,0 +1,217 @@
+// What the attention kernels share: the geometry of packed sequences, tiles of keys or queries in LDS, scores and masks.
+//
+// Tokens are packed: sequence i has queries cu_q[i] .. cu_q[i + 1] - 1 and keys cu_k[i] .. cu_k[i + 1] - 1, and its queries are the last of
+// its keys: query i stands at position p = i + n_k - n_q.  For a query, the visible keys are an interval lo <= j <= hi:
+//     hi = n_k - 1, causal: min(that, max(p, prefix - 1));     lo = 0, with a window: p - window + 1
+// both growing with p, so that whole tiles are seen by all rows, by none, or need a test per score.
+//
+// Operand layouts (v_mfma_f32_32x32x16_bf16): an operand's lane l holds row or column l % 32 and 8 values of k; the accumulator's
+// register v of lane l is [8 (v / 4) + 4 (l / 32) + v % 4][l % 32].  Scores are computed with the index that the next product sums over as
+// their row: a lane then holds, for one column, the values of k that the next product wants in one operand, in an order of k of its own
+// (first 4 h .. 4 h + 3, then 8 + 4 h .. 8 + 4 h + 3 of each 16, h = l / 32), and the other operand is read in that order.
+// So probabilities never leave the registers.
+#pragma once
+#include "qg_common.h"
+#include "qg_gemm_kernels.h"
+
+namespace qg {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+constexpr int64_t kAttnMaxTokens = int64_t(1) << 24;
+constexpr int kAttnMaxHeads = 1024, kAttnMaxSequences = 1 << 20;
+constexpr int64_t kHeadsMaxStride = int64_t(1) << 23;   // elements between tokens: 64 rows are addressed in 31 bits from one base
+
+int check_heads(const qg_heads* x, bool required);      // host, qg_attention.hip
+int check_cache(const qg_cache* c);                     // host, qg_rope.hip
+
+struct AttnArgs {
+    int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs, do_ts, do_hs, dq_ts, dq_hs, dk_ts, dk_hs, dv_ts, dv_hs;   // strides, elements
+    const uint16_t *q, *k, *v, *dO;
+    uint16_t *o, *dq, *dk, *dv;
+    float* lse;          // [heads_q][tokens_q]
+    float* delta;        // ... rowsum(dO o)
+    const int32_t *cu_q, *cu_k, *prefix;
+    const float* slopes;
+    int tokens_q, tokens_k, heads_q, group, d, sequences, causal, window, tiles;
+    float scale, cap;
+};
+
+// One tile of a sequence's rows.
+struct AttnTile {
+    int seq;       // `sequences`: the rows behind the last sequence
+    int tile;      // of the sequence
+    int q0, nq, k0, nk;
+};
+
+// Boundary i of packed sequences, inside the tokens whatever memory holds.
+__device__ __forceinline__ int attn_boundary(const int32_t* cu, int i, int sequences, int tokens) {
+    if (i == 0) return 0;
+    if (cu == nullptr) return tokens;
+    return min(max(cu[min(i, sequences)], 0), tokens);
+}
+
+// Tile t of the rows in blocks of BM per sequence.  Sequence i's tiles are numbered from boundary_i / BM + i on: that leaves room for each
+// sequence's last, partial one without a sum over the sequences before it (a number too many has no rows).  The rows behind the
+// last sequence are one more.  64 boundaries are looked at at once; the first always counts, so each turn narrows the range.
+// KEYS: the rows are keys.  The rows behind the last sequence have no partners.
+template <int BM, bool KEYS>
+__device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, int t) {
+    const int32_t* rows = KEYS ? a.cu_k : a.cu_q;
+    const int tokens = KEYS ? a.tokens_k : a.tokens_q;
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = a.sequences + 1;
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const bool below = at < n && attn_boundary(rows, lo + at, a.sequences, tokens) / BM + lo + at <= t;
+        const int count = max(1, (int)__popcll(__ballot(below)));
+        lo += (count - 1) * step;
+        n = min(step, n - (count - 1) * step);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    AttnTile r;
+    r.seq = lo;
+    const int first = attn_boundary(rows, lo, a.sequences, tokens);
+    r.tile = t - (first / BM + lo);
+    const bool tail = lo >= a.sequences;
+    r.q0 = attn_boundary(a.cu_q, lo, a.sequences, a.tokens_q);
+    r.k0 = attn_boundary(a.cu_k, lo, a.sequences, a.tokens_k);
+    const int q1 = tail ? a.tokens_q : attn_boundary(a.cu_q, lo + 1, a.sequences, a.tokens_q);
+    const int k1 = tail ? a.tokens_k : attn_boundary(a.cu_k, lo + 1, a.sequences, a.tokens_k);
+    r.nq = tail && KEYS ? 0 : max(0, q1 - r.q0);
+    r.nk = tail && !KEYS ? 0 : max(0, k1 - r.k0);
+    return r;
+}
+
+// Workgroup id -> (head, tile of rows).  Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles of consecutive heads, so that the
+// keys and values of a head are read into one L2.
+__device__ __forceinline__ bool attn_place(int work, int tiles, int& head, int& tile) {
+    const int per = (work + 7) / 8, at = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if (at >= work) return false;
+    head = at / tiles;
+    tile = at - head * tiles;
+    return true;
+}
+
+// Rows of a [rows][d] bf16 array as an LDS tile of `ROWS` rows of pitch P (64 or 128 elements), by direct loads.  The 16-byte chunk c of row r
+// is kept in slot c ^ swizzle(r): reads of one chunk of 16 consecutive rows (an operand whose k is d) and transposing reads of four
+// chunks of four consecutive rows (an operand whose k is the row) each spread over all banks.  Rows from `valid` on and elements from
+// d on become zero.
+template <int P>
+__device__ __forceinline__ int tile_swizzle(int r) {
+    return P == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 1) << 2) | ((r >> 1) & 3);
+}
+
+template <int P, int ROWS, int NT>
+struct RowsTile {
+    static constexpr int CPR = P / 8, PER = ROWS * CPR / NT, STEP = NT / CPR;   // chunks per row, loads per thread, rows per load
+    static_assert(STEP % 16 == 0, "a thread's rows share their swizzle");
+    uint32_t off;      // of the thread's first chunk, from the tile's first row
+    int row;
+    bool in;           // the chunk lies below d
+    __device__ __forceinline__ void init(int64_t stride, int d) {
+        const int idx = threadIdx.x;
+        row = idx / CPR;
+        const int chunk = (idx % CPR) ^ tile_swizzle<P>(row);
+        in = chunk * 8 < d;
+        off = (uint32_t)(row * (int)stride + chunk * 8) * 2u;
+    }
+    // lds: the tile; rows from `base` on, `valid` of them (more than ROWS: all)
+    __device__ __forceinline__ void load(uint16_t* lds, const uint16_t* base, int64_t stride, int valid) const {
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(base);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const bool there = in && row + p * STEP < valid;
+            buffer_load_lds16(rs, lds + p * NT * 8 + wave * 512, there ? off + (uint32_t)(p * STEP) * (uint32_t)stride * 2u : 0x80000000u, 0);
+        }
+    }
+};
+
+// Operand of 32 rows of a tile with k = d: 16 elements from 16 * step on.
+template <int P>
+__device__ __forceinline__ bf16x8 tile_frag(const uint16_t* tile, int row0, int step, int lane) {
+    const int r = lane & 31;
+    const int slot = (2 * step + (lane >> 5)) ^ tile_swizzle<P>(r);
+    return *reinterpret_cast<const bf16x8*>(tile + (row0 + r) * P + slot * 8);
+}
+// Operand of 32 elements of d (from 32 * block on) with k = 16 rows of the tile from row0 on, in the order of k of a score's registers.
+template <int P>
+__device__ __forceinline__ bf16x8 tile_frag_t(const uint16_t* tile, int row0, int block, int lane) {
+    const int s = lane & 15, g = lane >> 4, r = 4 * (g >> 1) + (s >> 2);
+    const int chunk = block * 4 + 2 * (g & 1) + ((s & 3) >> 1);
+    const uint16_t* lo = tile + (row0 + r) * P + ((chunk ^ tile_swizzle<P>(r)) * 8) + 4 * (s & 1);
+    const uint16_t* hi = tile + (row0 + r + 8) * P + ((chunk ^ tile_swizzle<P>(r + 8)) * 8) + 4 * (s & 1);
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// The same k = d operand straight from memory: row `row` of `rows`, zero past the end and from d on.
+__device__ __forceinline__ bf16x8 row_frag(const uint16_t* base, int64_t stride, int row, int rows, int step, int d, int lane) {
+    const int c = 2 * step + (lane >> 5);
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (row < rows && c * 8 < d) w = *reinterpret_cast<const u32x4*>(base + (int64_t)row * stride + c * 8);
+    return __builtin_bit_cast(bf16x8, w);
+}
+
+// Registers 8 t .. 8 t + 7 of a score block as the operand of the next product's step t.  Rounded to bf16, an operand of the matrix unit.
+__device__ __forceinline__ bf16x8 score_frag(const f32x16& s, int t) {
+    const u32x4 w = {pack_bf16x2(s[8 * t], s[8 * t + 1]), pack_bf16x2(s[8 * t + 2], s[8 * t + 3]), pack_bf16x2(s[8 * t + 4], s[8 * t + 5]),
+                     pack_bf16x2(s[8 * t + 6], s[8 * t + 7])};
+    return __builtin_bit_cast(bf16x8, w);
+}
+
+__device__ __forceinline__ float other_half(float v) {   // of lane ^ 32
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? (uint32_t)s[0] : (uint32_t)s[1]);
+}
+
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) z[v] = 0.f;
+    return z;
+}
+
+// Index of accumulator register v's row within its block of 32.
+__device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v >> 2) + (v & 3); }
+
+// A score times log2(e): from the product s, c = scale log2(e) (capped: scale / cap, factor = 1 - tanh^2).
+template <bool CAP>
+__device__ __forceinline__ float score_log2(float s, float c, float cap_log2e, float& factor) {
+    if constexpr (!CAP) {
+        factor = 1.f;
+        return s * c;
+    } else {
+        // tanh y = 1 - 2 / (exp(2 y) + 1); exp overflows to infinity and 1 is left
+        const float e = __builtin_amdgcn_exp2f(s * (c * (2.f * kLog2e)));
+        const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
+        factor = __builtin_fmaf(-t, t, 1.f);
+        return cap_log2e * t;
+    }
+}
+
+// Columns of a transposed result (acc[b]: elements 32 b .. 32 b + 31 of a row of d, the row being this lane's column): 16-byte pieces.
+template <int NB>
+__device__ __forceinline__ void store_columns(const f32x16 (&acc)[NB], float factor, uint16_t* row, int d, bool mine, int lane) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            uint32_t x[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    x[i][e] = pack_bf16x2(acc[b][4 * (j + i) + 2 * e] * factor, acc[b][4 * (j + i) + 2 * e + 1] * factor);
+            // the halves of the wave hold 4 elements of each 8: after the exchange one has the first 8, the other the next
+            const auto lo = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+            const int at = 32 * b + 8 * (j + (lane >> 5));
+            const u32x4 w = {(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+            if (mine && at < d) *reinterpret_cast<u32x4*>(row + at) = w;
+        }
+}
+
+}  // namespace qg

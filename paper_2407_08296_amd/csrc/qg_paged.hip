@@ -1,0 +1,307 @@
+// Attention of one new token per sequence over a cache in pages: o = softmax_j(x_j) v_j over positions j = first .. length - 1.
+// The cache is read once, 4 d bytes per key head and position: HBM is the bound, and what counts is how many bytes are on their way.  The
+// query heads that share a key head are taken together, up to 16 as the columns of a 16 x 16 x 32 product (one alone leaves 15
+// columns empty: at 8 TB/s that is still 5 % of the matrix pipe).  A sequence is cut into parts of kPart positions for as many workgroups,
+// whose results are joined by a second kernel; a workgroup's waves take 32 positions each in turn, each with tiles, maximum and sums of
+// its own, so that nothing waits for another wave before the end.
+//   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
+// transposed.  Scores are [position][head]; register i of block b is position 16 b + 4 (l / 16) + i, the order in which V is read then.
+#include "qg_attention.h"
+
+namespace qg {
+
+constexpr int kPart = 512;                  // positions of a workgroup
+constexpr int kPagedStep = 32;              // ... of a wave at a time
+
+struct PagedArgs {
+    const uint16_t *q, *k, *v;
+    uint16_t* o;
+    const int32_t *table, *lengths;
+    const float* slopes;
+    float* part;                            // [sequences][heads_q][parts][d + 2]: sums, maximum (log2), sum
+    int64_t q_ts, q_hs, o_ts, o_hs, pages;
+    int page_size, heads_k, group, d, sequences, width, parts, window;
+    float scale, cap;
+};
+
+// Visible positions of a sequence.
+__device__ __forceinline__ void paged_range(const PagedArgs& a, int seq, int& first, int& end) {
+    end = (int)min((int64_t)max(a.lengths[seq], 0), (int64_t)a.width * a.page_size);
+    first = a.window > 0 ? max(0, end - a.window) : 0;
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
+    constexpr int P = D <= 64 ? 64 : 128, NB = D / 16, NS = D / 32, CPR = P / 8, LOADS = kPagedStep * CPR / 64, PER = 64 / CPR;
+    constexpr int TILE = kPagedStep * P;
+    // V tiles, two per wave; at the end the waves' results, 16 rows of D (and a pad) and their maxima and sums
+    constexpr int ROW = D + 4;
+    static_assert(4 * 16 * ROW * 4 + 4 * 32 * 4 <= 4 * 2 * TILE * 2, "the results fit where the tiles were");
+    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * 2 * TILE];
+    const int part = blockIdx.x % a.parts, unit = blockIdx.x / a.parts;
+    const int groups = (a.group + 15) / 16;
+    const int hg = unit % groups, kv = unit / groups % a.heads_k, seq = unit / groups / a.heads_k;
+    int first, end;
+    paged_range(a, seq, first, end);
+    const int whole_first = first / kPagedStep * kPagedStep;     // parts begin at whole steps
+    const int begin = whole_first + part * kPart, stop = min(end, begin + kPart);
+    if (part > 0 && begin >= end) return;                        // (part 0 of an empty sequence still writes its zeros)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int head = kv * a.group + hg * 16 + col;
+    const bool has_head = hg * 16 + col < a.group;
+    const int64_t row = (int64_t)a.heads_k * a.d;
+    const uint16_t *kp = a.k + (int64_t)kv * a.d, *vp = a.v + (int64_t)kv * a.d;
+    const int32_t* pages = a.table + (int64_t)seq * a.width;
+
+    bf16x8 qf[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int c = 4 * s + g;
+        u32x4 w = {0u, 0u, 0u, 0u};
+        if (has_head && c * 8 < a.d) w = *reinterpret_cast<const u32x4*>(a.q + (int64_t)seq * a.q_ts + (int64_t)head * a.q_hs + c * 8);
+        qf[s] = __builtin_bit_cast(bf16x8, w);
+    }
+    const float c2 = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float slope = BIAS && has_head ? a.slopes[head] * kLog2e : 0.f;
+
+    // row of the cache that the wave's step holds at position lane % 32, -1: none (hidden, past the end, or without a page)
+    auto slot_of = [&](int j0) {
+        const int j = j0 + (lane & 31);
+        if (j < first || j >= stop) return -1;
+        const int at = (int)((uint32_t)j / (uint32_t)a.page_size), page = pages[at];
+        return page < 0 || page >= a.pages ? -1 : page * a.page_size + (j - at * a.page_size);
+    };
+    uint16_t* const tiles = smem + wave * 2 * TILE;
+    bf16x8 kf[2][2][NS];
+    auto fetch = [&](int slot, int stage, bf16x8 (&to)[2][NS]) {
+#pragma unroll
+        for (int p = 0; p < LOADS; ++p) {
+            const int r = p * PER + lane / CPR, chunk = (lane % CPR) ^ tile_swizzle<P>(r);
+            const int from = max(0, __shfl(slot, r, 64));
+            const uint16_t* src = vp + (int64_t)from * row + (chunk * 8 < a.d ? chunk * 8 : 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(tiles + stage * TILE + p * 512), 16, 0, 0);
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int from = max(0, __shfl(slot, 16 * b + col, 64));
+            const uint16_t* src = kp + (int64_t)from * row;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int c = 4 * s + g;
+                u32x4 w = *reinterpret_cast<const u32x4*>(src + (c * 8 < a.d ? c * 8 : 0));
+                to[b][s] = __builtin_bit_cast(bf16x8, w);
+            }
+        }
+    };
+    f32x4 o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    auto compute = [&](int j0, uint32_t there, int stage, const bf16x8 (&kk)[2][NS]) {
+        uint16_t* V = tiles + stage * TILE;
+        if (there != 0xFFFFFFFFu) {          // rows without a position: zero, whatever was read
+#pragma unroll
+            for (int p = 0; p < LOADS; ++p) {
+                const int r = p * PER + lane / CPR;
+                if (!(there >> r & 1)) *reinterpret_cast<u32x4*>(V + p * 512 + lane * 8) = u32x4{0u, 0u, 0u, 0u};
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        f32x4 s[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[b][k], qf[k], s[b], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float unused, x = score_log2<CAP>(s[b][i], c2, cap2, unused);
+                const int r = 16 * b + 4 * g + i;
+                if constexpr (BIAS) x = __builtin_fmaf(-slope, (float)(end - 1 - (j0 + r)), x);
+                s[b][i] = there >> r & 1 ? x : -INFINITY;
+                top = fmaxf(top, s[b][i]);
+            }
+        }
+        if (__ballot(top > m + 8.f) != 0) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float raised = fmaxf(m, top);
+            const float keep = raised == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - raised);
+            m = raised;
+            l *= keep;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b] *= keep;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - ref);
+                l += s[b][i];
+            }
+        const u32x4 pw = {pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])};
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+        const int r = 4 * g + (col >> 2);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int chunk = 2 * b + ((col & 3) >> 1);
+            const uint16_t* lo = V + r * P + ((chunk ^ tile_swizzle<P>(r)) * 8) + 4 * (col & 1);
+            const uint16_t* hi = V + (r + 16) * P + ((chunk ^ tile_swizzle<P>(r + 16)) * 8) + 4 * (col & 1);
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[b], 0, 0, 0);
+        }
+    };
+    // the wave's own LDS accesses and direct loads complete in order once waited for; the scheduler does not see the transposing reads as accesses
+    auto fence = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int j0 = begin + wave * kPagedStep, by = 4 * kPagedStep;
+    const int steps = j0 < stop ? (stop - j0 + by - 1) / by : 0;
+    int slot = steps > 0 ? slot_of(j0) : -1, next = steps > 1 ? slot_of(j0 + by) : -1;
+    if (steps > 0) fetch(slot, 0, kf[0]);
+    for (int i = 0; i < steps; i += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (i + u < steps) {
+                const uint32_t there = (uint32_t)__ballot(slot >= 0);
+                fence();
+                if (i + u + 1 < steps) {
+                    fetch(next, 1 - u, kf[1 - u]);
+                    slot = next;
+                    next = i + u + 2 < steps ? slot_of(j0 + (i + u + 2) * by) : -1;
+                }
+                compute(j0 + (i + u) * by, there, u, kf[u]);
+            }
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    // join the waves: columns of heads, in a fixed order
+    lds_barrier();
+    float* sums = reinterpret_cast<float*>(smem);                // [wave][16][ROW]
+    float* stat = sums + 4 * 16 * ROW;                           // [wave][16][2]
+#pragma unroll
+    for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(sums + (wave * 16 + col) * ROW + 16 * b + 4 * g) = o[b];
+    if (g == 0) {
+        stat[(wave * 16 + col) * 2] = m;
+        stat[(wave * 16 + col) * 2 + 1] = l;
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < 16 * (D / 4); idx += 256) {
+        const int q = idx / (D / 4), e = idx % (D / 4) * 4;
+        if (hg * 16 + q >= a.group || e >= a.d) continue;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[(w * 16 + q) * 2]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(stat[(w * 16 + q) * 2] - ref);
+            sum = __builtin_fmaf(stat[(w * 16 + q) * 2 + 1], f, sum);
+            x += *reinterpret_cast<const f32x4*>(sums + (w * 16 + q) * ROW + e) * f;
+        }
+        const int h = kv * a.group + hg * 16 + q;
+        if (a.parts == 1) {
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
+            uint32_t* to = reinterpret_cast<uint32_t*>(a.o + (int64_t)seq * a.o_ts + (int64_t)h * a.o_hs + e);
+            to[0] = pack_bf16x2(x[0] * f, x[1] * f);
+            to[1] = pack_bf16x2(x[2] * f, x[3] * f);
+        } else {
+            float* to = a.part + (((int64_t)seq * a.heads_k * a.group + h) * a.parts + part) * (a.d + 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[e + i] = x[i];
+            if (e == 0) {
+                to[a.d] = top;
+                to[a.d + 1] = sum;
+            }
+        }
+    }
+}
+
+// Joins the parts of a sequence's heads, in their order: a wave per head, two elements per lane.
+__global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
+    const int heads = a.heads_k * a.group;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= (int64_t)a.sequences * heads) return;
+    const int seq = (int)(unit / heads), h = (int)(unit - (int64_t)seq * heads), lane = threadIdx.x & 63;
+    int first, end;
+    paged_range(a, seq, first, end);
+    const int parts = max(1, (end - first / kPagedStep * kPagedStep + kPart - 1) / kPart);
+    const float* from = a.part + unit * a.parts * (a.d + 2);
+    const int e = 2 * lane, at = min(e, a.d - 2);
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, from[(int64_t)p * (a.d + 2) + a.d]);
+    top = wave_max(top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float x = 0.f, y = 0.f, sum = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float* one = from + (int64_t)p * (a.d + 2);
+        const float f = __builtin_amdgcn_exp2f(one[a.d] - ref);
+        sum = __builtin_fmaf(one[a.d + 1], f, sum);
+        x = __builtin_fmaf(one[at], f, x);
+        y = __builtin_fmaf(one[at + 1], f, y);
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    if (e < a.d) *reinterpret_cast<uint32_t*>(a.o + (int64_t)seq * a.o_ts + (int64_t)h * a.o_hs + e) = pack_bf16x2(x * f, y * f);
+}
+
+static int64_t paged_parts(const qg_cache* c) { return ((int64_t)c->width * c->page_size + kPagedStep - 1 + kPart - 1) / kPart; }
+
+static int check_paged(const qg_cache* c, int heads_q) {
+    if (int e = check_cache(c)) return e;
+    if (c->d > 128 || heads_q <= 0 || heads_q > kAttnMaxHeads || heads_q % c->heads != 0) return QG_ERR_SHAPE;
+    const int64_t groups = (heads_q / c->heads + 15) / 16;
+    if (paged_parts(c) * c->sequences * c->heads * groups >= (int64_t(1) << 24)) return QG_ERR_SHAPE;   // (2^32 threads in a launch)
+    return QG_OK;
+}
+
+}  // namespace qg
+
+using namespace qg;
+
+extern "C" size_t qg_attention_paged_workspace_bytes(const qg_cache* c, int heads_q) {
+    if (check_paged(c, heads_q) != QG_OK) return 0;
+    return ((size_t)paged_parts(c) * c->sequences * heads_q * (c->d + 2) * 4 + 15) / 16 * 16;
+}
+
+extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, const qg_heads* q, int heads_q, float scale, float cap, int64_t window,
+                                  const float* slopes, const qg_heads* o, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int e = check_paged(c, heads_q)) return e;
+    if (lengths == nullptr) return QG_ERR_NULL;
+    for (const qg_heads* x : {q, o})
+        if (int e = check_heads(x, true)) return e;
+    if (!(scale > 0.f && scale < INFINITY) || !(cap >= 0.f && cap < INFINITY) || window < 0) return QG_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(lengths) & 3) || (reinterpret_cast<uintptr_t>(slopes) & 3) || !aligned16(workspace)) return QG_ERR_ALIGN;
+    if (workspace == nullptr || workspace_bytes < qg_attention_paged_workspace_bytes(c, heads_q)) return QG_ERR_WORKSPACE;
+    PagedArgs a = {};
+    a.q = q->data, a.q_ts = q->token_stride, a.q_hs = q->head_stride;
+    a.o = o->data, a.o_ts = o->token_stride, a.o_hs = o->head_stride;
+    a.k = c->k, a.v = c->v, a.table = c->table, a.lengths = lengths, a.slopes = slopes, a.part = static_cast<float*>(workspace);
+    a.pages = c->pages, a.page_size = c->page_size, a.heads_k = c->heads, a.group = heads_q / c->heads, a.d = c->d;
+    a.sequences = c->sequences, a.width = c->width, a.parts = (int)paged_parts(c);
+    a.window = (int)(window < (int64_t(1) << 31) ? window : 0);
+    a.scale = scale, a.cap = cap;
+    const unsigned grid = (unsigned)((int64_t)a.parts * a.sequences * a.heads_k * ((a.group + 15) / 16));
+    auto launch = [&](auto d, auto cp, auto bias) {
+        hipLaunchKernelGGL((k_attention_paged<d.value, cp.value, bias.value>), dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
+    };
+    auto with_d = [&](auto cp, auto bias) {
+        if (a.d <= 64) launch(std::integral_constant<int, 64>(), cp, bias);
+        else launch(std::integral_constant<int, 128>(), cp, bias);
+    };
+    auto with_bias = [&](auto cp) { slopes != nullptr ? with_d(cp, std::true_type()) : with_d(cp, std::false_type()); };
+    cap > 0.f ? with_bias(std::true_type()) : with_bias(std::false_type());
+    if (a.parts > 1)
+        hipLaunchKernelGGL(k_attention_join, dim3((unsigned)(((int64_t)a.sequences * heads_q + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
+    return check_launch();
+}

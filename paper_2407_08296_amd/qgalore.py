@@ -37,6 +37,8 @@ EXPORTS = [
     "qg_residual_norm_forward", "qg_residual_norm_workspace_bytes", "qg_residual_norm_backward",
     "qg_int8_linear_act_forward", "qg_int8_linear_act_workspace_bytes", "qg_int8_linear_act_backward", "qg_int8_gated_forward",
     "qg_int8_gated_backward", "qg_int8_gated_workspace_bytes", "qg_head_loss_workspace_bytes", "qg_head_loss_forward", "qg_head_loss_backward",
+    "qg_rope_frequencies", "qg_rope_forward", "qg_rope_backward", "qg_attention_workspace_bytes", "qg_attention_forward",
+    "qg_attention_backward", "qg_cache_append", "qg_attention_paged_workspace_bytes", "qg_attention_paged",
 ]
 
 
@@ -64,6 +66,21 @@ class MatrixDesc(C.Structure):
 class RefreshDesc(C.Structure):
     _fields_ = [("Pq", C.c_void_p), ("Ps", C.c_void_p), ("G", C.c_void_p), ("Pq_new", C.c_void_p),
                 ("Ps_new", C.c_void_p)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("tokens_q", C.c_int64), ("tokens_k", C.c_int64), ("heads_q", C.c_int), ("heads_k", C.c_int), ("d", C.c_int),
+                ("sequences", C.c_int), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p), ("prefix", C.c_void_p), ("slopes", C.c_void_p),
+                ("scale", C.c_float), ("cap", C.c_float), ("causal", C.c_int), ("window", C.c_int64)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("pages", C.c_int64), ("page_size", C.c_int), ("heads", C.c_int),
+                ("d", C.c_int), ("sequences", C.c_int), ("width", C.c_int)]
 
 
 _lib = None
@@ -159,6 +176,18 @@ def lib() -> C.CDLL:
         L.qg_head_loss_workspace_bytes.argtypes = [i64, i64, i64]
         L.qg_head_loss_forward.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
         L.qg_head_loss_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
+        heads, attention, cache, f64 = C.POINTER(Heads), C.POINTER(Attention), C.POINTER(Cache), C.c_double
+        L.qg_rope_frequencies.argtypes = [i32, f64, f64, f64, f64, f64, vp]
+        L.qg_rope_forward.argtypes = [heads, i32, heads, i32, vp, vp, i64, i32, i32, i32, f32, heads, heads, vp]
+        L.qg_rope_backward.argtypes = L.qg_rope_forward.argtypes
+        L.qg_attention_workspace_bytes.restype = sz
+        L.qg_attention_workspace_bytes.argtypes = [attention]
+        L.qg_attention_forward.argtypes = [attention, heads, heads, heads, heads, vp, vp, sz, vp]
+        L.qg_attention_backward.argtypes = [attention] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
+        L.qg_cache_append.argtypes = [cache, heads, i32, heads, heads, vp, vp, i64, vp, i32, i32, f32, heads, vp]
+        L.qg_attention_paged_workspace_bytes.restype = sz
+        L.qg_attention_paged_workspace_bytes.argtypes = [cache, i32]
+        L.qg_attention_paged.argtypes = [cache, vp, heads, i32, f32, f32, i64, vp, heads, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -743,6 +772,182 @@ def head_loss_backward(x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, l
     _check(lib().qg_head_loss_backward(_ptr(x, _BF16), _ptr(W, _BF16), _ptr(labels, (torch.int64,)), _ptr(lse, _F32), _ptr(dloss, _F32),
                                        tokens, h, vocab, h, _ptr(dx), _ptr(dW), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
     return dx, dW
+
+
+# ---------------------------------------------------------------- attention half of a decoder layer
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+_I32, _I64, _F64 = (torch.int32,), (torch.int64,), (torch.float64,)
+
+
+def _heads(t: torch.Tensor | None):
+    """A [tokens][heads][d] tensor of any token and head stride (a slice of a linear layer's output, heads outside)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise QGError("device tensor expected")
+    if t.dim() != 3:
+        raise QGError(f"shape {tuple(t.shape)}, expected [tokens][heads][d]")
+    if t.dtype not in _BF16:
+        raise QGError(f"dtype {t.dtype} not in {_BF16}")
+    ts, hs, es = t.stride()
+    if es != 1 and t.shape[2] != 1:
+        raise QGError("elements of a head are expected next to each other")
+    return C.byref(Heads(t.data_ptr(), ts, hs))
+
+
+def _written(t: torch.Tensor | None, like: torch.Tensor, what: str) -> torch.Tensor:
+    """Where an output of like's shape goes: t, or a new tensor.  An expanded tensor has no place for every element."""
+    if t is None:
+        return like.new_empty(like.shape)
+    _expect(t, *like.shape)
+    if any(st == 0 and n > 1 for st, n in zip(t.stride(), t.shape)):
+        raise QGError(f"{what}: an expanded tensor cannot be written")
+    return t
+
+
+def _rope_layout(layout: str) -> int:
+    if layout not in ROPE_LAYOUTS:
+        raise QGError(f"layout {layout!r} not in {tuple(ROPE_LAYOUTS)}")
+    return ROPE_LAYOUTS[layout]
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, context: float = 0, low: float = 1.0, high: float = 4.0,
+                     device="cuda") -> torch.Tensor:
+    """The rot/2 frequencies of rotary positions, float64 on `device`: base^(-2i/rot), with a factor stretched to longer contexts."""
+    out = torch.empty(max(rot // 2, 1), dtype=torch.float64)
+    _check(lib().qg_rope_frequencies(rot, base, factor, context, low, high, out.data_ptr()))
+    return out.to(device)
+
+
+def _rope(f, q, k, positions, freqs, layout, amplitude, out):
+    tokens, heads_q, d = q.shape
+    rot = 2 * freqs.shape[0]
+    if k is not None:
+        _expect(k, tokens, k.shape[1], d)
+    _expect(positions, tokens)
+    _expect(freqs, rot // 2)
+    q_out = _written(None if out is None else out[0], q, "out")
+    k_out = None if k is None else _written(None if out is None else out[1], k, "out")
+    _check(f(_heads(q), heads_q, _heads(k), 0 if k is None else k.shape[1], _ptr(positions, _I64), _ptr(freqs, _F64), tokens, d, rot,
+             _rope_layout(layout), amplitude, _heads(q_out), _heads(k_out), _stream()))
+    return q_out, k_out
+
+
+def rope_forward(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half",
+                 amplitude: float = 1.0, out=None):
+    """Returns (q', k'): the first 2 * len(freqs) elements of every head of q [tokens][heads][d] and k (None: only q) turned by
+    positions[token] * freqs.  positions int64, freqs float64.  out: (q', k') to write into; the inputs themselves: in place."""
+    return _rope(lib().qg_rope_forward, q, k, positions, freqs, layout, amplitude, out)
+
+
+def rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half",
+                  amplitude: float = 1.0, out=None):
+    """Returns (dq, dk) of rope_forward, from the gradients of its outputs."""
+    return _rope(lib().qg_rope_backward, dq_out, dk_out, positions, freqs, layout, amplitude, out)
+
+
+def _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix) -> Attention:
+    tokens, heads, d = q.shape
+    tokens_k, heads_k, _ = k.shape
+    _expect(k, tokens_k, heads_k, d)
+    _expect(v, tokens_k, heads_k, d)
+    sequences = 1 if cu_q is None else cu_q.numel() - 1
+    _expect(cu_q, sequences + 1)
+    _expect(cu_k, sequences + 1)
+    _expect(prefix, sequences)
+    _expect(slopes, heads)
+    return Attention(tokens, tokens_k, heads, heads_k, d, sequences, _ptr(cu_q, _I32), _ptr(cu_k, _I32), _ptr(prefix, _I32),
+                     _ptr(slopes, _F32), d ** -0.5 if scale is None else scale, cap, int(causal), window)
+
+
+def _workspace(nbytes: int, like: torch.Tensor, given: torch.Tensor | None) -> torch.Tensor:
+    if given is not None:
+        return given
+    if nbytes == 0:
+        raise QGError("libqgalore: shape out of range")
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor | None = None, cu_k: torch.Tensor | None = None,
+                      causal: bool = True, scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
+                      window: int = 0, prefix: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None):
+    """Returns (o, lse): attention of q [tokens][heads][d] over k and v [tokens_k][heads_k][d], o bf16 [tokens][heads][d], lse fp32
+    [heads][tokens].  cu_q, cu_k: int32 [sequences + 1], boundaries of packed sequences (None: one sequence; cu_k None: as cu_q).
+    scale: d^-0.5 if None; cap, slopes (fp32 [heads]), window, prefix (int32 [sequences]): as in qg_attention_forward."""
+    a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
+    o = _written(out, q, "out")
+    lse = torch.empty(a.heads_q, a.tokens_q, dtype=torch.float32, device=q.device)
+    ws = _workspace(lib().qg_attention_workspace_bytes(C.byref(a)), q, workspace)
+    _check(lib().qg_attention_forward(C.byref(a), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), _ptr(ws, (torch.uint8,)), ws.numel(),
+                                      _stream()))
+    return o, lse
+
+
+def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       cu_q: torch.Tensor | None = None, cu_k: torch.Tensor | None = None, causal: bool = True,
+                       scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0,
+                       prefix: torch.Tensor | None = None, out=None, workspace: torch.Tensor | None = None):
+    """Returns (dq, dk, dv) of attention_forward, from its inputs and results and do, the gradient of o.  out: (dq, dk, dv) to write into
+    (slices of one gradient of the layer that gave q, k and v, say)."""
+    a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
+    for t in (do, o):
+        _expect(t, *q.shape)
+    _expect(lse, a.heads_q, a.tokens_q)
+    dq, dk, dv = (_written(None if out is None else out[i], t, "out") for i, t in enumerate((q, k, v)))
+    ws = _workspace(lib().qg_attention_workspace_bytes(C.byref(a)), q, workspace)
+    _check(lib().qg_attention_backward(C.byref(a), _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse, _F32), _heads(dq),
+                                       _heads(dk), _heads(dv), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+    return dq, dk, dv
+
+
+def _cache(k_pages, v_pages, table) -> Cache:
+    pages, page_size, heads, d = k_pages.shape
+    _expect(v_pages, pages, page_size, heads, d)
+    sequences, width = table.shape
+    return Cache(_ptr(k_pages, _BF16), _ptr(v_pages, _BF16), _ptr(table, _I32), pages, page_size, heads, d, sequences, width)
+
+
+def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, k_pages: torch.Tensor,
+                 v_pages: torch.Tensor, table: torch.Tensor, sequence: torch.Tensor | None = None, freqs: torch.Tensor | None = None,
+                 layout: str = "half", amplitude: float = 1.0, out: torch.Tensor | None = None):
+    """Puts k and v [tokens][heads_k][d] of new tokens into the pages [pages][page_size][heads_k][d] of a cache: token t to
+    position positions[t] (int64) of sequence[t] (int32; None: t), whose pages table[sequence] (int32 [sequences][width]) lists.  k is turned on its
+    way if freqs is given, and so is q, which is returned (None without q).  out: where q goes (q itself: in place)."""
+    c = _cache(k_pages, v_pages, table)
+    tokens = k.shape[0]
+    _expect(k, tokens, c.heads, c.d)
+    _expect(v, tokens, c.heads, c.d)
+    _expect(positions, tokens)
+    _expect(sequence, tokens)
+    rot = 0
+    if freqs is not None:
+        rot = 2 * freqs.shape[0]
+        _expect(freqs, rot // 2)
+    q_out = None
+    if q is not None:
+        _expect(q, tokens, q.shape[1], c.d)
+        q_out = _written(out, q, "out")
+    _check(lib().qg_cache_append(C.byref(c), _heads(q), 0 if q is None else q.shape[1], _heads(k), _heads(v), _ptr(positions, _I64),
+                                 _ptr(sequence, _I32), tokens, _ptr(freqs, _F64), rot, _rope_layout(layout), amplitude, _heads(q_out), _stream()))
+    return q_out
+
+
+def attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                    scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0,
+                    out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of one new token per sequence, q [sequences][heads][d], over the first lengths[s] (int32) positions of its pages; the token is
+    the last of them.  Returns o [sequences][heads][d].  workspace: uint8, qg_attention_paged_workspace_bytes of them (allocated if None)."""
+    c = _cache(k_pages, v_pages, table)
+    heads = q.shape[1]
+    _expect(q, c.sequences, heads, c.d)
+    _expect(lengths, c.sequences)
+    _expect(slopes, heads)
+    o = _written(out, q, "out")
+    ws = _workspace(lib().qg_attention_paged_workspace_bytes(C.byref(c), heads), q, workspace)
+    _check(lib().qg_attention_paged(C.byref(c), _ptr(lengths, _I32), _heads(q), heads, c.d ** -0.5 if scale is None else scale, cap, window,
+                                    _ptr(slopes, _F32), _heads(o), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+    return o
 
 
 # ---------------------------------------------------------------- subspace refresh
