@@ -447,10 +447,12 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  *   h / (heads_q / heads_k).  lse: fp32 [heads_q][tokens_q], may be NULL.  A query without a visible key, and tokens behind
  *   the last sequence: o = 0, lse = -inf.  Those tokens' q, k and v are not read; inside a sequence a value that is not finite can
  *   reach every query of its sequence.
- * qg_attention_backward: dq, dk, dv from do, the forward pass's inputs and its o and lse (as stored: delta = sum do o).  Sums of the heads that
+ * qg_attention_backward: dq, dk, dv from do, the forward pass's inputs and its o and lse (delta = sum do o from o as
+ *   stored, corrected by what the sum of the scores' gradients over a row, which is 0, then comes to).  Sums of the heads that
  *   share k and v, and over tokens, are added in a fixed order.  Slopes have no gradient.
  *   d: a multiple of 8 up to 128.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
- *   workspace: qg_attention_workspace_bytes(a) bytes, 16-byte aligned, for either call.
+ *   workspace: qg_attention_forward_workspace_bytes(a) or qg_attention_backward_workspace_bytes(a) bytes, 16-byte aligned; NULL where that is 0;
+ *   calls that may run at the same time need one each.
  *
  * qg_cache: keys and values of `sequences` sequences in pages: position p of sequence s is row p % page_size of page
  *   table[s][p / page_size].  An entry outside [0, pages) has no page: nothing is written there, and its keys are not visible.
@@ -483,7 +485,8 @@ typedef struct {
     int causal;
     int64_t window;
 } qg_attention;
-size_t qg_attention_workspace_bytes(const qg_attention* a);
+size_t qg_attention_forward_workspace_bytes(const qg_attention* a);
+size_t qg_attention_backward_workspace_bytes(const qg_attention* a);
 int qg_attention_forward(const qg_attention* a, const qg_heads* q, const qg_heads* k, const qg_heads* v, const qg_heads* o, float* lse,
                          void* workspace, size_t workspace_bytes, void* stream);
 int qg_attention_backward(const qg_attention* a, const qg_heads* dO, const qg_heads* q, const qg_heads* k, const qg_heads* v,

@@ -33,7 +33,8 @@ struct AttnArgs {
     float* delta;        // ... rowsum(dO o)
     const int32_t *cu_q, *cu_k, *prefix;
     const float* slopes;
-    int tokens_q, tokens_k, heads_q, group, d, sequences, causal, window, tiles;
+    float* part;         // sums of parts, to be joined (see qg_attention.hip)
+    int tokens_q, tokens_k, heads_q, group, d, sequences, causal, window, tiles, parts;
     float scale, cap;
 };
 
@@ -83,13 +84,15 @@ __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, int t) {
     return r;
 }
 
-// Workgroup id -> (head, tile of rows).  Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles of consecutive heads, so that the
-// keys and values of a head are read into one L2.
-__device__ __forceinline__ bool attn_place(int work, int tiles, int& head, int& tile) {
-    const int per = (work + 7) / 8, at = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+// Workgroup id -> (head, tile of rows, part of what passes by).  Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles of
+// consecutive heads, so that the keys and values of a head are read into one L2.
+__device__ __forceinline__ bool attn_place(int heads, int tiles, int parts, int& head, int& tile, int& part) {
+    const int work = heads * tiles * parts, per = (work + 7) / 8, at = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (at >= work) return false;
-    head = at / tiles;
-    tile = at - head * tiles;
+    const int rest = at / parts;
+    part = at - rest * parts;
+    head = rest / tiles;
+    tile = rest - head * tiles;
     return true;
 }
 
@@ -211,6 +214,19 @@ __device__ __forceinline__ void store_columns(const f32x16 (&acc)[NB], float fac
             const int at = 32 * b + 8 * (j + (lane >> 5));
             const u32x4 w = {(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
             if (mine && at < d) *reinterpret_cast<u32x4*>(row + at) = w;
+        }
+}
+
+// The same as a part's sums: fp32, elements from row on.
+template <int NB>
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[NB], float* row, int d, bool mine, int lane) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = 32 * b + 8 * j + 4 * (lane >> 5);
+            const f32x4 x = {acc[b][4 * j], acc[b][4 * j + 1], acc[b][4 * j + 2], acc[b][4 * j + 3]};
+            if (mine && at < d) *reinterpret_cast<f32x4*>(row + at) = x;
         }
 }
 

@@ -17,6 +17,8 @@ constexpr int kAttnStep = 64;      // rows that pass by, per step
 
 template <int D>
 constexpr int attn_pitch() { return D <= 64 ? 64 : 128; }
+template <int D>
+constexpr int attn_back_step() { return D <= 64 ? 64 : 32; }
 
 // What the scores of a query (or of a key's queries) need.
 struct ScoreRule {
@@ -49,8 +51,8 @@ template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16;
     __shared__ __attribute__((aligned(16))) uint16_t smem[4 * kAttnStep * P];
-    int head, t;
-    if (!attn_place(a.heads_q * a.tiles, a.tiles, head, t)) return;
+    int head, t, part;
+    if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, false>(a, a.tiles - 1 - t);   // late tiles first: with a causal mask they have most keys
     const int row0 = seq.tile * kAttnRows;
     if (row0 >= seq.nq) return;
@@ -67,9 +69,10 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = row_frag(qp, a.q_ts, i, seq.nq, s, a.d, lane);
     const int lo = see.lo(i), hi = see.hi(i);
-    // steps that some row of the workgroup sees, and, of the wave, those that all rows see whole
-    const int first = see.lo(row0) / kAttnStep, last = see.hi(min(row0 + kAttnRows, seq.nq) - 1) / kAttnStep;
-    const int steps = see.hi(min(row0 + kAttnRows, seq.nq) - 1) < 0 ? 0 : last - first + 1;
+    // steps that some row of the workgroup sees, of them the part's; and, of the wave, those that all rows see whole
+    const int first = see.lo(row0) / kAttnStep, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
+    const int all = most < 0 ? 0 : most / kAttnStep - first + 1;
+    const int begin = (int)((int64_t)all * part / a.parts), steps = (int)((int64_t)all * (part + 1) / a.parts);
     const int wave_lo = see.lo(w0), wave_hi = w0 < seq.nq ? see.hi(w1) : -1, all_lo = see.lo(w1), all_hi = see.hi(w0);
 
     f32x16 o[NB];
@@ -85,8 +88,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
         kt.load(smem + stage * 2 * kAttnStep * P, kp + (int64_t)j * a.k_ts, a.k_ts, seq.nk - j);
         vt.load(smem + (stage * 2 + 1) * kAttnStep * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
     };
-    const float pos = (float)(i + see.shift);
-    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, auto masked) {
+    const float pos = (float)(i + see.shift - 4 * h);     // from the register's key without its 4 h
+    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, bool masked) {
         f32x16 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -94,21 +97,31 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
 #pragma unroll
             for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(K, 32 * b, k, lane), qf[k], s[b], 0, 0, 0);
         }
-        constexpr bool kScaled = CAP || BIAS;     // s already holds x log2(e)
+        constexpr bool kScaled = CAP || BIAS;     // s holds x log2(e) then
         float top = -INFINITY;
+        if constexpr (kScaled) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    float unused;
+                    s[b][v] = score_log2<CAP>(s[b][v], rule.c, rule.cap_log2e, unused);
+                    if constexpr (BIAS) s[b][v] = __builtin_fmaf(-rule.slope, fabsf(pos - (float)(j0 + 32 * b + acc_row(v))), s[b][v]);
+                }
+        }
+        if (masked) {     // (a branch around the selects alone: with a masked and a plain body the registers of both spill)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int j = j0 + 32 * b + acc_row(v) + 4 * h;
+                    s[b][v] = j >= lo && j <= hi ? s[b][v] : -INFINITY;
+                }
+        }
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int j = j0 + 32 * b + acc_row(v) + 4 * h;
-                if constexpr (kScaled) {
-                    float unused;
-                    s[b][v] = score_log2<CAP>(s[b][v], rule.c, rule.cap_log2e, unused);
-                    if constexpr (BIAS) s[b][v] = __builtin_fmaf(-rule.slope, fabsf(pos - (float)j), s[b][v]);
-                }
-                if constexpr (decltype(masked)::value) s[b][v] = j >= lo && j <= hi ? s[b][v] : -INFINITY;
-                top = fmaxf(top, s[b][v]);
-            }
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, s[b][v]);
         top = fmaxf(top, other_half(top));
         if constexpr (!kScaled) top *= rule.c;
         // any reference near the maximum serves: it is raised only when the terms would pass 2^8 (the accumulators are rescaled then)
@@ -142,37 +155,67 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
             }
     };
 
-    if (steps > 0) fetch(0, 0);
-    for (int step = 0; step < steps; ++step) {
+    if (steps > begin) fetch(begin, begin & 1);
+    for (int step = begin; step < steps; ++step) {
         wait_loads<0>();
         lds_barrier();
         if (step + 1 < steps) fetch(step + 1, (step + 1) & 1);
         const int j0 = (first + step) * kAttnStep;
         const uint16_t *K = smem + (step & 1) * 2 * kAttnStep * P, *V = K + kAttnStep * P;
         if (j0 > wave_hi || j0 + kAttnStep <= wave_lo) continue;
-        if (j0 >= all_lo && j0 + kAttnStep - 1 <= all_hi) compute(j0, K, V, std::false_type());
-        else compute(j0, K, V, std::true_type());
+        compute(j0, K, V, j0 < all_lo || j0 + kAttnStep - 1 > all_hi);
     }
     l += other_half(l);
     const bool mine = i < seq.nq;
+    if (a.parts > 1) {
+        const int64_t row = ((int64_t)part * a.heads_q + head) * a.tokens_q + seq.q0 + i, rows = (int64_t)a.parts * a.heads_q * a.tokens_q;
+        store_part(o, a.part + row * a.d, a.d, mine, lane);
+        if (mine && h == 0) {
+            a.part[rows * a.d + 2 * row] = m;
+            a.part[rows * a.d + 2 * row + 1] = l;
+        }
+        return;
+    }
     if (mine && h == 0 && a.lse != nullptr)
         a.lse[(int64_t)head * a.tokens_q + seq.q0 + i] = l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     store_columns(o, l == 0.f ? 0.f : 1.f / l, a.o + (int64_t)(seq.q0 + i) * a.o_ts + (int64_t)head * a.o_hs, a.d, mine, lane);
 }
 
-// The scores' gradients of one 32 x 32 block, from the products s and dp (in place: s becomes p, dp becomes ds / scale).
-// lse2, delta: per register or per lane; the position and the visible interval too.
-template <bool CAP, bool BIAS, bool MASKED>
-__device__ __forceinline__ void score_gradient(float& s, float& dp, const ScoreRule& rule, float lse2, float delta, int j, float pos, int lo, int hi) {
-    float factor;
-    float x = score_log2<CAP>(s, rule.c, rule.cap_log2e, factor);
-    if constexpr (BIAS) x = __builtin_fmaf(-rule.slope, fabsf(pos - (float)j), x);
-    const bool seen = !MASKED || (j >= lo && j <= hi);
-    float p = __builtin_amdgcn_exp2f(x - lse2);
-    float g = p * (dp - delta);
-    if constexpr (CAP) g *= factor;
-    s = seen ? p : 0.f;
-    dp = seen ? g : 0.f;
+// Joins the parts of the forward pass in their order: four elements of a row per thread.
+__global__ __launch_bounds__(256) void k_attention_fwd_join(AttnArgs a) {
+    const int per = a.d / 4;
+    const int64_t rows = (int64_t)a.heads_q * a.tokens_q, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / per;
+    if (row >= rows) return;
+    const int e = (int)(at - row * per) * 4, head = (int)(row / a.tokens_q), token = (int)(row - (int64_t)head * a.tokens_q);
+    const float* stat = a.part + rows * a.parts * a.d + 2 * row;
+    float top = -INFINITY, sum = 0.f;
+    for (int p = 0; p < a.parts; ++p) top = fmaxf(top, stat[2 * rows * p]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.parts; ++p) {
+        const float f = __builtin_amdgcn_exp2f(stat[2 * rows * p] - ref);
+        sum = __builtin_fmaf(stat[2 * rows * p + 1], f, sum);
+        x += *reinterpret_cast<const f32x4*>(a.part + (rows * p + row) * a.d + e) * f;
+    }
+    if (e == 0 && a.lse != nullptr) a.lse[row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const u32x2 w = {pack_bf16x2(x[0] * f, x[1] * f), pack_bf16x2(x[2] * f, x[3] * f)};
+    *reinterpret_cast<u32x2*>(a.o + (int64_t)token * a.o_ts + (int64_t)head * a.o_hs + e) = w;
+}
+
+// Of one score: s becomes p, dp becomes p (dp - delta); returns what that is multiplied by for the gradient of scale q.k (1 - tanh^2, or 1).
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float lse2, float delta, float distance) {
+    float factor = 1.f;
+    if constexpr (!CAP && !BIAS) {
+        s = __builtin_amdgcn_exp2f(__builtin_fmaf(s, rule.c, -lse2));
+    } else {
+        float x = score_log2<CAP>(s, rule.c, rule.cap_log2e, factor);
+        if constexpr (BIAS) x = __builtin_fmaf(-rule.slope, fabsf(distance), x);
+        s = __builtin_amdgcn_exp2f(x - lse2);
+    }
+    dp = s * (dp - delta);
+    return factor;
 }
 
 // lse as the exponent's offset: a row without a visible key has p = 0.
@@ -180,10 +223,12 @@ __device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ?
 
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
-    constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16;
-    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * kAttnStep * P];
-    int head, t;
-    if (!attn_place(a.heads_q * a.tiles, a.tiles, head, t)) return;
+    constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
+    constexpr bool PARKED = D > 64;
+    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
+    uint16_t* const parked = smem + 4 * STEP * P;
+    int head, t, part;
+    if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, false>(a, a.tiles - 1 - t);
     const int row0 = seq.tile * kAttnRows;
     if (row0 >= seq.nq) return;
@@ -195,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     const uint16_t* vp = a.v + (int64_t)seq.k0 * a.v_ts + (int64_t)kv * a.v_hs;
     const int w0 = row0 + 32 * wave, i = w0 + (lane & 31), w1 = min(w0 + 31, seq.nq - 1);
     const bool mine = i < seq.nq;
-    bf16x8 qf[NS], gf[NS];
+    bf16x8 qf[NS], gf[PARKED ? 1 : NS];
     float delta = 0.f;
     {
         const uint16_t* qp = a.q + (int64_t)seq.q0 * a.q_ts + (int64_t)head * a.q_hs;
@@ -204,92 +249,163 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             qf[s] = row_frag(qp, a.q_ts, i, seq.nq, s, a.d, lane);
-            gf[s] = row_frag(gp, a.do_ts, i, seq.nq, s, a.d, lane);
+            const bf16x8 g = row_frag(gp, a.do_ts, i, seq.nq, s, a.d, lane);
+            if constexpr (!PARKED) gf[s] = g;
             const bf16x8 of = row_frag(op, a.o_ts, i, seq.nq, s, a.d, lane);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)gf[s][e], (float)of[e], delta);
+            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)g[e], (float)of[e], delta);
         }
         delta += other_half(delta);
+        if constexpr (PARKED) {
+            RowsTile<P, kAttnRows, 256> g;
+            g.init(a.do_ts, a.d);
+            g.load(parked, gp + (int64_t)row0 * a.do_ts, a.do_ts, seq.nq - row0);
+        }
     }
     const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-    if (mine && h == 0) a.delta[at] = delta;
     const float lse2 = mine ? lse_log2(a.lse[at]) : INFINITY;
     const int lo = see.lo(i), hi = see.hi(i);
-    const int first = see.lo(row0) / kAttnStep, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
-    const int steps = most < 0 ? 0 : most / kAttnStep - first + 1;
+    const int first = see.lo(row0) / STEP, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
+    const int all = most < 0 ? 0 : most / STEP - first + 1;
+    const int begin = (int)((int64_t)all * part / a.parts), steps = (int)((int64_t)all * (part + 1) / a.parts);
     const int wave_lo = see.lo(w0), wave_hi = w0 < seq.nq ? see.hi(w1) : -1, all_lo = see.lo(w1), all_hi = see.hi(w0);
     f32x16 dq[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) dq[b] = zero16();
-    RowsTile<P, kAttnStep, 256> kt, vt;
+    f32x16 mean[NB];
+    float rest = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mean[b] = zero16();
+    RowsTile<P, STEP, 256> kt, vt;
     kt.init(a.k_ts, a.d);
     vt.init(a.v_ts, a.d);
     auto fetch = [&](int step, int stage) {
-        const int j = (first + step) * kAttnStep;
-        kt.load(smem + stage * 2 * kAttnStep * P, kp + (int64_t)j * a.k_ts, a.k_ts, seq.nk - j);
-        vt.load(smem + (stage * 2 + 1) * kAttnStep * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
+        const int j = (first + step) * STEP;
+        kt.load(smem + stage * 2 * STEP * P, kp + (int64_t)j * a.k_ts, a.k_ts, seq.nk - j);
+        vt.load(smem + (stage * 2 + 1) * STEP * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
     };
-    const float pos = (float)(i + see.shift);
-    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, auto masked) {
+    const float pos = (float)(i + see.shift - 4 * h);
+    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, bool masked) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < STEP / 32; ++b) {
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(K, 32 * b, k, lane), qf[k], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(V, 32 * b, k, lane), gf[k], dp, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(V, 32 * b, k, lane), PARKED ? tile_frag<P>(parked, 32 * wave, k, lane) : gf[PARKED ? 0 : k], dp, 0, 0, 0);
             }
+            f32x16 factor;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 float p = s[v], g = dp[v];
-                score_gradient<CAP, BIAS, decltype(masked)::value>(p, g, rule, lse2, delta, j0 + 32 * b + acc_row(v) + 4 * h, pos, lo, hi);
+                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, lse2, delta, pos - (float)(j0 + 32 * b + acc_row(v)));
+                s[v] = p;
                 dp[v] = g;
+            }
+            if (masked) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int j = j0 + 32 * b + acc_row(v) + 4 * h;
+                    const bool seen = j >= lo && j <= hi;
+                    s[v] = seen ? s[v] : 0.f;
+                    dp[v] = seen ? dp[v] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) rest += dp[v];
+            if constexpr (CAP) {
+                s *= factor;
+                dp *= factor;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bf16x8 df = score_frag(dp, u);
+                const bf16x8 df = score_frag(dp, u), pf = score_frag(s, u);
 #pragma unroll
-                for (int c = 0; c < NB; ++c)
-                    dq[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag_t<P>(K, 32 * b + 16 * u, c, lane), df, dq[c], 0, 0, 0);
+                for (int c = 0; c < NB; ++c) {
+                    const bf16x8 kf = tile_frag_t<P>(K, 32 * b + 16 * u, c, lane);
+                    dq[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, df, dq[c], 0, 0, 0);
+                    mean[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, pf, mean[c], 0, 0, 0);
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);     // (one block of scores at a time: more of them in flight spill)
         }
     };
-    if (steps > 0) fetch(0, 0);
-    for (int step = 0; step < steps; ++step) {
+    if (steps > begin) fetch(begin, begin & 1);
+    for (int step = begin; step < steps; ++step) {
         wait_loads<0>();
         lds_barrier();
         if (step + 1 < steps) fetch(step + 1, (step + 1) & 1);
-        const int j0 = (first + step) * kAttnStep;
-        const uint16_t *K = smem + (step & 1) * 2 * kAttnStep * P, *V = K + kAttnStep * P;
-        if (j0 > wave_hi || j0 + kAttnStep <= wave_lo) continue;
-        if (j0 >= all_lo && j0 + kAttnStep - 1 <= all_hi) compute(j0, K, V, std::false_type());
-        else compute(j0, K, V, std::true_type());
+        const int j0 = (first + step) * STEP;
+        const uint16_t *K = smem + (step & 1) * 2 * STEP * P, *V = K + STEP * P;
+        if (j0 > wave_hi || j0 + STEP <= wave_lo) continue;
+        compute(j0, K, V, j0 < all_lo || j0 + STEP - 1 > all_hi);
     }
+    rest += other_half(rest);
+    if (a.parts > 1) {
+        const int64_t row = ((int64_t)part * a.heads_q + head) * a.tokens_q + seq.q0 + i, rows = (int64_t)a.parts * a.heads_q * a.tokens_q;
+        store_part(dq, a.part + row * a.d, a.d, mine, lane);
+        store_part(mean, a.part + (rows + row) * a.d, a.d, mine, lane);
+        if (mine && h == 0) a.part[2 * rows * a.d + row] = rest;
+        if (mine && h == 0 && part == 0) a.delta[at] = delta;
+        return;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dq[b][v] = __builtin_fmaf(-rest, mean[b][v], dq[b][v]);
+    if (mine && h == 0) a.delta[at] = delta + rest;
     store_columns(dq, a.scale, a.dq + (int64_t)(seq.q0 + i) * a.dq_ts + (int64_t)head * a.dq_hs, a.d, mine, lane);
 }
 
+// Joins the parts of dq: four elements of a row per thread.
+__global__ __launch_bounds__(256) void k_attention_dq_join(AttnArgs a) {
+    const int per = a.d / 4;
+    const int64_t rows = (int64_t)a.heads_q * a.tokens_q, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / per;
+    if (row >= rows) return;
+    const int e = (int)(at - row * per) * 4, head = (int)(row / a.tokens_q), token = (int)(row - (int64_t)head * a.tokens_q);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, mean = x;
+    float rest = 0.f;
+    for (int p = 0; p < a.parts; ++p) {
+        const float* from = a.part + (rows * p + row) * a.d + e;
+        x += *reinterpret_cast<const f32x4*>(from);
+        mean += *reinterpret_cast<const f32x4*>(from + rows * a.parts * a.d);
+        rest += a.part[2 * rows * a.parts * a.d + rows * p + row];
+    }
+    x = (x - mean * rest) * a.scale;
+    if (e == 0) a.delta[row] += rest;
+    const u32x2 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    *reinterpret_cast<u32x2*>(a.dq + (int64_t)token * a.dq_ts + (int64_t)head * a.dq_hs + e) = w;
+}
+
 template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 1) void k_attention_dkv(AttnArgs a) {
-    constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16;
-    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * kAttnStep * P];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][kAttnStep];   // lse and delta of a step's queries
+__global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
+    constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
+    constexpr bool PARKED = D > 64;
+    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
+    uint16_t* const parked = smem + 4 * STEP * P;
+    __shared__ __attribute__((aligned(16))) float stats[2][2][STEP];   // lse and delta of a step's queries
     const int heads_k = a.heads_q / a.group;
-    int kv, t;
-    if (!attn_place(heads_k * a.tiles, a.tiles, kv, t)) return;
+    int kv, t, part;
+    if (!attn_place(heads_k, a.tiles, a.parts, kv, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, true>(a, t);        // early tiles first: with a causal mask they have most queries
     const int row0 = seq.tile * kAttnRows;
     if (row0 >= seq.nk) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const Visible see(a, seq);
     const int w0 = row0 + 32 * wave, j = w0 + (lane & 31);
-    bf16x8 kf[NS], vf[NS];
+    bf16x8 kf[NS], vf[PARKED ? 1 : NS];
     {
         const uint16_t* kp = a.k + (int64_t)seq.k0 * a.k_ts + (int64_t)kv * a.k_hs;
         const uint16_t* vp = a.v + (int64_t)seq.k0 * a.v_ts + (int64_t)kv * a.v_hs;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             kf[s] = row_frag(kp, a.k_ts, j, seq.nk, s, a.d, lane);
-            vf[s] = row_frag(vp, a.v_ts, j, seq.nk, s, a.d, lane);
+            if constexpr (!PARKED) vf[s] = row_frag(vp, a.v_ts, j, seq.nk, s, a.d, lane);
+        }
+        if constexpr (PARKED) {
+            RowsTile<P, kAttnRows, 256> v;
+            v.init(a.v_ts, a.d);
+            v.load(parked, vp + (int64_t)row0 * a.v_ts, a.v_ts, seq.nk - row0);
         }
     }
     // queries that see a key of the workgroup: causal, those from the key's position on (all, if the key lies in the prefix); with a
@@ -300,34 +416,36 @@ __global__ __launch_bounds__(256, 1) void k_attention_dkv(AttnArgs a) {
         if (row0 >= see.prefix) qa = max(0, row0 - see.shift);
         if (see.window > 0) qb = (int)min((int64_t)qb, (int64_t)end - see.shift + see.window);
     }
-    const int first = qa / kAttnStep, steps = qb > qa ? (qb - 1) / kAttnStep - first + 1 : 0, total = steps * a.group;
+    const int first = qa / STEP, steps = qb > qa ? (qb - 1) / STEP - first + 1 : 0, all = steps * a.group;
+    const int begin = (int)((int64_t)all * part / a.parts), total = (int)((int64_t)all * (part + 1) / a.parts);
     f32x16 dk[NB], dv[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) dk[b] = dv[b] = zero16();
-    RowsTile<P, kAttnStep, 256> qt, gt;
+    RowsTile<P, STEP, 256> qt, gt;
     qt.init(a.q_ts, a.d);
     gt.init(a.do_ts, a.d);
     auto fetch = [&](int it, int stage) {
-        const int head = kv * a.group + it / steps, i0 = (first + it % steps) * kAttnStep;
-        qt.load(smem + stage * 2 * kAttnStep * P, a.q + (int64_t)(seq.q0 + i0) * a.q_ts + (int64_t)head * a.q_hs, a.q_ts, seq.nq - i0);
-        gt.load(smem + (stage * 2 + 1) * kAttnStep * P, a.dO + (int64_t)(seq.q0 + i0) * a.do_ts + (int64_t)head * a.do_hs, a.do_ts, seq.nq - i0);
+        const int head = kv * a.group + it / steps, i0 = (first + it % steps) * STEP;
+        qt.load(smem + stage * 2 * STEP * P, a.q + (int64_t)(seq.q0 + i0) * a.q_ts + (int64_t)head * a.q_hs, a.q_ts, seq.nq - i0);
+        gt.load(smem + (stage * 2 + 1) * STEP * P, a.dO + (int64_t)(seq.q0 + i0) * a.do_ts + (int64_t)head * a.do_hs, a.do_ts, seq.nq - i0);
     };
     // lse and delta of a step: read into registers a step ahead, put into LDS with the barrier
     float stat = 0.f;
     auto fetch_stats = [&](int it) {
-        const int head = kv * a.group + it / steps, i = (first + it % steps) * kAttnStep + (threadIdx.x & 63);
+        const int head = kv * a.group + it / steps, i = (first + it % steps) * STEP + (threadIdx.x & (STEP - 1));
         const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-        if (threadIdx.x < 64) stat = i < seq.nq ? lse_log2(a.lse[at]) : INFINITY;
-        else if (threadIdx.x < 128) stat = i < seq.nq ? a.delta[at] : 0.f;
+        if (threadIdx.x < STEP) stat = i < seq.nq ? lse_log2(a.lse[at]) : INFINITY;
+        else if (threadIdx.x < 2 * STEP) stat = i < seq.nq ? a.delta[at] : 0.f;
     };
-    auto compute = [&](int i0, const uint16_t* Q, const uint16_t* G, const float (*st)[kAttnStep], const ScoreRule& rule, auto masked) {
+    const float pos = (float)(j - see.shift - 4 * h);      // the distance from a register's query without its 4 h
+    auto compute = [&](int i0, const uint16_t* Q, const uint16_t* G, const float (*st)[STEP], const ScoreRule& rule, bool masked) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < STEP / 32; ++b) {
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(Q, 32 * b, k, lane), kf[k], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(G, 32 * b, k, lane), vf[k], dp, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(G, 32 * b, k, lane), PARKED ? tile_frag<P>(parked, 32 * wave, k, lane) : vf[PARKED ? 0 : k], dp, 0, 0, 0);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -335,16 +453,19 @@ __global__ __launch_bounds__(256, 1) void k_attention_dkv(AttnArgs a) {
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(&st[1][32 * b + 8 * r + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int i = i0 + 32 * b + 8 * r + 4 * h + e;
                     float p = s[4 * r + e], g = dp[4 * r + e];
-                    int lo = 0, hi = 0;
-                    if constexpr (decltype(masked)::value) {
-                        lo = see.lo(i);
-                        hi = see.hi(i);
-                    }
-                    score_gradient<CAP, BIAS, decltype(masked)::value>(p, g, rule, lse2[e], delta[e], j, (float)(i + see.shift), lo, hi);
+                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, lse2[e], delta[e], (float)(i0 + 32 * b + 8 * r + e) - pos);
                     s[4 * r + e] = p;
-                    dp[4 * r + e] = g;
+                    dp[4 * r + e] = CAP ? g * factor : g;
+                }
+            }
+            if (masked) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int i = i0 + 32 * b + acc_row(v) + 4 * h;
+                    const bool seen = j >= see.lo(i) && j <= see.hi(i);
+                    s[v] = seen ? s[v] : 0.f;
+                    dp[v] = seen ? dp[v] : 0.f;
                 }
             }
 #pragma unroll
@@ -356,31 +477,54 @@ __global__ __launch_bounds__(256, 1) void k_attention_dkv(AttnArgs a) {
                     dk[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag_t<P>(Q, 32 * b + 16 * u, c, lane), df, dk[c], 0, 0, 0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if (total > 0) {
-        fetch(0, 0);
-        fetch_stats(0);
+    if (total > begin) {
+        fetch(begin, begin & 1);
+        fetch_stats(begin);
     }
     const int last_key = min(w0 + 31, seq.nk - 1);
-    for (int it = 0; it < total; ++it) {
+    for (int it = begin; it < total; ++it) {
         wait_loads<0>();
-        if (threadIdx.x < 128) stats[it & 1][threadIdx.x >> 6][threadIdx.x & 63] = stat;
+        if (threadIdx.x < 2 * STEP) stats[it & 1][threadIdx.x / STEP][threadIdx.x & (STEP - 1)] = stat;
         lds_barrier();
         if (it + 1 < total) {
             fetch(it + 1, (it + 1) & 1);
             fetch_stats(it + 1);
         }
-        const int i0 = (first + it % steps) * kAttnStep, i1 = min(i0 + kAttnStep, seq.nq) - 1;
-        const uint16_t *Q = smem + (it & 1) * 2 * kAttnStep * P, *G = Q + kAttnStep * P;
+        const int i0 = (first + it % steps) * STEP, i1 = min(i0 + STEP, seq.nq) - 1;
+        const uint16_t *Q = smem + (it & 1) * 2 * STEP * P, *G = Q + STEP * P;
         if (w0 >= seq.nk || see.hi(i1) < w0 || see.lo(i0) > last_key) continue;
         const ScoreRule rule = score_rule<CAP, BIAS>(a, kv * a.group + it / steps);
-        if (see.lo(i1) <= w0 && see.hi(i0) >= last_key) compute(i0, Q, G, stats[it & 1], rule, std::false_type());
-        else compute(i0, Q, G, stats[it & 1], rule, std::true_type());
+        compute(i0, Q, G, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key);
     }
     const bool mine = j < seq.nk;
+    if (a.parts > 1) {
+        const int64_t rows = (int64_t)a.tokens_k * heads_k, row = (int64_t)(seq.k0 + j) * heads_k + kv;
+        store_part(dk, a.part + (rows * (2 * part) + row) * a.d, a.d, mine, lane);
+        store_part(dv, a.part + (rows * (2 * part + 1) + row) * a.d, a.d, mine, lane);
+        return;
+    }
     store_columns(dk, a.scale, a.dk + (int64_t)(seq.k0 + j) * a.dk_ts + (int64_t)kv * a.dk_hs, a.d, mine, lane);
     store_columns(dv, 1.f, a.dv + (int64_t)(seq.k0 + j) * a.dv_ts + (int64_t)kv * a.dv_hs, a.d, mine, lane);
+}
+
+// Joins the parts of dk and dv: four elements of both per thread.
+__global__ __launch_bounds__(256) void k_attention_dkv_join(AttnArgs a) {
+    const int per = a.d / 4, heads_k = a.heads_q / a.group;
+    const int64_t rows = (int64_t)a.tokens_k * heads_k, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / per;
+    if (row >= rows) return;
+    const int e = (int)(at - row * per) * 4, token = (int)(row / heads_k), kv = (int)(row - (int64_t)token * heads_k);
+    f32x4 dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
+    for (int p = 0; p < a.parts; ++p) {
+        dk += *reinterpret_cast<const f32x4*>(a.part + (rows * (2 * p) + row) * a.d + e);
+        dv += *reinterpret_cast<const f32x4*>(a.part + (rows * (2 * p + 1) + row) * a.d + e);
+    }
+    dk *= a.scale;
+    const u32x2 wk = {pack_bf16x2(dk[0], dk[1]), pack_bf16x2(dk[2], dk[3])}, wv = {pack_bf16x2(dv[0], dv[1]), pack_bf16x2(dv[2], dv[3])};
+    *reinterpret_cast<u32x2*>(a.dk + (int64_t)token * a.dk_ts + (int64_t)kv * a.dk_hs + e) = wk;
+    *reinterpret_cast<u32x2*>(a.dv + (int64_t)token * a.dv_ts + (int64_t)kv * a.dv_hs + e) = wv;
 }
 
 // f(padded d, capped, biased) of a call's kernels: d in 64, 96 or 128.
@@ -440,30 +584,66 @@ static AttnArgs attn_args(const qg_attention* a, const qg_heads* q, const qg_hea
     return r;
 }
 
-static dim3 attn_grid(int64_t work) { return dim3((unsigned)((work + 7) / 8 * 8)); }
+// Workgroups of `tiles` tiles of rows, `heads` of them and parts.
+static dim3 attn_grid(const AttnArgs& a, int heads) { return dim3((unsigned)(((int64_t)a.tiles * heads * a.parts + 7) / 8 * 8)); }
+static dim3 join_grid(int64_t rows, int d) { return dim3((unsigned)((rows * (d / 4) + 255) / 256)); }
+
+// Parts of the keys of a call with few tiles of queries (forward, dq), and of the queries, of all heads that share a key head, of one with few
+// tiles of keys (dkv); their fp32 sums go through the workspace and are joined in order.  `steps`: of 64 rows, of a sequence in the mean.
+struct AttnParts {
+    int forward, dq, dkv;
+};
+static int attn_parts(int64_t parts, int64_t steps) {
+    const int64_t most = steps / 4;      // (a part of fewer steps costs more in its ends and in the join than it saves)
+    return (int)(parts < 1 || most < 1 ? 1 : parts < most ? (parts < 16 ? parts : 16) : most < 16 ? most : 16);
+}
+// Keys: whole parts of 512 workgroups (us without / with; 2048 queries, 8 heads of 128 on one key head: forward 41 / 31; 4096, one head of 64: 56 / 22,
+// backward 196 / 70; but 2000, 24 heads, 432 tiles, in two parts: 27 / 34).  Queries: 1024 workgroups or more, since a causal mask gives
+// the first keys most of the work (us in one part / by the rule / for 2048: 8192 tokens, 32 heads on 8 of 128: backward 3140 / 2270 / 2230; 4096, 16 on
+// 4, four sequences: 343 / 184 / 207; 4096, 32 on 32 without a mask, 1088 tiles: 1092 / 1091 / 1225; 1003, 10 on 2, five sequences: 63 / 37 / 37).
+static AttnParts attn_parts(const qg_attention* a) {
+    const int64_t work_q = attn_tiles(a->tokens_q, a->sequences) * a->heads_q, work_k = attn_tiles(a->tokens_k, a->sequences) * a->heads_k;
+    const int keys = attn_parts(512 / work_q, a->tokens_k / a->sequences / 64);
+    return {keys, keys, attn_parts((1024 + work_k - 1) / work_k, a->tokens_q / a->sequences * (a->heads_q / a->heads_k) / 64)};
+}
+// Floats of the parts' sums.
+static int64_t forward_floats(const qg_attention* a, int parts) { return parts > 1 ? (int64_t)parts * a->heads_q * a->tokens_q * (a->d + 2) : 0; }
+static int64_t backward_floats(const qg_attention* a, const AttnParts& p) {
+    const int64_t dq = p.dq > 1 ? (int64_t)p.dq * a->heads_q * a->tokens_q * (2 * a->d + 1) : 0;
+    const int64_t dkv = p.dkv > 1 ? (int64_t)p.dkv * a->heads_k * a->tokens_k * 2 * a->d : 0;
+    return dq > dkv ? dq : dkv;
+}
+static int64_t delta_floats(const qg_attention* a) { return ((int64_t)a->heads_q * a->tokens_q + 3) / 4 * 4; }
 
 }  // namespace qg
 
 using namespace qg;
 
-extern "C" size_t qg_attention_workspace_bytes(const qg_attention* a) {
-    if (check_attention(a) != QG_OK) return 0;
-    return ((size_t)a->heads_q * a->tokens_q * 4 + 15) / 16 * 16;
+extern "C" size_t qg_attention_forward_workspace_bytes(const qg_attention* a) {
+    return check_attention(a) == QG_OK ? (size_t)forward_floats(a, attn_parts(a).forward) * 4 : 0;
+}
+
+extern "C" size_t qg_attention_backward_workspace_bytes(const qg_attention* a) {
+    return check_attention(a) == QG_OK ? (size_t)(delta_floats(a) + backward_floats(a, attn_parts(a))) * 4 : 0;
 }
 
 extern "C" int qg_attention_forward(const qg_attention* a, const qg_heads* q, const qg_heads* k, const qg_heads* v, const qg_heads* o,
                                     float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    (void)workspace, (void)workspace_bytes;
     if (int e = check_attention(a)) return e;
     for (const qg_heads* x : {q, k, v, o})
         if (int e = check_heads(x, true)) return e;
-    if (reinterpret_cast<uintptr_t>(lse) & 3) return QG_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3) || !aligned16(workspace)) return QG_ERR_ALIGN;
     AttnArgs args = attn_args(a, q, k, v, o, lse);
+    args.parts = attn_parts(a).forward;
+    const size_t need = (size_t)forward_floats(a, args.parts) * 4;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return QG_ERR_WORKSPACE;
+    args.part = static_cast<float*>(workspace);
     args.tiles = (int)attn_tiles(a->tokens_q, a->sequences);
     attn_shape(*a, [&](auto d, auto cap, auto bias) {
-        hipLaunchKernelGGL((k_attention_fwd<d.value, cap.value, bias.value>), attn_grid((int64_t)args.tiles * args.heads_q), dim3(256), 0,
-                           (hipStream_t)stream, args);
+        hipLaunchKernelGGL((k_attention_fwd<d.value, cap.value, bias.value>), attn_grid(args, args.heads_q), dim3(256), 0, (hipStream_t)stream, args);
     });
+    if (args.parts > 1)
+        hipLaunchKernelGGL(k_attention_fwd_join, join_grid(a->tokens_q * a->heads_q, a->d), dim3(256), 0, (hipStream_t)stream, args);
     return check_launch();
 }
 
@@ -475,20 +655,24 @@ extern "C" int qg_attention_backward(const qg_attention* a, const qg_heads* dO, 
         if (int e = check_heads(x, true)) return e;
     if (lse == nullptr) return QG_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(lse) & 3) || !aligned16(workspace)) return QG_ERR_ALIGN;
-    if (workspace == nullptr || workspace_bytes < qg_attention_workspace_bytes(a)) return QG_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < qg_attention_backward_workspace_bytes(a)) return QG_ERR_WORKSPACE;
     AttnArgs args = attn_args(a, q, k, v, o, const_cast<float*>(lse));
     args.dO = dO->data, args.do_ts = dO->token_stride, args.do_hs = dO->head_stride;
     args.dq = dq->data, args.dq_ts = dq->token_stride, args.dq_hs = dq->head_stride;
     args.dk = dk->data, args.dk_ts = dk->token_stride, args.dk_hs = dk->head_stride;
     args.dv = dv->data, args.dv_ts = dv->token_stride, args.dv_hs = dv->head_stride;
     args.delta = static_cast<float*>(workspace);
+    args.part = args.delta + delta_floats(a);
+    const AttnParts parts = attn_parts(a);
     attn_shape(*a, [&](auto d, auto cap, auto bias) {
-        args.tiles = (int)attn_tiles(a->tokens_q, a->sequences);
-        hipLaunchKernelGGL((k_attention_dq<d.value, cap.value, bias.value>), attn_grid((int64_t)args.tiles * args.heads_q), dim3(256), 0,
-                           (hipStream_t)stream, args);
-        args.tiles = (int)attn_tiles(a->tokens_k, a->sequences);
-        hipLaunchKernelGGL((k_attention_dkv<d.value, cap.value, bias.value>), attn_grid((int64_t)args.tiles * a->heads_k), dim3(256), 0,
-                           (hipStream_t)stream, args);
+        args.tiles = (int)attn_tiles(a->tokens_q, a->sequences), args.parts = parts.dq;
+        hipLaunchKernelGGL((k_attention_dq<d.value, cap.value, bias.value>), attn_grid(args, a->heads_q), dim3(256), 0, (hipStream_t)stream, args);
+        if (parts.dq > 1)
+            hipLaunchKernelGGL(k_attention_dq_join, join_grid(a->tokens_q * a->heads_q, a->d), dim3(256), 0, (hipStream_t)stream, args);
+        args.tiles = (int)attn_tiles(a->tokens_k, a->sequences), args.parts = parts.dkv;
+        hipLaunchKernelGGL((k_attention_dkv<d.value, cap.value, bias.value>), attn_grid(args, a->heads_k), dim3(256), 0, (hipStream_t)stream, args);
+        if (parts.dkv > 1)
+            hipLaunchKernelGGL(k_attention_dkv_join, join_grid(a->tokens_k * a->heads_k, a->d), dim3(256), 0, (hipStream_t)stream, args);
     });
     return check_launch();
 }

@@ -37,7 +37,7 @@ EXPORTS = [
     "qg_residual_norm_forward", "qg_residual_norm_workspace_bytes", "qg_residual_norm_backward",
     "qg_int8_linear_act_forward", "qg_int8_linear_act_workspace_bytes", "qg_int8_linear_act_backward", "qg_int8_gated_forward",
     "qg_int8_gated_backward", "qg_int8_gated_workspace_bytes", "qg_head_loss_workspace_bytes", "qg_head_loss_forward", "qg_head_loss_backward",
-    "qg_rope_frequencies", "qg_rope_forward", "qg_rope_backward", "qg_attention_workspace_bytes", "qg_attention_forward",
+    "qg_rope_frequencies", "qg_rope_forward", "qg_rope_backward", "qg_attention_forward_workspace_bytes", "qg_attention_backward_workspace_bytes", "qg_attention_forward",
     "qg_attention_backward", "qg_cache_append", "qg_attention_paged_workspace_bytes", "qg_attention_paged",
 ]
 
@@ -180,8 +180,8 @@ def lib() -> C.CDLL:
         L.qg_rope_frequencies.argtypes = [i32, f64, f64, f64, f64, f64, vp]
         L.qg_rope_forward.argtypes = [heads, i32, heads, i32, vp, vp, i64, i32, i32, i32, f32, heads, heads, vp]
         L.qg_rope_backward.argtypes = L.qg_rope_forward.argtypes
-        L.qg_attention_workspace_bytes.restype = sz
-        L.qg_attention_workspace_bytes.argtypes = [attention]
+        for f in (L.qg_attention_forward_workspace_bytes, L.qg_attention_backward_workspace_bytes):
+            f.restype, f.argtypes = sz, [attention]
         L.qg_attention_forward.argtypes = [attention, heads, heads, heads, heads, vp, vp, sz, vp]
         L.qg_attention_backward.argtypes = [attention] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
         L.qg_cache_append.argtypes = [cache, heads, i32, heads, heads, vp, vp, i64, vp, i32, i32, f32, heads, vp]
@@ -860,12 +860,13 @@ def _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix) 
                      _ptr(slopes, _F32), d ** -0.5 if scale is None else scale, cap, int(causal), window)
 
 
-def _workspace(nbytes: int, like: torch.Tensor, given: torch.Tensor | None) -> torch.Tensor:
-    if given is not None:
-        return given
-    if nbytes == 0:
-        raise QGError("libqgalore: shape out of range")
-    return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+def _workspace(nbytes: int, like: torch.Tensor, given: torch.Tensor | None):
+    """(pointer, bytes) of a call's workspace, and the tensor that holds it: the given one, or a new one if any is needed."""
+    if given is None:
+        if nbytes == 0:
+            return None, None, 0
+        given = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return given, _ptr(given, (torch.uint8,)), given.numel()
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor | None = None, cu_k: torch.Tensor | None = None,
@@ -878,9 +879,8 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: t
     a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
     o = _written(out, q, "out")
     lse = torch.empty(a.heads_q, a.tokens_q, dtype=torch.float32, device=q.device)
-    ws = _workspace(lib().qg_attention_workspace_bytes(C.byref(a)), q, workspace)
-    _check(lib().qg_attention_forward(C.byref(a), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), _ptr(ws, (torch.uint8,)), ws.numel(),
-                                      _stream()))
+    ws, *at = _workspace(lib().qg_attention_forward_workspace_bytes(C.byref(a)), q, workspace)
+    _check(lib().qg_attention_forward(C.byref(a), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *at, _stream()))
     return o, lse
 
 
@@ -895,9 +895,9 @@ def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
         _expect(t, *q.shape)
     _expect(lse, a.heads_q, a.tokens_q)
     dq, dk, dv = (_written(None if out is None else out[i], t, "out") for i, t in enumerate((q, k, v)))
-    ws = _workspace(lib().qg_attention_workspace_bytes(C.byref(a)), q, workspace)
+    ws, *at = _workspace(lib().qg_attention_backward_workspace_bytes(C.byref(a)), q, workspace)
     _check(lib().qg_attention_backward(C.byref(a), _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse, _F32), _heads(dq),
-                                       _heads(dk), _heads(dv), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+                                       _heads(dk), _heads(dv), *at, _stream()))
     return dq, dk, dv
 
 
@@ -944,9 +944,9 @@ def attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     _expect(lengths, c.sequences)
     _expect(slopes, heads)
     o = _written(out, q, "out")
-    ws = _workspace(lib().qg_attention_paged_workspace_bytes(C.byref(c), heads), q, workspace)
+    ws, *at = _workspace(lib().qg_attention_paged_workspace_bytes(C.byref(c), heads), q, workspace)
     _check(lib().qg_attention_paged(C.byref(c), _ptr(lengths, _I32), _heads(q), heads, c.d ** -0.5 if scale is None else scale, cap, window,
-                                    _ptr(slopes, _F32), _heads(o), _ptr(ws, (torch.uint8,)), ws.numel(), _stream()))
+                                    _ptr(slopes, _F32), _heads(o), *at, _stream()))
     return o
 
 

@@ -6,9 +6,10 @@ factor e + (keys + 16) 2^-24 (the sum; exponentials; lse's own rounding, |lse| 2
     |o - want|  <= (h + 2 e') sum p |v| + h |o|                                   (o's own rounding)
     |lse - want| <= e + (keys + 16) 2^-24 + |lse| 2^-22
     |dv - want| <= (h + 2 e') sum p |do| + h |dv|
-ds = p (do.v - delta) factor scale, rounded to bf16, delta = sum do o with o as stored:
-    |ds - want| <= (h + 2 e') |ds| + p scale ((d + 4) 2^-24 (|do|.|v| + |do|.|o|) + 2^-19 |do.v - delta| if capped)
-    |dq - want| <= sum |ds's error| |k| + h |dq|,  dk alike;  fp32 sums over n terms add n 2^-24 of the sum of magnitudes.
+ds = p (do.v - delta) factor scale, rounded to bf16.  delta is formed from o as stored and corrected by the sum of the row's p (do.v - delta), fp32:
+    |ds - want| <= (h + 2 e') |ds| + p scale ((d + keys + 8) 2^-24 (|do|.|v| + |do|.|o|) + 2^-19 |do.v - delta| if capped)
+    |dq - want| <= sum |ds's error| |k| + h |dq| + (h |do|.|o|) (h + 2 e') scale sum p |k|         (the correction and its bf16 p), dk without that;
+fp32 sums over n terms add n 2^-24 of the sum of magnitudes.
 (All first order; 1 % on top for the products of errors.)"""
 import math
 
@@ -67,11 +68,12 @@ def check(q, k, v, do, lengths, lengths_k=None, causal=True, scale=None, cap=0.0
             assert np.all(off <= ep[~empty, 0]), ("lse", s, h, float(off.max()))
             if grads is None:
                 continue
-            dq, dk, dv, ds = A.attention_gradients(gh, qh, kh, vh, scale, seen, cap, slope, o=got)
-            inner = gh @ vh.T - (gh * got).sum(axis=1, keepdims=True)
-            eds = (H + 2 * ep) * np.abs(ds) + p * scale * ((d + 4) * 2.0 ** -24 * (np.abs(gh) @ np.abs(vh).T + (np.abs(gh) * np.abs(got)).sum(1, keepdims=True))
+            dq, dk, dv, ds = A.attention_gradients(gh, qh, kh, vh, scale, seen, cap, slope)
+            inner = gh @ vh.T - (gh * want).sum(axis=1, keepdims=True)
+            go = (np.abs(gh) * np.abs(want)).sum(axis=1, keepdims=True)
+            eds = (H + 2 * ep) * np.abs(ds) + p * scale * ((d + m + 8) * 2.0 ** -24 * (np.abs(gh) @ np.abs(vh).T + go)
                                                          + (2.0 ** -19 * np.abs(inner) if cap else 0.0)) + np.abs(ds) * 2.0 ** -20
-            tol = 1.01 * ((eds + m * 2.0 ** -24 * np.abs(ds)) @ np.abs(kh) + H * np.abs(dq)) + 1e-30
+            tol = 1.01 * ((eds + m * 2.0 ** -24 * np.abs(ds)) @ np.abs(kh) + H * np.abs(dq) + H * go * (H + 2 * ep) * scale * (p @ np.abs(kh))) + 1e-30
             off = np.abs(dQ[q0:q0 + n, h] - dq)
             assert np.all(off <= tol), ("dq", s, h, float((off / tol).max()))
             want_dk[k0:k0 + m, g] += dk
@@ -245,7 +247,7 @@ def test_captured_and_replayed_with_other_boundaries():
     """The launch goes by the tokens and the number of sequences; lengths may change between replays."""
     q, k, v, do = tensors(500, 500, 4, 2, 64, 16)
     bounds = cu([100, 400])
-    ws = torch.empty(4 * 500 * 4, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(16 * 500 * 4 * 130 * 4, dtype=torch.uint8, device=DEV)
 
     def both():
         o, lse = qg.attention_forward(q, k, v, bounds, workspace=ws)
@@ -266,7 +268,7 @@ def test_captured_and_replayed_with_other_boundaries():
 
 
 def test_a_training_pass_against_automatic_differentiation():
-    """The whole formula's gradients (delta from the exact o): o's rounding adds h sum |do| |o| to delta."""
+    """The whole formula's gradients: a rounding of an operand and one of the result, each h / sqrt(3) of the size in the mean."""
     T, d = 130, 64
     q, k, v, do = tensors(T, T, 1, 1, d, 17)
     leaves = [t[:, 0].double().requires_grad_() for t in (q, k, v)]
@@ -277,7 +279,7 @@ def test_a_training_pass_against_automatic_differentiation():
     o, lse = qg.attention_forward(q, k, v)
     got = qg.attention_backward(do, q, k, v, o, lse)
     for g, leaf in zip(got, leaves):
-        assert float((g[:, 0].double() - leaf.grad).norm()) <= 3 * H * float(leaf.grad.norm())
+        assert float((g[:, 0].double() - leaf.grad).norm()) <= 0.9 * H * float(leaf.grad.norm())
 
 
 def test_refusals():
