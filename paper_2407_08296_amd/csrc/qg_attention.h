@@ -131,30 +131,54 @@ struct RowsTile {
     }
 };
 
-// Operand of 32 rows of a tile with k = d: 16 elements from 16 * step on.
-template <int P>
-__device__ __forceinline__ bf16x8 tile_frag(const uint16_t* tile, int row0, int step, int lane) {
-    const int r = lane & 31;
-    const int slot = (2 * step + (lane >> 5)) ^ tile_swizzle<P>(r);
-    return *reinterpret_cast<const bf16x8*>(tile + (row0 + r) * P + slot * 8);
+// Address in LDS of a tile, a multiple of its rows' pitch.
+__device__ __forceinline__ uint32_t tile_address(const uint16_t* tile) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)tile;
 }
-// Operand of 32 elements of d (from 32 * block on) with k = 16 rows of the tile from row0 on, in the order of k of a score's registers.
+// Reads of a tile's operands.  A lane's address is one number per tile: steps and blocks change the slot alone, by exclusive or, and rows are
+// constant offsets.  (Separate addresses for each step and block were 24 registers, of 256 that spill.)
 template <int P>
-__device__ __forceinline__ bf16x8 tile_frag_t(const uint16_t* tile, int row0, int block, int lane) {
-    const int s = lane & 15, g = lane >> 4, r = 4 * (g >> 1) + (s >> 2);
-    const int chunk = block * 4 + 2 * (g & 1) + ((s & 3) >> 1);
-    const uint16_t* lo = tile + (row0 + r) * P + ((chunk ^ tile_swizzle<P>(r)) * 8) + 4 * (s & 1);
-    const uint16_t* hi = tile + (row0 + r + 8) * P + ((chunk ^ tile_swizzle<P>(r + 8)) * 8) + 4 * (s & 1);
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-}
+struct TileReader {
+    uint32_t rows, columns;
+    __device__ __forceinline__ explicit TileReader(int lane) {
+        const int r = lane & 31, s = lane & 15, g = lane >> 4, t = 4 * (g >> 1) + (s >> 2);
+        rows = r * P * 2 + ((lane >> 5) ^ tile_swizzle<P>(r)) * 16;
+        columns = t * P * 2 + ((2 * (g & 1) + ((s & 3) >> 1)) ^ tile_swizzle<P>(t)) * 16 + 8 * (s & 1);
+    }
+    // Operand of 32 rows (from row0 on) with k = d, 16 elements from 16 * step on; at: the tile's address + rows.
+    __device__ __forceinline__ static bf16x8 frag(uint32_t at, int row0, int step) {
+        return *(__attribute__((address_space(3))) const bf16x8*)((at ^ (uint32_t)(step * 32)) + (uint32_t)(row0 * P * 2));
+    }
+    // Operand of 32 elements of d (from 32 * block on) with k = 16 rows from row0 on, in the order of k of a score's registers; at: the tile's
+    // address + columns.
+    __device__ __forceinline__ static bf16x8 frag_t(uint32_t at, int row0, int block) {
+        const uint32_t lo = at ^ (uint32_t)(block * 64), hi = at ^ (uint32_t)(block * 64 ^ (P == 128 ? 32 : 0));    // (8 rows on the swizzle differs by 2)
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lo + (uint32_t)(row0 * P * 2)));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(hi + (uint32_t)((row0 + 8) * P * 2)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
 // The same k = d operand straight from memory: row `row` of `rows`, zero past the end and from d on.
 __device__ __forceinline__ bf16x8 row_frag(const uint16_t* base, int64_t stride, int row, int rows, int step, int d, int lane) {
     const int c = 2 * step + (lane >> 5);
     u32x4 w = {0u, 0u, 0u, 0u};
     if (row < rows && c * 8 < d) w = *reinterpret_cast<const u32x4*>(base + (int64_t)row * stride + c * 8);
     return __builtin_bit_cast(bf16x8, w);
+}
+
+// use(i, operands) for i = 0 .. N - 1, the operands of i + 1 read from LDS before the products of i begin: with 250 of 256 registers taken the
+// compiler reads an operand and waits for it, time after time.  (Two ahead spill: 8192 tokens, 32 heads of 128, dq and dkv 1210 -> 1305 us.)
+template <int N, typename OPERANDS, typename READ, typename USE>
+__device__ __forceinline__ void read_ahead(READ read, USE use) {
+    OPERANDS x[2];
+    read(0, x[0]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + 1 < N) read(i + 1, x[(i + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        use(i, x[i & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Registers 8 t .. 8 t + 7 of a score block as the operand of the next product's step t.  Rounded to bf16, an operand of the matrix unit.

@@ -50,7 +50,7 @@ struct Visible {
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16;
-    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * kAttnStep * P];
+    __shared__ __attribute__((aligned(256))) uint16_t smem[4 * kAttnStep * P];
     int head, t, part;
     if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, false>(a, a.tiles - 1 - t);   // late tiles first: with a causal mask they have most keys
@@ -89,14 +89,19 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
         vt.load(smem + (stage * 2 + 1) * kAttnStep * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
     };
     const float pos = (float)(i + see.shift - 4 * h);     // from the register's key without its 4 h
-    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, bool masked) {
+    using Reader = TileReader<P>;
+    const Reader reader(lane);
+    auto compute = [&](int j0, uint32_t tile, bool masked) {       // tile: K's rows, V's behind them
+        const uint32_t kr = tile + reader.rows, vc = tile + kAttnStep * P * 2 + reader.columns;
         f32x16 s[2];
+        __builtin_amdgcn_s_setprio(kMfmaPrio);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             s[b] = zero16();
 #pragma unroll
-            for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(K, 32 * b, k, lane), qf[k], s[b], 0, 0, 0);
+            for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Reader::frag(kr, 32 * b, k), qf[k], s[b], 0, 0, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
         constexpr bool kScaled = CAP || BIAS;     // s holds x log2(e) then
         float top = -INFINITY;
         if constexpr (kScaled) {
@@ -151,7 +156,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
                 const bf16x8 pf = score_frag(s[b], u);
 #pragma unroll
                 for (int c = 0; c < NB; ++c)
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag_t<P>(V, 32 * b + 16 * u, c, lane), pf, o[c], 0, 0, 0);
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Reader::frag_t(vc, 32 * b + 16 * u, c), pf, o[c], 0, 0, 0);
             }
     };
 
@@ -161,9 +166,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
         lds_barrier();
         if (step + 1 < steps) fetch(step + 1, (step + 1) & 1);
         const int j0 = (first + step) * kAttnStep;
-        const uint16_t *K = smem + (step & 1) * 2 * kAttnStep * P, *V = K + kAttnStep * P;
         if (j0 > wave_hi || j0 + kAttnStep <= wave_lo) continue;
-        compute(j0, K, V, j0 < all_lo || j0 + kAttnStep - 1 > all_hi);
+        compute(j0, tile_address(smem) + (step & 1) * 4 * kAttnStep * P, j0 < all_lo || j0 + kAttnStep - 1 > all_hi);
     }
     l += other_half(l);
     const bool mine = i < seq.nq;
@@ -203,29 +207,43 @@ __global__ __launch_bounds__(256) void k_attention_fwd_join(AttnArgs a) {
     *reinterpret_cast<u32x2*>(a.o + (int64_t)token * a.o_ts + (int64_t)head * a.o_hs + e) = w;
 }
 
-// Of one score: s becomes p, dp becomes p (dp - delta); returns what that is multiplied by for the gradient of scale q.k (1 - tanh^2, or 1).
+// The products of a score begin at what is taken off them: dp at -delta, and s at -lse / scale, where x is linear in it (its rounding then is lse's, as
+// an exponent's offset would have it too).  s becomes p, dp becomes p (dp - delta); returns what that is multiplied by for the gradient of
+// scale q.k (1 - tanh^2, or 1).
 template <bool CAP, bool BIAS>
-__device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float lse2, float delta, float distance) {
+__device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float lse2, float distance) {
     float factor = 1.f;
     if constexpr (!CAP && !BIAS) {
-        s = __builtin_amdgcn_exp2f(__builtin_fmaf(s, rule.c, -lse2));
+        s = __builtin_amdgcn_exp2f(s * rule.c);
     } else {
         float x = score_log2<CAP>(s, rule.c, rule.cap_log2e, factor);
         if constexpr (BIAS) x = __builtin_fmaf(-rule.slope, fabsf(distance), x);
         s = __builtin_amdgcn_exp2f(x - lse2);
     }
-    dp = s * (dp - delta);
+    dp *= s;
     return factor;
 }
 
-// lse as the exponent's offset: a row without a visible key has p = 0.
-__device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// lse as score_gradient and the products' beginnings want it: times log2(e), or -lse / scale.  A row without a visible key has p = 0.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float lse_offset(float lse, const AttnArgs& a) {
+    if constexpr (!CAP && !BIAS) return lse == -INFINITY ? -INFINITY : -lse / a.scale;
+    else return lse == -INFINITY ? INFINITY : lse * kLog2e;
+}
+// (made anew each time: sixteen registers that hold one value all along the loop spill others)
+__device__ __forceinline__ f32x16 all16(float x) {
+    f32x16 z;
+    asm volatile("" : "+v"(x));
+#pragma unroll
+    for (int v = 0; v < 16; ++v) z[v] = x;
+    return z;
+}
 
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
     constexpr bool PARKED = D > 64;
-    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
+    __shared__ __attribute__((aligned(256))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
     uint16_t* const parked = smem + 4 * STEP * P;
     int head, t, part;
     if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
@@ -263,7 +281,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         }
     }
     const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-    const float lse2 = mine ? lse_log2(a.lse[at]) : INFINITY;
+    constexpr bool kPlain = !CAP && !BIAS;
+    const float lse2 = lse_offset<CAP, BIAS>(mine ? a.lse[at] : -INFINITY, a);
     const int lo = see.lo(i), hi = see.hi(i);
     const int first = see.lo(row0) / STEP, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
     const int all = most < 0 ? 0 : most / STEP - first + 1;
@@ -285,20 +304,36 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         vt.load(smem + (stage * 2 + 1) * STEP * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
     };
     const float pos = (float)(i + see.shift - 4 * h);
-    auto compute = [&](int j0, const uint16_t* K, const uint16_t* V, bool masked) {
+    using Reader = TileReader<P>;
+    const Reader reader(lane);
+    auto compute = [&](int j0, uint32_t tile, bool masked) {       // tile: K's rows, V's behind them
+        const uint32_t kr = tile + reader.rows, kc = tile + reader.columns;
+        uint32_t gr = tile_address(parked) + 32 * wave * P * 2 + reader.rows;
+        asm volatile("" : "+v"(gr));       // (not an address per step, kept all along the loop)
 #pragma unroll
         for (int b = 0; b < STEP / 32; ++b) {
-            f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(K, 32 * b, k, lane), qf[k], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(V, 32 * b, k, lane), PARKED ? tile_frag<P>(parked, 32 * wave, k, lane) : gf[PARKED ? 0 : k], dp, 0, 0, 0);
-            }
+            f32x16 s = all16(kPlain ? lse2 : 0.f), dp = all16(-delta);
+            struct Rows {
+                bf16x8 k, v, g;
+            };
+            __builtin_amdgcn_s_setprio(kMfmaPrio);
+            read_ahead<NS, Rows>(
+                [&](int k, Rows& r) {
+                    r.k = Reader::frag(kr, 32 * b, k);
+                    r.v = Reader::frag(kr, STEP + 32 * b, k);
+                    if constexpr (PARKED) r.g = Reader::frag(gr, 0, k);
+                    else r.g = gf[PARKED ? 0 : k];
+                },
+                [&](int k, const Rows& r) {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.k, qf[k], s, 0, 0, 0);
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.v, r.g, dp, 0, 0, 0);
+                });
+            __builtin_amdgcn_s_setprio(0);
             f32x16 factor;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 float p = s[v], g = dp[v];
-                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, lse2, delta, pos - (float)(j0 + 32 * b + acc_row(v)));
+                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, lse2, pos - (float)(j0 + 32 * b + acc_row(v)));
                 s[v] = p;
                 dp[v] = g;
             }
@@ -317,16 +352,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
                 s *= factor;
                 dp *= factor;
             }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bf16x8 df = score_frag(dp, u), pf = score_frag(s, u);
-#pragma unroll
-                for (int c = 0; c < NB; ++c) {
-                    const bf16x8 kf = tile_frag_t<P>(K, 32 * b + 16 * u, c, lane);
-                    dq[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, df, dq[c], 0, 0, 0);
-                    mean[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, pf, mean[c], 0, 0, 0);
-                }
-            }
+            const bf16x8 df[2] = {score_frag(dp, 0), score_frag(dp, 1)}, pf[2] = {score_frag(s, 0), score_frag(s, 1)};
+            __builtin_amdgcn_s_setprio(kMfmaPrio);
+            read_ahead<2 * NB, bf16x8>([&](int n, bf16x8& k) { k = Reader::frag_t(kc, 32 * b + 16 * (n / NB), n % NB); },
+                                            [&](int n, const bf16x8& k) {
+                                                dq[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, df[n / NB], dq[n % NB], 0, 0, 0);
+                                                mean[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, pf[n / NB], mean[n % NB], 0, 0, 0);
+                                            });
+            __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);     // (one block of scores at a time: more of them in flight spill)
         }
     };
@@ -336,9 +369,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         lds_barrier();
         if (step + 1 < steps) fetch(step + 1, (step + 1) & 1);
         const int j0 = (first + step) * STEP;
-        const uint16_t *K = smem + (step & 1) * 2 * STEP * P, *V = K + STEP * P;
         if (j0 > wave_hi || j0 + STEP <= wave_lo) continue;
-        compute(j0, K, V, j0 < all_lo || j0 + STEP - 1 > all_hi);
+        compute(j0, tile_address(smem) + (step & 1) * 4 * STEP * P, j0 < all_lo || j0 + STEP - 1 > all_hi);
     }
     rest += other_half(rest);
     if (a.parts > 1) {
@@ -381,9 +413,9 @@ template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
     constexpr bool PARKED = D > 64;
-    __shared__ __attribute__((aligned(16))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
+    __shared__ __attribute__((aligned(256))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
     uint16_t* const parked = smem + 4 * STEP * P;
-    __shared__ __attribute__((aligned(16))) float stats[2][2][STEP];   // lse and delta of a step's queries
+    __shared__ __attribute__((aligned(16))) float stats[2][2][STEP];   // lse's offset and -delta of a step's queries
     const int heads_k = a.heads_q / a.group;
     int kv, t, part;
     if (!attn_place(heads_k, a.tiles, a.parts, kv, t, part)) return;
@@ -424,37 +456,63 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     RowsTile<P, STEP, 256> qt, gt;
     qt.init(a.q_ts, a.d);
     gt.init(a.do_ts, a.d);
-    auto fetch = [&](int it, int stage) {
-        const int head = kv * a.group + it / steps, i0 = (first + it % steps) * STEP;
+    // step `step` of the queries of head kv * group + `member`, in this order
+    auto fetch = [&](int member, int step, int stage) {
+        const int head = kv * a.group + member, i0 = (first + step) * STEP;
         qt.load(smem + stage * 2 * STEP * P, a.q + (int64_t)(seq.q0 + i0) * a.q_ts + (int64_t)head * a.q_hs, a.q_ts, seq.nq - i0);
         gt.load(smem + (stage * 2 + 1) * STEP * P, a.dO + (int64_t)(seq.q0 + i0) * a.do_ts + (int64_t)head * a.do_hs, a.do_ts, seq.nq - i0);
     };
     // lse and delta of a step: read into registers a step ahead, put into LDS with the barrier
     float stat = 0.f;
-    auto fetch_stats = [&](int it) {
-        const int head = kv * a.group + it / steps, i = (first + it % steps) * STEP + (threadIdx.x & (STEP - 1));
+    auto fetch_stats = [&](int member, int step) {
+        const int head = kv * a.group + member, i = (first + step) * STEP + (threadIdx.x & (STEP - 1));
         const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-        if (threadIdx.x < STEP) stat = i < seq.nq ? lse_log2(a.lse[at]) : INFINITY;
-        else if (threadIdx.x < 2 * STEP) stat = i < seq.nq ? a.delta[at] : 0.f;
+        if (threadIdx.x < STEP) stat = lse_offset<CAP, BIAS>(i < seq.nq ? a.lse[at] : -INFINITY, a);
+        else if (threadIdx.x < 2 * STEP) stat = i < seq.nq ? -a.delta[at] : 0.f;
     };
     const float pos = (float)(j - see.shift - 4 * h);      // the distance from a register's query without its 4 h
-    auto compute = [&](int i0, const uint16_t* Q, const uint16_t* G, const float (*st)[STEP], const ScoreRule& rule, bool masked) {
+    using Reader = TileReader<P>;
+    const Reader reader(lane);
+    auto compute = [&](int i0, uint32_t tile, const float (*st)[STEP], const ScoreRule& rule, bool masked) {       // tile: Q's rows, dO's behind them
+        const uint32_t qr = tile + reader.rows, qc = tile + reader.columns;
+        uint32_t vr = tile_address(parked) + 32 * wave * P * 2 + reader.rows;
+        asm volatile("" : "+v"(vr));       // (not an address per step, kept all along the loop)
 #pragma unroll
         for (int b = 0; b < STEP / 32; ++b) {
-            f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(Q, 32 * b, k, lane), kf[k], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag<P>(G, 32 * b, k, lane), PARKED ? tile_frag<P>(parked, 32 * wave, k, lane) : vf[PARKED ? 0 : k], dp, 0, 0, 0);
-            }
+            f32x16 s, dp;
+            f32x4 lse2[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
+                lse2[r] = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(&st[1][32 * b + 8 * r + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    s[4 * r + e] = CAP || BIAS ? 0.f : lse2[r][e];
+                    dp[4 * r + e] = delta[e];
+                }
+            }
+            struct Rows {
+                bf16x8 q, g, v;
+            };
+            __builtin_amdgcn_s_setprio(kMfmaPrio);
+            read_ahead<NS, Rows>(
+                [&](int k, Rows& r) {
+                    r.q = Reader::frag(qr, 32 * b, k);
+                    r.g = Reader::frag(qr, STEP + 32 * b, k);
+                    if constexpr (PARKED) r.v = Reader::frag(vr, 0, k);
+                    else r.v = vf[PARKED ? 0 : k];
+                },
+                [&](int k, const Rows& r) {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.q, kf[k], s, 0, 0, 0);
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.g, r.v, dp, 0, 0, 0);
+                });
+            __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
                     float p = s[4 * r + e], g = dp[4 * r + e];
-                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, lse2[e], delta[e], (float)(i0 + 32 * b + 8 * r + e) - pos);
+                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, lse2[r][e], (float)(i0 + 32 * b + 8 * r + e) - pos);
                     s[4 * r + e] = p;
                     dp[4 * r + e] = CAP ? g * factor : g;
                 }
@@ -468,36 +526,46 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
                     dp[v] = seen ? dp[v] : 0.f;
                 }
             }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bf16x8 pf = score_frag(s, u), df = score_frag(dp, u);
-#pragma unroll
-                for (int c = 0; c < NB; ++c) {
-                    dv[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag_t<P>(G, 32 * b + 16 * u, c, lane), pf, dv[c], 0, 0, 0);
-                    dk[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_frag_t<P>(Q, 32 * b + 16 * u, c, lane), df, dk[c], 0, 0, 0);
-                }
-            }
+            const bf16x8 pf[2] = {score_frag(s, 0), score_frag(s, 1)}, df[2] = {score_frag(dp, 0), score_frag(dp, 1)};
+            struct Columns {
+                bf16x8 g, q;
+            };
+            __builtin_amdgcn_s_setprio(kMfmaPrio);
+            read_ahead<2 * NB, Columns>(
+                [&](int n, Columns& r) {
+                    r.g = Reader::frag_t(qc, STEP + 32 * b + 16 * (n / NB), n % NB);
+                    r.q = Reader::frag_t(qc, 32 * b + 16 * (n / NB), n % NB);
+                },
+                [&](int n, const Columns& r) {
+                    dv[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.g, pf[n / NB], dv[n % NB], 0, 0, 0);
+                    dk[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.q, df[n / NB], dk[n % NB], 0, 0, 0);
+                });
+            __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    int member = steps > 0 ? begin / steps : 0, step = begin - member * steps;
     if (total > begin) {
-        fetch(begin, begin & 1);
-        fetch_stats(begin);
+        fetch(member, step, begin & 1);
+        fetch_stats(member, step);
     }
     const int last_key = min(w0 + 31, seq.nk - 1);
     for (int it = begin; it < total; ++it) {
         wait_loads<0>();
         if (threadIdx.x < 2 * STEP) stats[it & 1][threadIdx.x / STEP][threadIdx.x & (STEP - 1)] = stat;
         lds_barrier();
-        if (it + 1 < total) {
-            fetch(it + 1, (it + 1) & 1);
-            fetch_stats(it + 1);
+        const int now = kv * a.group + member, i0 = (first + step) * STEP, i1 = min(i0 + STEP, seq.nq) - 1;
+        if (++step == steps) {
+            step = 0;
+            ++member;
         }
-        const int i0 = (first + it % steps) * STEP, i1 = min(i0 + STEP, seq.nq) - 1;
-        const uint16_t *Q = smem + (it & 1) * 2 * STEP * P, *G = Q + STEP * P;
+        if (it + 1 < total) {
+            fetch(member, step, (it + 1) & 1);
+            fetch_stats(member, step);
+        }
         if (w0 >= seq.nk || see.hi(i1) < w0 || see.lo(i0) > last_key) continue;
-        const ScoreRule rule = score_rule<CAP, BIAS>(a, kv * a.group + it / steps);
-        compute(i0, Q, G, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key);
+        const ScoreRule rule = score_rule<CAP, BIAS>(a, now);
+        compute(i0, tile_address(smem) + (it & 1) * 4 * STEP * P, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key);
     }
     const bool mine = j < seq.nk;
     if (a.parts > 1) {
@@ -549,7 +617,7 @@ static int check_attention(const qg_attention* a) {
     if (a->heads_q <= 0 || a->heads_k <= 0 || a->heads_q % a->heads_k != 0 || a->heads_q > kAttnMaxHeads) return QG_ERR_SHAPE;
     if (a->d <= 0 || a->d > 128 || a->d % 8 != 0 || a->sequences <= 0 || a->sequences > kAttnMaxSequences) return QG_ERR_SHAPE;
     if (a->cu_k == nullptr && a->cu_q != nullptr && a->tokens_q != a->tokens_k) return QG_ERR_SHAPE;
-    if (!(a->scale > 0.f && a->scale < INFINITY) || !(a->cap >= 0.f && a->cap < INFINITY)) return QG_ERR_SHAPE;
+    if (!(a->scale >= 0x1p-60f && a->scale <= 0x1p60f) || !(a->cap >= 0.f && a->cap < INFINITY)) return QG_ERR_SHAPE;
     if (a->window < 0 || (!a->causal && (a->window > 0 || a->prefix != nullptr)) || (a->window > 0 && a->prefix != nullptr)) return QG_ERR_SHAPE;
     for (const void* p : {(const void*)a->cu_q, (const void*)a->cu_k, (const void*)a->prefix, (const void*)a->slopes})
         if (reinterpret_cast<uintptr_t>(p) & 3) return QG_ERR_ALIGN;

@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a cache in pages: o = softmax_j(x_j) v_j over positions j = first .. length - 1.
 // The cache is read once, 4 d bytes per key head and position: HBM is the bound, and what counts is how many bytes are on their way.  The
 // query heads that share a key head are taken together, up to 16 as the columns of a 16 x 16 x 32 product (one alone leaves 15
-// columns empty: at 8 TB/s that is still 5 % of the matrix pipe).  A sequence is cut into parts of kPart positions for as many workgroups,
+// columns empty: at 8 TB/s that is still 5 % of the matrix pipe).  A sequence is cut into parts for as many workgroups,
 // whose results are joined by a second kernel; a workgroup's waves take 32 positions each in turn, each with tiles, maximum and sums of
 // its own, so that nothing waits for another wave before the end.
 //   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
@@ -10,7 +10,6 @@
 
 namespace qg {
 
-constexpr int kPart = 512;                  // positions of a workgroup
 constexpr int kPagedStep = 32;              // ... of a wave at a time
 
 struct PagedArgs {
@@ -18,9 +17,9 @@ struct PagedArgs {
     uint16_t* o;
     const int32_t *table, *lengths;
     const float* slopes;
-    float* part;                            // [sequences][heads_q][parts][d + 2]: sums, maximum (log2), sum
+    float* part;                            // [sequences][heads_q][parts][d] sums, then [..][2]: maximum (log2), sum
     int64_t q_ts, q_hs, o_ts, o_hs, pages;
-    int page_size, heads_k, group, d, sequences, width, parts, window;
+    int page_size, heads_k, group, d, sequences, width, parts, part_length, window;
     float scale, cap;
 };
 
@@ -44,7 +43,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     int first, end;
     paged_range(a, seq, first, end);
     const int whole_first = first / kPagedStep * kPagedStep;     // parts begin at whole steps
-    const int begin = whole_first + part * kPart, stop = min(end, begin + kPart);
+    const int begin = whole_first + part * a.part_length, stop = min(end, begin + a.part_length);
     if (part > 0 && begin >= end) return;                        // (part 0 of an empty sequence still writes its zeros)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int head = kv * a.group + hg * 16 + col;
@@ -216,52 +215,86 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
             to[0] = pack_bf16x2(x[0] * f, x[1] * f);
             to[1] = pack_bf16x2(x[2] * f, x[3] * f);
         } else {
-            float* to = a.part + (((int64_t)seq * a.heads_k * a.group + h) * a.parts + part) * (a.d + 2);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) to[e + i] = x[i];
+            const int64_t row = ((int64_t)seq * a.heads_k * a.group + h) * a.parts + part;
+            *reinterpret_cast<f32x4*>(a.part + row * a.d + e) = x;
             if (e == 0) {
-                to[a.d] = top;
-                to[a.d + 1] = sum;
+                float* to = a.part + (int64_t)a.sequences * a.heads_k * a.group * a.parts * a.d + 2 * row;
+                to[0] = top;
+                to[1] = sum;
             }
         }
     }
 }
 
-// Joins the parts of a sequence's heads, in their order: a wave per head, two elements per lane.
+// Joins the parts of a sequence's heads in a fixed order: WAVES waves per head, of each 64 / (d / 4) parts at once, four elements per lane.
+template <int WAVES>
 __global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
-    const int heads = a.heads_k * a.group;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= (int64_t)a.sequences * heads) return;
-    const int seq = (int)(unit / heads), h = (int)(unit - (int64_t)seq * heads), lane = threadIdx.x & 63;
+    constexpr int HEADS = 4 / WAVES;
+    __shared__ __attribute__((aligned(16))) float sums[4][128 + 4];
+    const int heads = a.heads_k * a.group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % WAVES;
+    const int64_t unit = min((int64_t)blockIdx.x * HEADS + wave / WAVES, (int64_t)a.sequences * heads - 1);
+    const int seq = (int)(unit / heads), h = (int)(unit - (int64_t)seq * heads);
     int first, end;
     paged_range(a, seq, first, end);
-    const int parts = max(1, (end - first / kPagedStep * kPagedStep + kPart - 1) / kPart);
-    const float* from = a.part + unit * a.parts * (a.d + 2);
-    const int e = 2 * lane, at = min(e, a.d - 2);
+    const int parts = max(1, (end - first / kPagedStep * kPagedStep + a.part_length - 1) / a.part_length);
+    const float *from = a.part + unit * a.parts * a.d, *stat = a.part + (int64_t)a.sequences * heads * a.parts * a.d + 2 * unit * a.parts;
+    const int per = a.d / 4, at_once = 64 / per, e = lane % per * 4, mine = lane / per;
     float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, from[(int64_t)p * (a.d + 2) + a.d]);
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, stat[2 * p]);
     top = wave_max(top);
     const float ref = top == -INFINITY ? 0.f : top;
-    float x = 0.f, y = 0.f, sum = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    if (mine < at_once)
 #pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const float* one = from + (int64_t)p * (a.d + 2);
-        const float f = __builtin_amdgcn_exp2f(one[a.d] - ref);
-        sum = __builtin_fmaf(one[a.d + 1], f, sum);
-        x = __builtin_fmaf(one[at], f, x);
-        y = __builtin_fmaf(one[at + 1], f, y);
+        for (int p = w * at_once + mine; p < parts; p += WAVES * at_once) {
+            const float f = __builtin_amdgcn_exp2f(stat[2 * p] - ref);
+            sum = __builtin_fmaf(stat[2 * p + 1], f, sum);
+            x += *reinterpret_cast<const f32x4*>(from + (int64_t)p * a.d + e) * f;
+        }
+    // the parts of a wave, then the waves
+    float y[5] = {x[0], x[1], x[2], x[3], sum};
+    for (int o = 1; o < at_once; ++o)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const float v = __shfl(i < 4 ? x[i & 3] : sum, lane % per + o * per, 64);
+            y[i] += v;
+        }
+    if constexpr (WAVES > 1) {
+        if (mine == 0) *reinterpret_cast<f32x4*>(&sums[wave][e]) = f32x4{y[0], y[1], y[2], y[3]};
+        if (lane == 0) sums[wave][128] = y[4];
+        __syncthreads();
+        if (w != 0) return;
+#pragma unroll
+        for (int o = 1; o < WAVES; ++o) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += sums[wave + o][min(e, 124) + i];
+            y[4] += sums[wave + o][128];
+        }
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    if (e < a.d) *reinterpret_cast<uint32_t*>(a.o + (int64_t)seq * a.o_ts + (int64_t)h * a.o_hs + e) = pack_bf16x2(x * f, y * f);
+    if (mine != 0) return;
+    const float f = y[4] == 0.f ? 0.f : 1.f / y[4];
+    const u32x2 o = {pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f)};
+    *reinterpret_cast<u32x2*>(a.o + (int64_t)seq * a.o_ts + (int64_t)h * a.o_hs + e) = o;
 }
 
-static int64_t paged_parts(const qg_cache* c) { return ((int64_t)c->width * c->page_size + kPagedStep - 1 + kPart - 1) / kPart; }
+// Positions of a workgroup: 512, and 256 where that leaves fewer than 512 workgroups (us with 256 / 512 / 1024: 128 sequences of up to 1000, 8 heads
+// on one: 14.7 / 16.4 / 16.4; one of 32768, 8 key heads of 128: 35.1 / 34.2 / 34.0; 64 of up to 4096, 16 of 64: - / 37.1 / 39.5; 8 of up to 8000, 32 of
+// 128: - / 136 / 138).
+static int part_length(const qg_cache* c, int heads_q) {
+    const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16);
+    return units * c->width * c->page_size < 512 * 512 ? 256 : 512;
+}
+static int64_t paged_parts(const qg_cache* c, int heads_q) {
+    const int length = part_length(c, heads_q);
+    return ((int64_t)c->width * c->page_size + kPagedStep - 1 + length - 1) / length;
+}
 
 static int check_paged(const qg_cache* c, int heads_q) {
     if (int e = check_cache(c)) return e;
     if (c->d > 128 || heads_q <= 0 || heads_q > kAttnMaxHeads || heads_q % c->heads != 0) return QG_ERR_SHAPE;
     const int64_t groups = (heads_q / c->heads + 15) / 16;
-    if (paged_parts(c) * c->sequences * c->heads * groups >= (int64_t(1) << 24)) return QG_ERR_SHAPE;   // (2^32 threads in a launch)
+    if (paged_parts(c, heads_q) * c->sequences * c->heads * groups >= (int64_t(1) << 24)) return QG_ERR_SHAPE;   // (2^32 threads in a launch)
     return QG_OK;
 }
 
@@ -271,7 +304,7 @@ using namespace qg;
 
 extern "C" size_t qg_attention_paged_workspace_bytes(const qg_cache* c, int heads_q) {
     if (check_paged(c, heads_q) != QG_OK) return 0;
-    return ((size_t)paged_parts(c) * c->sequences * heads_q * (c->d + 2) * 4 + 15) / 16 * 16;
+    return ((size_t)paged_parts(c, heads_q) * c->sequences * heads_q * (c->d + 2) * 4 + 15) / 16 * 16;
 }
 
 extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, const qg_heads* q, int heads_q, float scale, float cap, int64_t window,
@@ -288,7 +321,7 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     a.o = o->data, a.o_ts = o->token_stride, a.o_hs = o->head_stride;
     a.k = c->k, a.v = c->v, a.table = c->table, a.lengths = lengths, a.slopes = slopes, a.part = static_cast<float*>(workspace);
     a.pages = c->pages, a.page_size = c->page_size, a.heads_k = c->heads, a.group = heads_q / c->heads, a.d = c->d;
-    a.sequences = c->sequences, a.width = c->width, a.parts = (int)paged_parts(c);
+    a.sequences = c->sequences, a.width = c->width, a.parts = (int)paged_parts(c, heads_q), a.part_length = part_length(c, heads_q);
     a.window = (int)(window < (int64_t(1) << 31) ? window : 0);
     a.scale = scale, a.cap = cap;
     const unsigned grid = (unsigned)((int64_t)a.parts * a.sequences * a.heads_k * ((a.group + 15) / 16));
@@ -301,7 +334,8 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     };
     auto with_bias = [&](auto cp) { slopes != nullptr ? with_d(cp, std::true_type()) : with_d(cp, std::false_type()); };
     cap > 0.f ? with_bias(std::true_type()) : with_bias(std::false_type());
-    if (a.parts > 1)
-        hipLaunchKernelGGL(k_attention_join, dim3((unsigned)(((int64_t)a.sequences * heads_q + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
+    const int64_t heads = (int64_t)a.sequences * heads_q;
+    if (a.parts > 16) hipLaunchKernelGGL(k_attention_join<4>, dim3((unsigned)heads), dim3(256), 0, (hipStream_t)stream, a);
+    else if (a.parts > 1) hipLaunchKernelGGL(k_attention_join<1>, dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
     return check_launch();
 }

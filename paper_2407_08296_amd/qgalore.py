@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -68,19 +69,11 @@ class RefreshDesc(C.Structure):
                 ("Ps_new", C.c_void_p)]
 
 
-class Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
-
-
-class Attention(C.Structure):
-    _fields_ = [("tokens_q", C.c_int64), ("tokens_k", C.c_int64), ("heads_q", C.c_int), ("heads_k", C.c_int), ("d", C.c_int),
-                ("sequences", C.c_int), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p), ("prefix", C.c_void_p), ("slopes", C.c_void_p),
-                ("scale", C.c_float), ("cap", C.c_float), ("causal", C.c_int), ("window", C.c_int64)]
-
-
-class Cache(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("pages", C.c_int64), ("page_size", C.c_int), ("heads", C.c_int),
-                ("d", C.c_int), ("sequences", C.c_int), ("width", C.c_int)]
+# qg_heads, qg_attention and qg_cache as bytes, the fields in the header's order and alignment (packed in 0.2 us where a ctypes structure and its
+# pointer take 0.9 of the 10 us of a small call, which has up to nine of them)
+_pack_heads = struct.Struct("@Pqq").pack
+_pack_attention = struct.Struct("@qqiiiiPPPPffiq").pack
+_pack_cache = struct.Struct("@PPPqiiiii").pack
 
 
 _lib = None
@@ -176,7 +169,8 @@ def lib() -> C.CDLL:
         L.qg_head_loss_workspace_bytes.argtypes = [i64, i64, i64]
         L.qg_head_loss_forward.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
         L.qg_head_loss_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, vp]
-        heads, attention, cache, f64 = C.POINTER(Heads), C.POINTER(Attention), C.POINTER(Cache), C.c_double
+        heads = attention = cache = vp          # their bytes
+        f64 = C.c_double
         L.qg_rope_frequencies.argtypes = [i32, f64, f64, f64, f64, f64, vp]
         L.qg_rope_forward.argtypes = [heads, i32, heads, i32, vp, vp, i64, i32, i32, i32, f32, heads, heads, vp]
         L.qg_rope_backward.argtypes = L.qg_rope_forward.argtypes
@@ -790,9 +784,9 @@ def _heads(t: torch.Tensor | None):
     if t.dtype not in _BF16:
         raise QGError(f"dtype {t.dtype} not in {_BF16}")
     ts, hs, es = t.stride()
-    if es != 1 and t.shape[2] != 1:
+    if es != 1:
         raise QGError("elements of a head are expected next to each other")
-    return C.byref(Heads(t.data_ptr(), ts, hs))
+    return _pack_heads(t.data_ptr(), ts, hs)
 
 
 def _written(t: torch.Tensor | None, like: torch.Tensor, what: str) -> torch.Tensor:
@@ -800,7 +794,7 @@ def _written(t: torch.Tensor | None, like: torch.Tensor, what: str) -> torch.Ten
     if t is None:
         return like.new_empty(like.shape)
     _expect(t, *like.shape)
-    if any(st == 0 and n > 1 for st, n in zip(t.stride(), t.shape)):
+    if 0 in t.stride() and any(st == 0 and n > 1 for st, n in zip(t.stride(), t.shape)):
         raise QGError(f"{what}: an expanded tensor cannot be written")
     return t
 
@@ -846,7 +840,7 @@ def rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor | None, positions: 
     return _rope(lib().qg_rope_backward, dq_out, dk_out, positions, freqs, layout, amplitude, out)
 
 
-def _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix) -> Attention:
+def _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix) -> bytes:
     tokens, heads, d = q.shape
     tokens_k, heads_k, _ = k.shape
     _expect(k, tokens_k, heads_k, d)
@@ -856,8 +850,11 @@ def _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix) 
     _expect(cu_k, sequences + 1)
     _expect(prefix, sequences)
     _expect(slopes, heads)
-    return Attention(tokens, tokens_k, heads, heads_k, d, sequences, _ptr(cu_q, _I32), _ptr(cu_k, _I32), _ptr(prefix, _I32),
-                     _ptr(slopes, _F32), d ** -0.5 if scale is None else scale, cap, int(causal), window)
+    try:
+        return _pack_attention(tokens, tokens_k, heads, heads_k, d, sequences, _ptr(cu_q, _I32) or 0, _ptr(cu_k, _I32) or 0, _ptr(prefix, _I32) or 0,
+                               _ptr(slopes, _F32) or 0, d ** -0.5 if scale is None else scale, cap, int(causal), window)
+    except (OverflowError, struct.error) as e:
+        raise QGError(f"libqgalore: {e}") from None
 
 
 def _workspace(nbytes: int, like: torch.Tensor, given: torch.Tensor | None):
@@ -878,9 +875,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: t
     scale: d^-0.5 if None; cap, slopes (fp32 [heads]), window, prefix (int32 [sequences]): as in qg_attention_forward."""
     a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
     o = _written(out, q, "out")
-    lse = torch.empty(a.heads_q, a.tokens_q, dtype=torch.float32, device=q.device)
-    ws, *at = _workspace(lib().qg_attention_forward_workspace_bytes(C.byref(a)), q, workspace)
-    _check(lib().qg_attention_forward(C.byref(a), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *at, _stream()))
+    lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32)
+    ws, *at = _workspace(lib().qg_attention_forward_workspace_bytes(a), q, workspace)
+    _check(lib().qg_attention_forward(a, _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *at, _stream()))
     return o, lse
 
 
@@ -893,19 +890,19 @@ def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
     for t in (do, o):
         _expect(t, *q.shape)
-    _expect(lse, a.heads_q, a.tokens_q)
+    _expect(lse, q.shape[1], q.shape[0])
     dq, dk, dv = (_written(None if out is None else out[i], t, "out") for i, t in enumerate((q, k, v)))
-    ws, *at = _workspace(lib().qg_attention_backward_workspace_bytes(C.byref(a)), q, workspace)
-    _check(lib().qg_attention_backward(C.byref(a), _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse, _F32), _heads(dq),
+    ws, *at = _workspace(lib().qg_attention_backward_workspace_bytes(a), q, workspace)
+    _check(lib().qg_attention_backward(a, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse, _F32), _heads(dq),
                                        _heads(dk), _heads(dv), *at, _stream()))
     return dq, dk, dv
 
 
-def _cache(k_pages, v_pages, table) -> Cache:
+def _cache(k_pages, v_pages, table) -> bytes:
     pages, page_size, heads, d = k_pages.shape
     _expect(v_pages, pages, page_size, heads, d)
     sequences, width = table.shape
-    return Cache(_ptr(k_pages, _BF16), _ptr(v_pages, _BF16), _ptr(table, _I32), pages, page_size, heads, d, sequences, width)
+    return _pack_cache(_ptr(k_pages, _BF16), _ptr(v_pages, _BF16), _ptr(table, _I32), pages, page_size, heads, d, sequences, width)
 
 
 def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, k_pages: torch.Tensor,
@@ -916,8 +913,9 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posit
     way if freqs is given, and so is q, which is returned (None without q).  out: where q goes (q itself: in place)."""
     c = _cache(k_pages, v_pages, table)
     tokens = k.shape[0]
-    _expect(k, tokens, c.heads, c.d)
-    _expect(v, tokens, c.heads, c.d)
+    heads, d = k_pages.shape[2:]
+    _expect(k, tokens, heads, d)
+    _expect(v, tokens, heads, d)
     _expect(positions, tokens)
     _expect(sequence, tokens)
     rot = 0
@@ -926,9 +924,9 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posit
         _expect(freqs, rot // 2)
     q_out = None
     if q is not None:
-        _expect(q, tokens, q.shape[1], c.d)
+        _expect(q, tokens, q.shape[1], d)
         q_out = _written(out, q, "out")
-    _check(lib().qg_cache_append(C.byref(c), _heads(q), 0 if q is None else q.shape[1], _heads(k), _heads(v), _ptr(positions, _I64),
+    _check(lib().qg_cache_append(c, _heads(q), 0 if q is None else q.shape[1], _heads(k), _heads(v), _ptr(positions, _I64),
                                  _ptr(sequence, _I32), tokens, _ptr(freqs, _F64), rot, _rope_layout(layout), amplitude, _heads(q_out), _stream()))
     return q_out
 
@@ -939,13 +937,13 @@ def attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     """Attention of one new token per sequence, q [sequences][heads][d], over the first lengths[s] (int32) positions of its pages; the token is
     the last of them.  Returns o [sequences][heads][d].  workspace: uint8, qg_attention_paged_workspace_bytes of them (allocated if None)."""
     c = _cache(k_pages, v_pages, table)
-    heads = q.shape[1]
-    _expect(q, c.sequences, heads, c.d)
-    _expect(lengths, c.sequences)
+    sequences, heads, d = table.shape[0], q.shape[1], k_pages.shape[3]
+    _expect(q, sequences, heads, d)
+    _expect(lengths, sequences)
     _expect(slopes, heads)
     o = _written(out, q, "out")
-    ws, *at = _workspace(lib().qg_attention_paged_workspace_bytes(C.byref(c), heads), q, workspace)
-    _check(lib().qg_attention_paged(C.byref(c), _ptr(lengths, _I32), _heads(q), heads, c.d ** -0.5 if scale is None else scale, cap, window,
+    ws, *at = _workspace(lib().qg_attention_paged_workspace_bytes(c, heads), q, workspace)
+    _check(lib().qg_attention_paged(c, _ptr(lengths, _I32), _heads(q), heads, d ** -0.5 if scale is None else scale, cap, window,
                                     _ptr(slopes, _F32), _heads(o), *at, _stream()))
     return o
 
