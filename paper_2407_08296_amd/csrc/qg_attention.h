@@ -30,7 +30,7 @@ struct AttnArgs {
     const uint16_t *q, *k, *v, *dO;
     uint16_t *o, *dq, *dk, *dv;
     float* lse;          // [heads_q][tokens_q]
-    float* delta;        // ... rowsum(dO o)
+    float* stats;        // [2][heads_q][tokens_q]: what dkv begins the products at
     const int32_t *cu_q, *cu_k, *prefix;
     const float* slopes;
     float* part;         // sums of parts, to be joined (see qg_attention.hip)
@@ -42,7 +42,7 @@ struct AttnArgs {
 struct AttnTile {
     int seq;       // `sequences`: the rows behind the last sequence
     int tile;      // of the sequence
-    int q0, nq, k0, nk;
+    int q0, nq, k0, nk, prefix;
 };
 
 // Boundary i of packed sequences, inside the tokens whatever memory holds.
@@ -81,6 +81,7 @@ __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, int t) {
     const int k1 = tail ? a.tokens_k : attn_boundary(a.cu_k, lo + 1, a.sequences, a.tokens_k);
     r.nq = tail && KEYS ? 0 : max(0, q1 - r.q0);
     r.nk = tail && !KEYS ? 0 : max(0, k1 - r.k0);
+    r.prefix = a.prefix != nullptr && !tail ? a.prefix[lo] : 0;
     return r;
 }
 

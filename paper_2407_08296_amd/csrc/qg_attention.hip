@@ -17,6 +17,8 @@ constexpr int kAttnStep = 64;      // rows that pass by, per step
 
 template <int D>
 constexpr int attn_pitch() { return D <= 64 ? 64 : 128; }
+// Rows per step of the backward passes: beyond d = 64, 32 of them leave room in LDS for dO's (V's) rows and a second workgroup.  (Three or four steps in
+// LDS instead of two: the same times for 16 sequences of 256 tokens and for one of 8192.)
 template <int D>
 constexpr int attn_back_step() { return D <= 64 ? 64 : 32; }
 
@@ -40,7 +42,7 @@ struct Visible {
         shift = t.nk - t.nq;
         last = t.nk - 1;
         causal = a.causal;
-        prefix = a.prefix != nullptr && t.seq < a.sequences ? a.prefix[t.seq] : 0;
+        prefix = t.prefix;
         window = a.window;
     }
     __device__ __forceinline__ int hi(int i) const { return causal ? min(last, max(i + shift, prefix - 1)) : last; }
@@ -207,36 +209,20 @@ __global__ __launch_bounds__(256) void k_attention_fwd_join(AttnArgs a) {
     *reinterpret_cast<u32x2*>(a.o + (int64_t)token * a.o_ts + (int64_t)head * a.o_hs + e) = w;
 }
 
-// The products of a score begin at what is taken off them: dp at -delta, and s at -lse / scale, where x is linear in it (its rounding then is lse's, as
-// an exponent's offset would have it too).  s becomes p, dp becomes p (dp - delta); returns what that is multiplied by for the gradient of
-// scale q.k (1 - tanh^2, or 1).
+// s, a product, becomes p = exp2(x - lse), the exponent being s c + offset where x is linear in it and x + offset else; dp, less delta, becomes p (dp -
+// delta).  Returns what that is multiplied by for the gradient of scale q.k (1 - tanh^2, or 1).
 template <bool CAP, bool BIAS>
-__device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float lse2, float distance) {
+__device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float offset, float distance) {
     float factor = 1.f;
     if constexpr (!CAP && !BIAS) {
-        s = __builtin_amdgcn_exp2f(s * rule.c);
+        s = __builtin_amdgcn_exp2f(__builtin_fmaf(s, rule.c, offset));
     } else {
         float x = score_log2<CAP>(s, rule.c, rule.cap_log2e, factor);
         if constexpr (BIAS) x = __builtin_fmaf(-rule.slope, fabsf(distance), x);
-        s = __builtin_amdgcn_exp2f(x - lse2);
+        s = __builtin_amdgcn_exp2f(x + offset);
     }
     dp *= s;
     return factor;
-}
-
-// lse as score_gradient and the products' beginnings want it: times log2(e), or -lse / scale.  A row without a visible key has p = 0.
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ float lse_offset(float lse, const AttnArgs& a) {
-    if constexpr (!CAP && !BIAS) return lse == -INFINITY ? -INFINITY : -lse / a.scale;
-    else return lse == -INFINITY ? INFINITY : lse * kLog2e;
-}
-// (made anew each time: sixteen registers that hold one value all along the loop spill others)
-__device__ __forceinline__ f32x16 all16(float x) {
-    f32x16 z;
-    asm volatile("" : "+v"(x));
-#pragma unroll
-    for (int v = 0; v < 16; ++v) z[v] = x;
-    return z;
 }
 
 template <int D, bool CAP, bool BIAS>
@@ -281,8 +267,16 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         }
     }
     const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-    constexpr bool kPlain = !CAP && !BIAS;
-    const float lse2 = lse_offset<CAP, BIAS>(mine ? a.lse[at] : -INFINITY, a);
+    // a row without a visible key, or none, has p = 0: its offset is -inf
+    const float lse = mine ? a.lse[at] : -INFINITY, offset = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+    // For dkv, which begins its products at them, in accumulators read from LDS: -delta, and the offset in terms of the product where x is linear in it
+    // (its rounding then is the one it has in the exponent too).
+    auto keep_stats = [&](float d) {
+        if (mine && h == 0) {
+            a.stats[at] = CAP || BIAS ? offset : lse == -INFINITY ? -INFINITY : -lse / a.scale;
+            a.stats[(int64_t)a.heads_q * a.tokens_q + at] = -d;
+        }
+    };
     const int lo = see.lo(i), hi = see.hi(i);
     const int first = see.lo(row0) / STEP, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
     const int all = most < 0 ? 0 : most / STEP - first + 1;
@@ -312,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         asm volatile("" : "+v"(gr));       // (not an address per step, kept all along the loop)
 #pragma unroll
         for (int b = 0; b < STEP / 32; ++b) {
-            f32x16 s = all16(kPlain ? lse2 : 0.f), dp = all16(-delta);
+            f32x16 s = zero16(), dp = zero16();
             struct Rows {
                 bf16x8 k, v, g;
             };
@@ -332,8 +326,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
             f32x16 factor;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                float p = s[v], g = dp[v];
-                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, lse2, pos - (float)(j0 + 32 * b + acc_row(v)));
+                float p = s[v], g = dp[v] - delta;
+                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, offset, pos - (float)(j0 + 32 * b + acc_row(v)));
                 s[v] = p;
                 dp[v] = g;
             }
@@ -341,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int j = j0 + 32 * b + acc_row(v) + 4 * h;
-                    const bool seen = j >= lo && j <= hi;
+                    const bool seen = (j >= lo) & (j <= hi);
                     s[v] = seen ? s[v] : 0.f;
                     dp[v] = seen ? dp[v] : 0.f;
                 }
@@ -378,14 +372,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         store_part(dq, a.part + row * a.d, a.d, mine, lane);
         store_part(mean, a.part + (rows + row) * a.d, a.d, mine, lane);
         if (mine && h == 0) a.part[2 * rows * a.d + row] = rest;
-        if (mine && h == 0 && part == 0) a.delta[at] = delta;
+        if (part == 0) keep_stats(delta);
         return;
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) dq[b][v] = __builtin_fmaf(-rest, mean[b][v], dq[b][v]);
-    if (mine && h == 0) a.delta[at] = delta + rest;
+    keep_stats(delta + rest);
     store_columns(dq, a.scale, a.dq + (int64_t)(seq.q0 + i) * a.dq_ts + (int64_t)head * a.dq_hs, a.d, mine, lane);
 }
 
@@ -404,7 +398,7 @@ __global__ __launch_bounds__(256) void k_attention_dq_join(AttnArgs a) {
         rest += a.part[2 * rows * a.parts * a.d + rows * p + row];
     }
     x = (x - mean * rest) * a.scale;
-    if (e == 0) a.delta[row] += rest;
+    if (e == 0) a.stats[rows + row] -= rest;
     const u32x2 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
     *reinterpret_cast<u32x2*>(a.dq + (int64_t)token * a.dq_ts + (int64_t)head * a.dq_hs + e) = w;
 }
@@ -415,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     constexpr bool PARKED = D > 64;
     __shared__ __attribute__((aligned(256))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
     uint16_t* const parked = smem + 4 * STEP * P;
-    __shared__ __attribute__((aligned(16))) float stats[2][2][STEP];   // lse's offset and -delta of a step's queries
+    __shared__ __attribute__((aligned(16))) float stats[2][2][64];     // of a step's queries
     const int heads_k = a.heads_q / a.group;
     int kv, t, part;
     if (!attn_place(heads_k, a.tiles, a.parts, kv, t, part)) return;
@@ -461,33 +455,32 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
         const int head = kv * a.group + member, i0 = (first + step) * STEP;
         qt.load(smem + stage * 2 * STEP * P, a.q + (int64_t)(seq.q0 + i0) * a.q_ts + (int64_t)head * a.q_hs, a.q_ts, seq.nq - i0);
         gt.load(smem + (stage * 2 + 1) * STEP * P, a.dO + (int64_t)(seq.q0 + i0) * a.do_ts + (int64_t)head * a.do_hs, a.do_ts, seq.nq - i0);
+        // one array of statistics by half of the waves each; rows past the last are masked, and 0 is as good as any for them
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.stats + ((int64_t)(wave & 1) * a.heads_q + head) * a.tokens_q + seq.q0 + i0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)&stats[stage][wave & 1][0], 4,
+                                                 i0 + lane < seq.nq ? 4 * lane : 0x80000000u, 0, 0, 0);
     };
-    // lse and delta of a step: read into registers a step ahead, put into LDS with the barrier
-    float stat = 0.f;
-    auto fetch_stats = [&](int member, int step) {
-        const int head = kv * a.group + member, i = (first + step) * STEP + (threadIdx.x & (STEP - 1));
-        const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-        if (threadIdx.x < STEP) stat = lse_offset<CAP, BIAS>(i < seq.nq ? a.lse[at] : -INFINITY, a);
-        else if (threadIdx.x < 2 * STEP) stat = i < seq.nq ? -a.delta[at] : 0.f;
-    };
+    // queries from .. to that see the lane's key
+    const int from = see.causal && j >= see.prefix ? j - see.shift : 0;
+    const int to = see.window > 0 ? min(seq.nq - 1, j - see.shift + see.window - 1) : seq.nq - 1;
     const float pos = (float)(j - see.shift - 4 * h);      // the distance from a register's query without its 4 h
     using Reader = TileReader<P>;
     const Reader reader(lane);
-    auto compute = [&](int i0, uint32_t tile, const float (*st)[STEP], const ScoreRule& rule, bool masked) {       // tile: Q's rows, dO's behind them
+    auto compute = [&](int i0, uint32_t tile, const float (*st)[64], const ScoreRule& rule, bool masked) {       // tile: Q's rows, dO's behind them
         const uint32_t qr = tile + reader.rows, qc = tile + reader.columns;
         uint32_t vr = tile_address(parked) + 32 * wave * P * 2 + reader.rows;
         asm volatile("" : "+v"(vr));       // (not an address per step, kept all along the loop)
 #pragma unroll
         for (int b = 0; b < STEP / 32; ++b) {
             f32x16 s, dp;
-            f32x4 lse2[4];
+            f32x4 offset[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                lse2[r] = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
+                offset[r] = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(&st[1][32 * b + 8 * r + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[4 * r + e] = CAP || BIAS ? 0.f : lse2[r][e];
+                    s[4 * r + e] = CAP || BIAS ? 0.f : offset[r][e];
                     dp[4 * r + e] = delta[e];
                 }
             }
@@ -512,7 +505,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float p = s[4 * r + e], g = dp[4 * r + e];
-                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, lse2[r][e], (float)(i0 + 32 * b + 8 * r + e) - pos);
+                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, CAP || BIAS ? offset[r][e] : 0.f, (float)(i0 + 32 * b + 8 * r + e) - pos);
                     s[4 * r + e] = p;
                     dp[4 * r + e] = CAP ? g * factor : g;
                 }
@@ -521,7 +514,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int i = i0 + 32 * b + acc_row(v) + 4 * h;
-                    const bool seen = j >= see.lo(i) && j <= see.hi(i);
+                    const bool seen = (i >= from) & (i <= to);
                     s[v] = seen ? s[v] : 0.f;
                     dp[v] = seen ? dp[v] : 0.f;
                 }
@@ -544,28 +537,29 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    int member = steps > 0 ? begin / steps : 0, step = begin - member * steps;
-    if (total > begin) {
-        fetch(member, step, begin & 1);
-        fetch_stats(member, step);
-    }
+    int ahead = steps > 0 ? begin / steps : 0, ahead_step = begin - ahead * steps;       // what is fetched next: member and step
+    auto fetch_next = [&](int it) {
+        fetch(ahead, ahead_step, it & 1);
+        if (++ahead_step == steps) {
+            ahead_step = 0;
+            ++ahead;
+        }
+    };
+    int member = ahead, step = ahead_step;
+    if (total > begin) fetch_next(begin);
     const int last_key = min(w0 + 31, seq.nk - 1);
     for (int it = begin; it < total; ++it) {
         wait_loads<0>();
-        if (threadIdx.x < 2 * STEP) stats[it & 1][threadIdx.x / STEP][threadIdx.x & (STEP - 1)] = stat;
         lds_barrier();
+        if (it + 1 < total) fetch_next(it + 1);
         const int now = kv * a.group + member, i0 = (first + step) * STEP, i1 = min(i0 + STEP, seq.nq) - 1;
         if (++step == steps) {
             step = 0;
             ++member;
         }
-        if (it + 1 < total) {
-            fetch(member, step, (it + 1) & 1);
-            fetch_stats(member, step);
-        }
         if (w0 >= seq.nk || see.hi(i1) < w0 || see.lo(i0) > last_key) continue;
         const ScoreRule rule = score_rule<CAP, BIAS>(a, now);
-        compute(i0, tile_address(smem) + (it & 1) * 4 * STEP * P, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key);
+        compute(i0, tile_address(smem) + (it & 1) * 4 * STEP * P, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key || i0 + STEP > seq.nq);
     }
     const bool mine = j < seq.nk;
     if (a.parts > 1) {
@@ -661,18 +655,19 @@ static dim3 join_grid(int64_t rows, int d) { return dim3((unsigned)((rows * (d /
 struct AttnParts {
     int forward, dq, dkv;
 };
-static int attn_parts(int64_t parts, int64_t steps) {
-    const int64_t most = steps / 4;      // (a part of fewer steps costs more in its ends and in the join than it saves)
+static int attn_parts(int64_t parts, int64_t steps, int least) {
+    const int64_t most = steps / least;     // (a part of fewer steps costs more in its ends and in the join than it saves)
     return (int)(parts < 1 || most < 1 ? 1 : parts < most ? (parts < 16 ? parts : 16) : most < 16 ? most : 16);
 }
 // Keys: whole parts of 512 workgroups (us without / with; 2048 queries, 8 heads of 128 on one key head: forward 41 / 31; 4096, one head of 64: 56 / 22,
 // backward 196 / 70; but 2000, 24 heads, 432 tiles, in two parts: 27 / 34).  Queries: 1024 workgroups or more, since a causal mask gives
 // the first keys most of the work (us in one part / by the rule / for 2048: 8192 tokens, 32 heads on 8 of 128: backward 3140 / 2270 / 2230; 4096, 16 on
-// 4, four sequences: 343 / 184 / 207; 4096, 32 on 32 without a mask, 1088 tiles: 1092 / 1091 / 1225; 1003, 10 on 2, five sequences: 63 / 37 / 37).
+// 4, four sequences: 343 / 184 / 207; 4096, 32 on 32 without a mask, 1088 tiles: 1092 / 1091 / 1225), of four steps or more; of two where the
+// parts are few all the same (2000, 4 on 1, ten sequences: 32 / 29).
 static AttnParts attn_parts(const qg_attention* a) {
     const int64_t work_q = attn_tiles(a->tokens_q, a->sequences) * a->heads_q, work_k = attn_tiles(a->tokens_k, a->sequences) * a->heads_k;
-    const int keys = attn_parts(512 / work_q, a->tokens_k / a->sequences / 64);
-    return {keys, keys, attn_parts((1024 + work_k - 1) / work_k, a->tokens_q / a->sequences * (a->heads_q / a->heads_k) / 64)};
+    const int keys = attn_parts(512 / work_q, a->tokens_k / a->sequences / 64, 4);
+    return {keys, keys, attn_parts((1024 + work_k - 1) / work_k, a->tokens_q / a->sequences * (a->heads_q / a->heads_k) / 64, work_k < 128 ? 2 : 4)};
 }
 // Floats of the parts' sums.
 static int64_t forward_floats(const qg_attention* a, int parts) { return parts > 1 ? (int64_t)parts * a->heads_q * a->tokens_q * (a->d + 2) : 0; }
@@ -681,7 +676,7 @@ static int64_t backward_floats(const qg_attention* a, const AttnParts& p) {
     const int64_t dkv = p.dkv > 1 ? (int64_t)p.dkv * a->heads_k * a->tokens_k * 2 * a->d : 0;
     return dq > dkv ? dq : dkv;
 }
-static int64_t delta_floats(const qg_attention* a) { return ((int64_t)a->heads_q * a->tokens_q + 3) / 4 * 4; }
+static int64_t stats_floats(const qg_attention* a) { return ((int64_t)a->heads_q * a->tokens_q * 2 + 3) / 4 * 4; }
 
 }  // namespace qg
 
@@ -692,7 +687,7 @@ extern "C" size_t qg_attention_forward_workspace_bytes(const qg_attention* a) {
 }
 
 extern "C" size_t qg_attention_backward_workspace_bytes(const qg_attention* a) {
-    return check_attention(a) == QG_OK ? (size_t)(delta_floats(a) + backward_floats(a, attn_parts(a))) * 4 : 0;
+    return check_attention(a) == QG_OK ? (size_t)(stats_floats(a) + backward_floats(a, attn_parts(a))) * 4 : 0;
 }
 
 extern "C" int qg_attention_forward(const qg_attention* a, const qg_heads* q, const qg_heads* k, const qg_heads* v, const qg_heads* o,
@@ -729,8 +724,8 @@ extern "C" int qg_attention_backward(const qg_attention* a, const qg_heads* dO, 
     args.dq = dq->data, args.dq_ts = dq->token_stride, args.dq_hs = dq->head_stride;
     args.dk = dk->data, args.dk_ts = dk->token_stride, args.dk_hs = dk->head_stride;
     args.dv = dv->data, args.dv_ts = dv->token_stride, args.dv_hs = dv->head_stride;
-    args.delta = static_cast<float*>(workspace);
-    args.part = args.delta + delta_floats(a);
+    args.stats = static_cast<float*>(workspace);
+    args.part = args.stats + stats_floats(a);
     const AttnParts parts = attn_parts(a);
     attn_shape(*a, [&](auto d, auto cap, auto bias) {
         args.tiles = (int)attn_tiles(a->tokens_q, a->sequences), args.parts = parts.dq;
