@@ -81,7 +81,7 @@ __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, int t) {
     const int k1 = tail ? a.tokens_k : attn_boundary(a.cu_k, lo + 1, a.sequences, a.tokens_k);
     r.nq = tail && KEYS ? 0 : max(0, q1 - r.q0);
     r.nk = tail && !KEYS ? 0 : max(0, k1 - r.k0);
-    r.prefix = a.prefix != nullptr && !tail ? a.prefix[lo] : 0;
+    r.prefix = a.prefix != nullptr && !tail ? max(0, a.prefix[lo]) : 0;
     return r;
 }
 
@@ -95,6 +95,13 @@ __device__ __forceinline__ bool attn_place(int heads, int tiles, int parts, int&
     head = rest / tiles;
     tile = rest - head * tiles;
     return true;
+}
+
+// Steps begin .. end - 1 of `all` that belong to a part.
+__device__ __forceinline__ void attn_share(int all, int parts, int part, int& begin, int& end) {
+    const int per = all / parts, more = all - per * parts;
+    begin = per * part + min(part, more);
+    end = begin + per + (part < more ? 1 : 0);
 }
 
 // Rows of a [rows][d] bf16 array as an LDS tile of `ROWS` rows of pitch P (64 or 128 elements), by direct loads.  The 16-byte chunk c of row r
@@ -212,9 +219,11 @@ __device__ __forceinline__ float score_log2(float s, float c, float cap_log2e, f
         factor = 1.f;
         return s * c;
     } else {
-        // tanh y = 1 - 2 / (exp(2 y) + 1); exp overflows to infinity and 1 is left
-        const float e = __builtin_amdgcn_exp2f(s * (c * (2.f * kLog2e)));
-        const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
+        // tanh y = 1 - 2 / (exp(2 y) + 1); exp overflows to infinity and 1 is left.  That is off by 2^-24, which the cap multiplies; so up to 1/4, where
+        // most scores lie, by the series, off by 2^-22 of y (scores within a cap of 30: lse 9 to 10 times nearer).
+        const float y = s * c, e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e)), z = y * y;
+        const float series = y * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+        const float t = z < 0.0625f ? series : __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
         factor = __builtin_fmaf(-t, t, 1.f);
         return cap_log2e * t;
     }

@@ -74,7 +74,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     // steps that some row of the workgroup sees, of them the part's; and, of the wave, those that all rows see whole
     const int first = see.lo(row0) / kAttnStep, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
     const int all = most < 0 ? 0 : most / kAttnStep - first + 1;
-    const int begin = (int)((int64_t)all * part / a.parts), steps = (int)((int64_t)all * (part + 1) / a.parts);
+    int begin, steps;
+    attn_share(all, a.parts, part, begin, steps);
     const int wave_lo = see.lo(w0), wave_hi = w0 < seq.nq ? see.hi(w1) : -1, all_lo = see.lo(w1), all_hi = see.hi(w0);
 
     f32x16 o[NB];
@@ -280,7 +281,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     const int lo = see.lo(i), hi = see.hi(i);
     const int first = see.lo(row0) / STEP, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
     const int all = most < 0 ? 0 : most / STEP - first + 1;
-    const int begin = (int)((int64_t)all * part / a.parts), steps = (int)((int64_t)all * (part + 1) / a.parts);
+    int begin, steps;
+    attn_share(all, a.parts, part, begin, steps);
     const int wave_lo = see.lo(w0), wave_hi = w0 < seq.nq ? see.hi(w1) : -1, all_lo = see.lo(w1), all_hi = see.hi(w0);
     f32x16 dq[NB];
 #pragma unroll
@@ -443,7 +445,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
         if (see.window > 0) qb = (int)min((int64_t)qb, (int64_t)end - see.shift + see.window);
     }
     const int first = qa / STEP, steps = qb > qa ? (qb - 1) / STEP - first + 1 : 0, all = steps * a.group;
-    const int begin = (int)((int64_t)all * part / a.parts), total = (int)((int64_t)all * (part + 1) / a.parts);
+    int begin, total;
+    attn_share(all, a.parts, part, begin, total);
     f32x16 dk[NB], dv[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) dk[b] = dv[b] = zero16();

@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a cache in pages: o = softmax_j(x_j) v_j over positions j = first .. length - 1.
 // The cache is read once, 4 d bytes per key head and position: HBM is the bound, and what counts is how many bytes are on their way.  The
 // query heads that share a key head are taken together, up to 16 as the columns of a 16 x 16 x 32 product (one alone leaves 15
-// columns empty: at 8 TB/s that is still 5 % of the matrix pipe).  A sequence is cut into parts for as many workgroups,
+// columns empty: at 8 TB/s that is still 5 % of the matrix pipe).  A sequence is cut into parts for many workgroups,
 // whose results are joined by a second kernel; a workgroup's waves take 32 positions each in turn, each with tiles, maximum and sums of
 // its own, so that nothing waits for another wave before the end.
 //   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
@@ -17,16 +17,19 @@ struct PagedArgs {
     uint16_t* o;
     const int32_t *table, *lengths;
     const float* slopes;
-    float* part;                            // [sequences][heads_q][parts][d] sums, then [..][2]: maximum (log2), sum
+    float* part;                            // [sequences][heads_q][shares][d] sums, then [..][2]: maximum (log2), sum
     int64_t q_ts, q_hs, o_ts, o_hs, pages;
-    int page_size, heads_k, group, d, sequences, width, parts, part_length, window;
+    int page_size, heads_k, group, d, sequences, width, part_length, shares, window;     // shares: workgroups that take a sequence's parts in turn
     float scale, cap;
 };
 
-// Visible positions of a sequence.
+// Visible positions of a sequence, and their parts, which begin at whole steps: one at least, so that a sequence without any gets its zeros.
 __device__ __forceinline__ void paged_range(const PagedArgs& a, int seq, int& first, int& end) {
     end = (int)min((int64_t)max(a.lengths[seq], 0), (int64_t)a.width * a.page_size);
     first = a.window > 0 ? max(0, end - a.window) : 0;
+}
+__device__ __forceinline__ int paged_parts(const PagedArgs& a, int first, int end) {
+    return max(1, (end - first / kPagedStep * kPagedStep + a.part_length - 1) / a.part_length);
 }
 
 template <int D, bool CAP, bool BIAS>
@@ -37,14 +40,18 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     constexpr int ROW = D + 4;
     static_assert(4 * 16 * ROW * 4 + 4 * 32 * 4 <= 4 * 2 * TILE * 2, "the results fit where the tiles were");
     __shared__ __attribute__((aligned(16))) uint16_t smem[4 * 2 * TILE];
-    const int part = blockIdx.x % a.parts, unit = blockIdx.x / a.parts;
-    const int groups = (a.group + 15) / 16;
+    // the first shares of all sequences and heads, then the second ...: workgroups go to the 8 XCDs in turn, and with a sequence's shares next to each
+    // other the first ones, which have work, would be the same XCD's (64 of up to 4096, eight shares: 65 us against 30)
+    const int groups = (a.group + 15) / 16, units = a.sequences * a.heads_k * groups;
+    const int part0 = blockIdx.x / units, at = blockIdx.x - part0 * units;
+    // ... and of every eight units another to each XCD from one part and eight to the next: with heads of 64 an XCD that always had the same one read
+    // every eighth 128-byte line, from few channels of its L2 (one of 130000, 8 heads: 64 us against 57)
+    const int unit = (at | 7) < units ? (at & ~7) | ((at + (at >> 3) + part0) & 7) : at;
     const int hg = unit % groups, kv = unit / groups % a.heads_k, seq = unit / groups / a.heads_k;
     int first, end;
     paged_range(a, seq, first, end);
-    const int whole_first = first / kPagedStep * kPagedStep;     // parts begin at whole steps
-    const int begin = whole_first + part * a.part_length, stop = min(end, begin + a.part_length);
-    if (part > 0 && begin >= end) return;                        // (part 0 of an empty sequence still writes its zeros)
+    const int parts = paged_parts(a, first, end);
+    if (part0 >= parts) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int head = kv * a.group + hg * 16 + col;
     const bool has_head = hg * 16 + col < a.group;
@@ -66,7 +73,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     // row of the cache that the wave's step holds at position lane % 32, -1: none (hidden, past the end, or without a page)
     auto slot_of = [&](int j0) {
         const int j = j0 + (lane & 31);
-        if (j < first || j >= stop) return -1;
+        if (j < first || j >= end) return -1;
         const int at = (int)((uint32_t)j / (uint32_t)a.page_size), page = pages[at];
         return page < 0 || page >= a.pages ? -1 : page * a.page_size + (j - at * a.page_size);
     };
@@ -161,9 +168,15 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    const int j0 = begin + wave * kPagedStep, by = 4 * kPagedStep;
-    const int steps = j0 < stop ? (stop - j0 + by - 1) / by : 0;
-    int slot = steps > 0 ? slot_of(j0) : -1, next = steps > 1 ? slot_of(j0 + by) : -1;
+    // The wave's steps: of each part of this share every fourth; the last part of a sequence may end early.
+    const int by = 4 * kPagedStep, per = a.part_length / by, base = first / kPagedStep * kPagedStep + wave * kPagedStep;
+    const int mine = (parts - part0 + a.shares - 1) / a.shares, last = part0 + (mine - 1) * a.shares;
+    const int steps = (mine - 1) * per + min(max((end - base - last * a.part_length + by - 1) / by, 0), per);
+    auto position = [&](int i) {
+        const int part = i / per;
+        return base + (part0 + part * a.shares) * a.part_length + (i - part * per) * by;
+    };
+    int slot = steps > 0 ? slot_of(position(0)) : -1, next = steps > 1 ? slot_of(position(1)) : -1;
     if (steps > 0) fetch(slot, 0, kf[0]);
     for (int i = 0; i < steps; i += 2) {
 #pragma unroll
@@ -174,9 +187,9 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
                 if (i + u + 1 < steps) {
                     fetch(next, 1 - u, kf[1 - u]);
                     slot = next;
-                    next = i + u + 2 < steps ? slot_of(j0 + (i + u + 2) * by) : -1;
+                    next = i + u + 2 < steps ? slot_of(position(i + u + 2)) : -1;
                 }
-                compute(j0 + (i + u) * by, there, u, kf[u]);
+                compute(position(i + u), there, u, kf[u]);
             }
         }
     }
@@ -209,16 +222,16 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
             x += *reinterpret_cast<const f32x4*>(sums + (w * 16 + q) * ROW + e) * f;
         }
         const int h = kv * a.group + hg * 16 + q;
-        if (a.parts == 1) {
+        if (a.shares == 1) {
             const float f = sum == 0.f ? 0.f : 1.f / sum;
             uint32_t* to = reinterpret_cast<uint32_t*>(a.o + (int64_t)seq * a.o_ts + (int64_t)h * a.o_hs + e);
             to[0] = pack_bf16x2(x[0] * f, x[1] * f);
             to[1] = pack_bf16x2(x[2] * f, x[3] * f);
         } else {
-            const int64_t row = ((int64_t)seq * a.heads_k * a.group + h) * a.parts + part;
+            const int64_t row = ((int64_t)seq * a.heads_k * a.group + h) * a.shares + part0;
             *reinterpret_cast<f32x4*>(a.part + row * a.d + e) = x;
             if (e == 0) {
-                float* to = a.part + (int64_t)a.sequences * a.heads_k * a.group * a.parts * a.d + 2 * row;
+                float* to = a.part + (int64_t)a.sequences * a.heads_k * a.group * a.shares * a.d + 2 * row;
                 to[0] = top;
                 to[1] = sum;
             }
@@ -226,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     }
 }
 
-// Joins the parts of a sequence's heads in a fixed order: WAVES waves per head, of each 64 / (d / 4) parts at once, four elements per lane.
+// Joins the shares of a sequence's heads in a fixed order: WAVES waves per head, of each 64 / (d / 4) shares at once, four elements per lane.
 template <int WAVES>
 __global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
     constexpr int HEADS = 4 / WAVES;
@@ -236,8 +249,8 @@ __global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
     const int seq = (int)(unit / heads), h = (int)(unit - (int64_t)seq * heads);
     int first, end;
     paged_range(a, seq, first, end);
-    const int parts = max(1, (end - first / kPagedStep * kPagedStep + a.part_length - 1) / a.part_length);
-    const float *from = a.part + unit * a.parts * a.d, *stat = a.part + (int64_t)a.sequences * heads * a.parts * a.d + 2 * unit * a.parts;
+    const int parts = min(a.shares, paged_parts(a, first, end));
+    const float *from = a.part + unit * a.shares * a.d, *stat = a.part + (int64_t)a.sequences * heads * a.shares * a.d + 2 * unit * a.shares;
     const int per = a.d / 4, at_once = 64 / per, e = lane % per * 4, mine = lane / per;
     float top = -INFINITY;
     for (int p = lane; p < parts; p += 64) top = fmaxf(top, stat[2 * p]);
@@ -252,7 +265,7 @@ __global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
             sum = __builtin_fmaf(stat[2 * p + 1], f, sum);
             x += *reinterpret_cast<const f32x4*>(from + (int64_t)p * a.d + e) * f;
         }
-    // the parts of a wave, then the waves
+    // the shares of a wave, then the waves
     float y[5] = {x[0], x[1], x[2], x[3], sum};
     for (int o = 1; o < at_once; ++o)
 #pragma unroll
@@ -285,16 +298,22 @@ static int part_length(const qg_cache* c, int heads_q) {
     const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16);
     return units * c->width * c->page_size < 512 * 512 ? 256 : 512;
 }
-static int64_t paged_parts(const qg_cache* c, int heads_q) {
+static int64_t most_parts(const qg_cache* c, int heads_q) {
     const int length = part_length(c, heads_q);
     return ((int64_t)c->width * c->page_size + kPagedStep - 1 + length - 1) / length;
+}
+// Workgroups per sequence and key head: all parts, but no more than make 8192 in all (a table is as wide as the longest sequence may get: 64 sequences of
+// 1000 positions, 8 key heads, in a table for 131072, one workgroup for each part 143 us, of which most had nothing to do).
+static int64_t most_shares(const qg_cache* c, int heads_q) {
+    const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16), parts = most_parts(c, heads_q);
+    const int64_t shares = (8192 + units - 1) / units;
+    return shares < parts ? shares : parts;
 }
 
 static int check_paged(const qg_cache* c, int heads_q) {
     if (int e = check_cache(c)) return e;
     if (c->d > 128 || heads_q <= 0 || heads_q > kAttnMaxHeads || heads_q % c->heads != 0) return QG_ERR_SHAPE;
-    const int64_t groups = (heads_q / c->heads + 15) / 16;
-    if (paged_parts(c, heads_q) * c->sequences * c->heads * groups >= (int64_t(1) << 24)) return QG_ERR_SHAPE;   // (2^32 threads in a launch)
+    if ((int64_t)c->sequences * heads_q >= (int64_t(1) << 24)) return QG_ERR_SHAPE;   // (2^32 threads in a launch)
     return QG_OK;
 }
 
@@ -304,7 +323,7 @@ using namespace qg;
 
 extern "C" size_t qg_attention_paged_workspace_bytes(const qg_cache* c, int heads_q) {
     if (check_paged(c, heads_q) != QG_OK) return 0;
-    return ((size_t)paged_parts(c, heads_q) * c->sequences * heads_q * (c->d + 2) * 4 + 15) / 16 * 16;
+    return ((size_t)most_shares(c, heads_q) * c->sequences * heads_q * (c->d + 2) * 4 + 15) / 16 * 16;
 }
 
 extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, const qg_heads* q, int heads_q, float scale, float cap, int64_t window,
@@ -321,10 +340,11 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     a.o = o->data, a.o_ts = o->token_stride, a.o_hs = o->head_stride;
     a.k = c->k, a.v = c->v, a.table = c->table, a.lengths = lengths, a.slopes = slopes, a.part = static_cast<float*>(workspace);
     a.pages = c->pages, a.page_size = c->page_size, a.heads_k = c->heads, a.group = heads_q / c->heads, a.d = c->d;
-    a.sequences = c->sequences, a.width = c->width, a.parts = (int)paged_parts(c, heads_q), a.part_length = part_length(c, heads_q);
+    a.sequences = c->sequences, a.width = c->width, a.part_length = part_length(c, heads_q);
+    a.shares = (int)most_shares(c, heads_q);
     a.window = (int)(window < (int64_t(1) << 31) ? window : 0);
     a.scale = scale, a.cap = cap;
-    const unsigned grid = (unsigned)((int64_t)a.parts * a.sequences * a.heads_k * ((a.group + 15) / 16));
+    const unsigned grid = (unsigned)((int64_t)a.shares * a.sequences * a.heads_k * ((a.group + 15) / 16));
     auto launch = [&](auto d, auto cp, auto bias) {
         hipLaunchKernelGGL((k_attention_paged<d.value, cp.value, bias.value>), dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
     };
@@ -335,7 +355,7 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     auto with_bias = [&](auto cp) { slopes != nullptr ? with_d(cp, std::true_type()) : with_d(cp, std::false_type()); };
     cap > 0.f ? with_bias(std::true_type()) : with_bias(std::false_type());
     const int64_t heads = (int64_t)a.sequences * heads_q;
-    if (a.parts > 16) hipLaunchKernelGGL(k_attention_join<4>, dim3((unsigned)heads), dim3(256), 0, (hipStream_t)stream, a);
-    else if (a.parts > 1) hipLaunchKernelGGL(k_attention_join<1>, dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
+    if (a.shares > 16) hipLaunchKernelGGL(k_attention_join<4>, dim3((unsigned)heads), dim3(256), 0, (hipStream_t)stream, a);
+    else if (a.shares > 1) hipLaunchKernelGGL(k_attention_join<1>, dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
     return check_launch();
 }

@@ -196,7 +196,7 @@ int check_cache(const qg_cache* c) {
     if (c->pages <= 0 || c->page_size <= 0 || c->heads <= 0 || c->heads > kAttnMaxHeads || c->d <= 0 || c->d % 8 != 0 || c->d > kRopeMaxD) return QG_ERR_SHAPE;
     if (c->sequences <= 0 || c->sequences > kAttnMaxSequences || c->width <= 0) return QG_ERR_SHAPE;
     const int64_t most = int64_t(1) << 31;
-    if (c->pages >= most || c->pages * c->page_size >= most || (int64_t)c->width * c->page_size >= most || (int64_t)c->sequences * c->width >= most)
+    if (c->pages >= most || c->pages * c->page_size >= most || (int64_t)c->width * c->page_size >= most / 2 || (int64_t)c->sequences * c->width >= most)
         return QG_ERR_SHAPE;
     if (!aligned16(c->k) || !aligned16(c->v) || (reinterpret_cast<uintptr_t>(c->table) & 3)) return QG_ERR_ALIGN;
     return QG_OK;
