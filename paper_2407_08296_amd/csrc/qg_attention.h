@@ -219,11 +219,10 @@ __device__ __forceinline__ float score_log2(float s, float c, float cap_log2e, f
         factor = 1.f;
         return s * c;
     } else {
-        // tanh y = 1 - 2 / (exp(2 y) + 1); exp overflows to infinity and 1 is left.  That is off by 2^-24, which the cap multiplies; so up to 1/4, where
-        // most scores lie, by the series, off by 2^-22 of y (scores within a cap of 30: lse 9 to 10 times nearer).
-        const float y = s * c, e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e)), z = y * y;
-        const float series = y * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
-        const float t = z < 0.0625f ? series : __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
+        // |tanh y| = (1 - e) / (1 + e), e = exp(-2 |y|).  Near 0 off by half the exponential's rounding, 2^-25, which the cap multiplies (1 - 2 /
+        // (exp(2 y) + 1): six times that; a series for small y: none of it, but kernels a third longer).
+        const float y = s * (c * (2.f * kLog2e)), e = __builtin_amdgcn_exp2f(-fabsf(y));
+        const float t = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
         factor = __builtin_fmaf(-t, t, 1.f);
         return cap_log2e * t;
     }

@@ -476,14 +476,13 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
 #pragma unroll
         for (int b = 0; b < STEP / 32; ++b) {
             f32x16 s, dp;
-            f32x4 offset[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                offset[r] = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
+                const f32x4 offset = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(&st[1][32 * b + 8 * r + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[4 * r + e] = CAP || BIAS ? 0.f : offset[r][e];
+                    s[4 * r + e] = CAP || BIAS ? 0.f : offset[e];
                     dp[4 * r + e] = delta[e];
                 }
             }
@@ -505,10 +504,12 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
             __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
+                f32x4 offset = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (CAP || BIAS) offset = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float p = s[4 * r + e], g = dp[4 * r + e];
-                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, CAP || BIAS ? offset[r][e] : 0.f, (float)(i0 + 32 * b + 8 * r + e) - pos);
+                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, offset[e], (float)(i0 + 32 * b + 8 * r + e) - pos);
                     s[4 * r + e] = p;
                     dp[4 * r + e] = CAP ? g * factor : g;
                 }

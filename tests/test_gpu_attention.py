@@ -64,7 +64,7 @@ def check(q, k, v, do, lengths, lengths_k=None, causal=True, scale=None, cap=0.0
             assert np.all(np.abs(got - want) <= tol), ("o", s, h, float((np.abs(got - want) / tol).max()))
             empty = ~seen.any(axis=1)
             assert np.all(got[empty] == 0) and np.all(got_lse[empty] == -np.inf)
-            off = np.abs(got_lse - want_lse)[~empty]
+            off = np.abs(got_lse[~empty] - want_lse[~empty])
             assert np.all(off <= ep[~empty, 0]), ("lse", s, h, float(off.max()))
             if grads is None:
                 continue
@@ -101,6 +101,29 @@ def run(lengths, heads=2, heads_k=2, d=64, seed=0, lengths_k=None, pad=0, pad_k=
     check(q, k, v, do, lengths, lengths_k, o=o, lse=lse, grads=grads, **how)
 
 
+def slopes_of(heads):
+    return torch.tensor([0.5 ** h for h in range(heads)], device=DEV)
+
+
+# (tokens, tokens_k, heads, heads_k, d, sequences, flags: 1 causal, 2 cap, 4 slopes): calls that the host cuts into parts, and every kernel
+PARTS = [(2048, 2048, 2, 1, 128, 1, 1), (16, 3000, 2, 2, 64, 1, 1), (1, 3000, 1, 1, 80, 1, 1), (700, 700, 3, 1, 96, 1, 0), (3000, 40, 2, 1, 64, 1, 0), (1500, 1500, 1, 1, 72, 1, 7),
+         (1200, 1200, 6, 1, 128, 1, 3)]
+KERNELS = [(150, 150, 2, 1, d, 1, f) for d in (64, 96, 128) for f in (1, 3, 5, 7)]
+
+
+@pytest.mark.parametrize("tokens,tokens_k,heads,heads_k,d,sequences,flags", PARTS + KERNELS)
+def test_every_kernel(tokens, tokens_k, heads, heads_k, d, sequences, flags):
+    run([tokens], heads=heads, heads_k=heads_k, d=d, lengths_k=None if tokens == tokens_k else [tokens_k], causal=bool(flags & 1), cap=6.0 if flags & 2 else 0.0,
+        slopes=slopes_of(heads) if flags & 4 else None, seed=tokens)
+
+
+@pytest.mark.parametrize("how", [dict(), dict(window=300), dict(prefix=True, cap=9.0)])
+def test_parts_of_packed_sequences(how):
+    """Parts where sequences are of very different lengths: some have steps for every part, some for none; a padded end."""
+    how = dict(how, prefix=torch.tensor([900, 0, 3, 40], dtype=torch.int32, device=DEV)) if how.get("prefix") else how
+    run([1900, 0, 5, 700], heads=2, heads_k=1, d=64, pad=50, seed=21, **how)
+
+
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 257, 600])
 @pytest.mark.parametrize("causal", [True, False])
 def test_lengths(n, causal):
@@ -117,11 +140,7 @@ def test_grouped_heads(heads, heads_k):
     run([70, 90], heads=heads, heads_k=heads_k, d=64, seed=heads)
 
 
-def slopes_of(heads):
-    return torch.tensor([0.5 ** h for h in range(heads)], device=DEV)
-
-
-HOW = [dict(cap=5.0), dict(slopes=True), dict(cap=8.0, slopes=True), dict(window=1), dict(window=37), dict(window=64, cap=5.0), dict(window=10 ** 9),
+HOW = [dict(cap=5.0), dict(cap=200.0), dict(slopes=True), dict(cap=8.0, slopes=True), dict(window=1), dict(window=37), dict(window=64, cap=5.0), dict(window=10 ** 9),
        dict(window=90, slopes=True), dict(causal=False, slopes=True), dict(causal=False, cap=5.0), dict(prefix=(0, 0, 0, 0)), dict(prefix=(1, 0, 100, 40)),
        dict(prefix=(999, -3, 65, 130), slopes=True), dict(scale=0.01), dict(scale=1.0)]
 
@@ -131,7 +150,7 @@ HOW = [dict(cap=5.0), dict(slopes=True), dict(cap=8.0, slopes=True), dict(window
 def test_scores_and_masks(how, d):
     how = dict(HOW[how])
     if how.get("slopes"):
-        how["slopes"] = slopes_of(2)
+        how["slopes"] = slopes_of(2) * (1 if d != 80 else -0.01)      # (one that favours far keys, too)
     if "prefix" in how:
         how["prefix"] = torch.tensor(how["prefix"], dtype=torch.int32, device=DEV)
     run([1, 64, 100, 170], heads=2, heads_k=1, d=d, pad=9, seed=3, **how)

@@ -180,6 +180,33 @@ def test_paged_lengths(n):
     run_paged([n], 4, 2, 64, 16, seed=n)
 
 
+# (lengths, heads, heads_k, d, page): one share of a sequence, a few, many (joined by four waves per head)
+SHARES = [([100], 4, 2, 64, 16), ([700, 5], 4, 2, 64, 16), ([9000], 4, 2, 64, 16), ([9000, 0, 4000], 3, 1, 128, 100), ([6000], 2, 2, 40, 7)]
+
+
+@pytest.mark.parametrize("lengths,heads,heads_k,d,page", SHARES)
+@pytest.mark.parametrize("window", [0, 2500])
+def test_paged_shares(lengths, heads, heads_k, d, page, window):
+    run_paged(lengths, heads, heads_k, d, page, seed=len(lengths), slack=0, window=window)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_more_parts_than_workgroups(d):
+    """700 sequences, 4 key heads: three workgroups each take a long sequence's eight parts in turn; a table far wider than most need."""
+    lengths = [4000 if i in (0, 350, 699) else i % 40 for i in range(700)]
+    page, width = 16, 400
+    pages = sum(-(-n // page) for n in lengths)
+    kp, vp = normal(pages, page, 4, d, seed=1, std=1.5), normal(pages, page, 4, d, seed=2)
+    ids = torch.randperm(pages, generator=torch.Generator().manual_seed(3)).tolist()
+    table, at = torch.full((700, width), -1, dtype=torch.int32), 0
+    for i, n in enumerate(lengths):
+        for j in range(-(-n // page)):
+            table[i, j], at = ids[at], at + 1
+    q = normal(700, 4, d, seed=4, std=1.5)
+    got = qg.attention_paged(q, kp, vp, table.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    check_paged(q, kp, vp, table, lengths, got)
+
+
 @pytest.mark.parametrize("page", [1, 3, 16, 31, 64, 100, 1000])
 def test_paged_page_sizes(page):
     run_paged([700, 5, 0, 64, 333], 4, 2, 64, page, seed=page)
