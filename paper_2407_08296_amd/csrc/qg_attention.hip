@@ -108,13 +108,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
         constexpr bool kScaled = CAP || BIAS;     // s holds x log2(e) then
         float top = -INFINITY;
         if constexpr (kScaled) {
+            const float away = pos - (float)j0;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     float unused;
                     s[b][v] = score_log2<CAP>(s[b][v], rule.c, rule.cap_log2e, unused);
-                    if constexpr (BIAS) s[b][v] = __builtin_fmaf(-rule.slope, fabsf(pos - (float)(j0 + 32 * b + acc_row(v))), s[b][v]);
+                    if constexpr (BIAS) s[b][v] = __builtin_fmaf(-rule.slope, fabsf(away - (float)(32 * b + acc_row(v))), s[b][v]);
                 }
         }
         if (masked) {     // (a branch around the selects alone: with a masked and a plain body the registers of both spill)
@@ -326,10 +327,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
                 });
             __builtin_amdgcn_s_setprio(0);
             f32x16 factor;
+            const float away = pos - (float)j0;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 float p = s[v], g = dp[v] - delta;
-                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, offset, pos - (float)(j0 + 32 * b + acc_row(v)));
+                factor[v] = score_gradient<CAP, BIAS>(p, g, rule, offset, away - (float)(32 * b + acc_row(v)));
                 s[v] = p;
                 dp[v] = g;
             }
@@ -502,6 +504,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
                     dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.g, r.v, dp, 0, 0, 0);
                 });
             __builtin_amdgcn_s_setprio(0);
+            const float away = (float)i0 - pos;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f32x4 offset = {0.f, 0.f, 0.f, 0.f};
@@ -509,7 +512,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float p = s[4 * r + e], g = dp[4 * r + e];
-                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, offset[e], (float)(i0 + 32 * b + 8 * r + e) - pos);
+                    const float factor = score_gradient<CAP, BIAS>(p, g, rule, offset[e], away + (float)(32 * b + 8 * r + e));
                     s[4 * r + e] = p;
                     dp[4 * r + e] = CAP ? g * factor : g;
                 }
