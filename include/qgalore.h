@@ -461,7 +461,8 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  *   multiple of 8.
  * qg_cache_append: k and v of `tokens` tokens to their place: token t belongs to sequence[t] (NULL: t) and stands at positions[t]; one without
  *   a place is left out.  k is turned as by qg_rope_forward on its way, and so is q (NULL, with heads_q = 0: none) to q_out (may be q); rot 0:
- *   nothing is turned (freqs NULL).  Of two tokens with one place either may win.
+ *   nothing is turned (freqs NULL).  Tokens of one call need places of
+ *   their own: one that two of them share ends up with pieces of both.
  * qg_attention_paged: one new token per sequence: o = softmax over positions 0 .. lengths[s] - 1 of the cache, the query standing
  *   at lengths[s] - 1; scores, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  What the
  *   cache holds outside the visible positions is not looked at.  workspace: qg_attention_paged_workspace_bytes(c, heads_q) bytes, 16-byte

@@ -20,7 +20,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 
 constexpr int64_t kAttnMaxTokens = int64_t(1) << 24;
 constexpr int kAttnMaxHeads = 1024, kAttnMaxSequences = 1 << 20;
-constexpr int64_t kHeadsMaxStride = int64_t(1) << 23;   // elements between tokens: 64 rows are addressed in 31 bits from one base
+constexpr int64_t kHeadsMaxStride = int64_t(1) << 23;   // elements between tokens: 128 rows are addressed in 31 bits from one base
 
 int check_heads(const qg_heads* x, bool required);      // host, qg_attention.hip
 int check_cache(const qg_cache* c);                     // host, qg_rope.hip

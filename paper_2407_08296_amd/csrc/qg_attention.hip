@@ -6,7 +6,17 @@
 // One pass over the keys with a running maximum and sum; exponentials to the base 2.  p and ds are rounded to bf16, operands of
 // matrix products, as every product of the library has them; maxima, sums, lse, delta and all accumulators are fp32.
 // Backward: one kernel for dq (queries stay, keys pass by) and one for dk and dv (keys stay, queries of all heads that share them
-// pass by): seven products where one kernel would do five, but each sum has one owner and one order: no atomics, the same bits every time.
+// pass by): eight products where one kernel would do five, but each sum has one owner and one order: no atomics, the same bits every time.
+// o is stored in bf16, and a delta from that is off by a rounding of sum do o in all of a row (dq and dk off by 0.0031 of their size at 64 keys, 0.0028 at
+// 512, where their own roundings make 0.0024).  But the true p_j (do.v_j - delta) add up to 0 over a row: what they come to, r, is what delta
+// lacks.  So the pass for dq also forms r and the mean key k' = sum_j p_j (1 - tanh^2) k_j, takes r k' off in the end and leaves delta + r for dk:
+// a product more, from operands that are there (8192 tokens, 32 heads of 128 on 8: dq 924 -> 1020 us).
+//
+// What bounds them, by counters (4096 tokens, 16 heads, no mask): cycles of the matrix pipe and of vector instructions add up to those that pass, in all
+// three, at d = 128 51 + 49 % (forward) and at d = 64 38 + 62 %, with two to four waves per SIMD and at 1.9 to 2.0 GHz; LDS is busy for a third,
+// without conflicts.  Interleaving a step's exponentials with the next step's products by hand changes nothing (forward 545 -> 555 us).
+// us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 560 (0.98), backward 2040 (0.67); 32 on 32, two
+// sequences: 325 (0.91), 1190 (0.62: dq 565, dkv 605); 32 heads of 64, one sequence: 350 (0.79), 1120 (0.61).
 #include "qg_attention.h"
 
 namespace qg {
@@ -49,6 +59,8 @@ struct Visible {
     __device__ __forceinline__ int lo(int i) const { return window > 0 ? max(0, i + shift - window + 1) : 0; }
 };
 
+// Forward: 128 queries per workgroup, 32 per wave, in registers; keys and values pass by in steps of 64 through two stages of LDS.  A wave's scores are
+// transposed ([key][query]), so that a query's maximum and sum are its lane's, and probabilities become operands as they lie.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16;
@@ -227,6 +239,8 @@ __device__ __forceinline__ float score_gradient(float& s, float& dp, const Score
     return factor;
 }
 
+// dq, in the forward pass's shape.  From d = 65 on dO's rows are parked in LDS (registers: dq and the mean key 64 each, q 32, a block of scores and their
+// gradients 32), and one block of 32 x 32 scores is worked on at a time, its operands read one ahead.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
@@ -288,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     f32x16 dq[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) dq[b] = zero16();
-    f32x16 mean[NB];
+    f32x16 mean[NB];          // of the keys, and what the row's p (dp - delta) add up to: see above
     float rest = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) mean[b] = zero16();
@@ -407,6 +421,9 @@ __global__ __launch_bounds__(256) void k_attention_dq_join(AttnArgs a) {
     *reinterpret_cast<u32x2*>(a.dq + (int64_t)token * a.dq_ts + (int64_t)head * a.dq_hs + e) = w;
 }
 
+// dk and dv: 128 keys per workgroup, 32 per wave; the queries of every head that shares them pass by, head after head.  Scores are [query][key] here, and
+// their products begin at -delta and, where x is linear in the product, at lse's offset, which LDS holds for a step's queries.  V's rows are parked
+// from d = 65 on, as dO's in dq.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();

@@ -2,7 +2,8 @@
 //     amplitude (a cos t - b sin t, a sin t + b cos t),  t = position * frequency;  the backward pass turns by -t.
 // The angle is formed and reduced to one turn in 64 bits (a far position times a frequency loses it in 32), its sine and cosine are fp32, and
 // the result is rounded once.  A workgroup computes the sines of its tokens once, for all heads, into LDS; then every element
-// is read and written once: HBM is the bound, for a few tokens the chain of position, frequency and sine ahead of the first store.
+// is read and written once: HBM is the bound (4096 tokens, 32 + 32 heads of 128: 24.6 us, 5.5 TB/s with part of the inputs in the last-level cache;
+// 4000 tokens into a cache, 32 + 8 heads: 17.7 us), for a few tokens the chain of position, frequency and sine ahead of the first store (2.8 us).
 #include "qg_attention.h"
 
 #include <cmath>

@@ -172,10 +172,11 @@ def test_many_sequences(n):
 
 
 @pytest.mark.parametrize("lengths,lengths_k", [([5], [200]), ([130], [400]), ([200], [50]), ([64, 1, 0, 40], [64, 300, 20, 0]), ([33, 100], [129, 70])])
-@pytest.mark.parametrize("how", [dict(), dict(causal=False), dict(window=40), dict(slopes=True, cap=6.0)])
+@pytest.mark.parametrize("how", [dict(), dict(causal=False), dict(window=40), dict(slopes=True, cap=6.0), dict(prefix=30)])
 def test_other_keys_than_queries(lengths, lengths_k, how):
     """A chunk of queries behind keys that are there already; more queries than keys (the first see none); none of one or the other."""
     how = dict(how, slopes=slopes_of(4)) if how.get("slopes") else how
+    how = dict(how, prefix=torch.full((len(lengths),), how["prefix"], dtype=torch.int32, device=DEV)) if how.get("prefix") else how
     run(lengths, heads=4, heads_k=2, d=64, lengths_k=lengths_k, pad=4, pad_k=11, seed=7, **how)
 
 
@@ -299,6 +300,19 @@ def test_a_training_pass_against_automatic_differentiation():
     got = qg.attention_backward(do, q, k, v, o, lse)
     for g, leaf in zip(got, leaves):
         assert float((g[:, 0].double() - leaf.grad).norm()) <= 0.9 * H * float(leaf.grad.norm())
+
+
+def test_boundaries_that_make_no_sense():
+    """Descending, negative, past the end: what comes out is of no use, but nothing outside the arrays is touched."""
+    q, k, v, do = tensors(300, 300, 2, 1, 64, 19)
+    guard = torch.full((3, 300, 2, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    for b in ([0, 200, 100, 300], [5, -7, 2 ** 31 - 1, 50], [300, 0, 300, 0], [-1, -1, -1, -1]):
+        bounds = torch.tensor(b, dtype=torch.int32, device=DEV)
+        out = guard[1]
+        o, lse = qg.attention_forward(q, k, v, bounds, out=out)
+        qg.attention_backward(do, q, k, v, o, lse, bounds)
+        torch.cuda.synchronize()
+        assert bool((guard[0] == 3).all()) and bool((guard[2] == 3).all())
 
 
 def test_refusals():
