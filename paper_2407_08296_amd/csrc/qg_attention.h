@@ -105,12 +105,14 @@ __device__ __forceinline__ void attn_share(int all, int parts, int part, int& be
 }
 
 // Rows of a [rows][d] bf16 array as an LDS tile of `ROWS` rows of pitch P (64 or 128 elements), by direct loads.  The 16-byte chunk c of row r
-// is kept in slot c ^ swizzle(r): reads of one chunk of 16 consecutive rows (an operand whose k is d) and transposing reads of four
-// chunks of four consecutive rows (an operand whose k is the row) each spread over all banks.  Rows from `valid` on and elements from
-// d on become zero.
+// is kept in slot c ^ swizzle(r): reads of one chunk of 16 consecutive rows (an operand whose k is d), transposing reads of four
+// chunks of four consecutive rows (an operand whose k is the row) and of two chunks of eight each take every bank once.  All 64 banks are one row at
+// P = 128 and two at P = 64, so that there the row's lowest bit places it already.  (P = 64 swizzled by that bit too: each
+// read took twice as long, 8192 tokens, 32 heads of 64, backward 1161 -> 1149 us.)
+// Rows from `valid` on and elements from d on become zero.
 template <int P>
 __device__ __forceinline__ int tile_swizzle(int r) {
-    return P == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 1) << 2) | ((r >> 1) & 3);
+    return (P == 128 ? (r & 3) << 2 : (r & 2) << 1) | ((r >> 1) & 2) | ((r >> 3) & 1);
 }
 
 template <int P, int ROWS, int NT>
@@ -160,7 +162,7 @@ struct TileReader {
     // Operand of 32 elements of d (from 32 * block on) with k = 16 rows from row0 on, in the order of k of a score's registers; at: the tile's
     // address + columns.
     __device__ __forceinline__ static bf16x8 frag_t(uint32_t at, int row0, int block) {
-        const uint32_t lo = at ^ (uint32_t)(block * 64), hi = at ^ (uint32_t)(block * 64 ^ (P == 128 ? 32 : 0));    // (8 rows on the swizzle differs by 2)
+        const uint32_t lo = at ^ (uint32_t)(block * 64), hi = at ^ (uint32_t)(block * 64 ^ 16);    // (8 rows on the swizzle differs by 1)
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lo + (uint32_t)(row0 * P * 2)));
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(hi + (uint32_t)((row0 + 8) * P * 2)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));

@@ -12,11 +12,12 @@
 // lacks.  So the pass for dq also forms r and the mean key k' = sum_j p_j (1 - tanh^2) k_j, takes r k' off in the end and leaves delta + r for dk:
 // a product more, from operands that are there (8192 tokens, 32 heads of 128 on 8: dq 924 -> 1020 us).
 //
-// What bounds them, by counters (4096 tokens, 16 heads, no mask): cycles of the matrix pipe and of vector instructions add up to those that pass, in all
-// three, at d = 128 51 + 49 % (forward) and at d = 64 38 + 62 %, with two to four waves per SIMD and at 1.9 to 2.0 GHz; LDS is busy for a third,
-// without conflicts.  Interleaving a step's exponentials with the next step's products by hand changes nothing (forward 545 -> 555 us).
-// us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 560 (0.98), backward 2040 (0.67); 32 on 32, two
-// sequences: 325 (0.91), 1190 (0.62: dq 565, dkv 605); 32 heads of 64, one sequence: 350 (0.79), 1120 (0.61).
+// What bounds them, by counters (4096 tokens, 16 heads, no mask; shares of the time that the matrix pipe + the vector instructions take): d = 128
+// forward 53 + 51 %, dq 63 + 47 %, dkv 57 + 35 %; d = 64 37 + 61 %, 51 + 57 %, 49 + 44 %: they hardly overlap, with two to four waves per SIMD.  LDS
+// is busy for 18 to 43 %, without bank conflicts.  Interleaving a step's exponentials with the next step's products by hand gains nothing (8192 tokens,
+// 32 heads of 128 on 8, forward: 546 -> 558 us).
+// us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 584 (0.94), backward 2133 (0.64); 32 on 32, two
+// sequences: 338 (0.87), 1235 (0.60); 32 heads of 64, one sequence: 364 (0.76), 1149 (0.60).
 #include "qg_attention.h"
 
 namespace qg {
