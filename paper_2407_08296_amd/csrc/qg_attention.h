@@ -147,6 +147,12 @@ __device__ __forceinline__ uint32_t tile_address(const uint16_t* tile) {
 }
 // Reads of a tile's operands.  A lane's address is one number per tile: steps and blocks change the slot alone, by exclusive or, and rows are
 // constant offsets.  (Separate addresses for each step and block were 24 registers, of 256 that spill.)
+// Reads from LDS that the compiler takes for reads of what no direct load in flight writes: each step waits for its own tile.  (Without `__restrict__`
+// it waits for every such load ahead of a transposing read, so for the next step's rows in the middle of this one.)
+__device__ __forceinline__ s16x4 lds_read_tr(lds_s16x4* __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
+typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+__device__ __forceinline__ f32x4 lds_read4(lds_f32x4* __restrict__ p) { return *p; }
+
 template <int P>
 struct TileReader {
     uint32_t rows, columns;
@@ -163,8 +169,8 @@ struct TileReader {
     // address + columns.
     __device__ __forceinline__ static bf16x8 frag_t(uint32_t at, int row0, int block) {
         const uint32_t lo = at ^ (uint32_t)(block * 64), hi = at ^ (uint32_t)(block * 64 ^ 16);    // (8 rows on the swizzle differs by 1)
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lo + (uint32_t)(row0 * P * 2)));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(hi + (uint32_t)((row0 + 8) * P * 2)));
+        const s16x4 x = lds_read_tr((lds_s16x4*)(lo + (uint32_t)(row0 * P * 2)));
+        const s16x4 y = lds_read_tr((lds_s16x4*)(hi + (uint32_t)((row0 + 8) * P * 2)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };

@@ -429,9 +429,11 @@ template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     constexpr int P = attn_pitch<D>(), NB = D / 32, NS = D / 16, STEP = attn_back_step<D>();
     constexpr bool PARKED = D > 64;
-    __shared__ __attribute__((aligned(256))) uint16_t smem[4 * STEP * P + (PARKED ? kAttnRows * P : 0)];
+    constexpr int TILES = 4 * STEP * P + (PARKED ? kAttnRows * P : 0);
+    // (one array: with two the compiler tells their loads apart, and waits again, for all in flight, ahead of the reads of each)
+    __shared__ __attribute__((aligned(256))) uint16_t smem[TILES + 2 * 2 * 64 * 2];
     uint16_t* const parked = smem + 4 * STEP * P;
-    __shared__ __attribute__((aligned(16))) float stats[2][2][64];     // of a step's queries
+    float* const stats = reinterpret_cast<float*>(smem + TILES);       // [stage][offset of lse, -delta][64] of a step's queries
     const int heads_k = a.heads_q / a.group;
     int kv, t, part;
     if (!attn_place(heads_k, a.tiles, a.parts, kv, t, part)) return;
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
         gt.load(smem + (stage * 2 + 1) * STEP * P, a.dO + (int64_t)(seq.q0 + i0) * a.do_ts + (int64_t)head * a.do_hs, a.do_ts, seq.nq - i0);
         // one array of statistics by half of the waves each; rows past the last are masked, and 0 is as good as any for them
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.stats + ((int64_t)(wave & 1) * a.heads_q + head) * a.tokens_q + seq.q0 + i0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)&stats[stage][wave & 1][0], 4,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(stats + (2 * stage + (wave & 1)) * 64), 4,
                                                  i0 + lane < seq.nq ? 4 * lane : 0x80000000u, 0, 0, 0);
     };
     // queries from .. to that see the lane's key
@@ -489,7 +491,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     const float pos = (float)(j - see.shift - 4 * h);      // the distance from a register's query without its 4 h
     using Reader = TileReader<P>;
     const Reader reader(lane);
-    auto compute = [&](int i0, uint32_t tile, const float (*st)[64], const ScoreRule& rule, bool masked) {       // tile: Q's rows, dO's behind them
+    auto compute = [&](int i0, uint32_t tile, uint32_t st, const ScoreRule& rule, bool masked) {       // tile: Q's rows, dO's behind them
         const uint32_t qr = tile + reader.rows, qc = tile + reader.columns;
         uint32_t vr = tile_address(parked) + 32 * wave * P * 2 + reader.rows;
         asm volatile("" : "+v"(vr));       // (not an address per step, kept all along the loop)
@@ -498,8 +500,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
             f32x16 s, dp;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const f32x4 offset = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
-                const f32x4 delta = *reinterpret_cast<const f32x4*>(&st[1][32 * b + 8 * r + 4 * h]);
+                const f32x4 offset = lds_read4((lds_f32x4*)(st + (32 * b + 8 * r) * 4));
+                const f32x4 delta = lds_read4((lds_f32x4*)(st + (64 + 32 * b + 8 * r) * 4));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[4 * r + e] = CAP || BIAS ? 0.f : offset[e];
@@ -526,7 +528,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f32x4 offset = {0.f, 0.f, 0.f, 0.f};
-                if constexpr (CAP || BIAS) offset = *reinterpret_cast<const f32x4*>(&st[0][32 * b + 8 * r + 4 * h]);
+                if constexpr (CAP || BIAS) offset = lds_read4((lds_f32x4*)(st + (32 * b + 8 * r) * 4));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float p = s[4 * r + e], g = dp[4 * r + e];
@@ -573,6 +575,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     int member = ahead, step = ahead_step;
     if (total > begin) fetch_next(begin);
     const int last_key = min(w0 + 31, seq.nk - 1);
+    const uint32_t stats_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const float*)stats + 16 * h;
     for (int it = begin; it < total; ++it) {
         wait_loads<0>();
         lds_barrier();
@@ -584,7 +587,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
         }
         if (w0 >= seq.nk || see.hi(i1) < w0 || see.lo(i0) > last_key) continue;
         const ScoreRule rule = score_rule<CAP, BIAS>(a, now);
-        compute(i0, tile_address(smem) + (it & 1) * 4 * STEP * P, stats[it & 1], rule, see.lo(i1) > w0 || see.hi(i0) < last_key || i0 + STEP > seq.nq);
+        compute(i0, tile_address(smem) + (it & 1) * 4 * STEP * P, stats_at + (it & 1) * 2 * 64 * 4, rule, see.lo(i1) > w0 || see.hi(i0) < last_key || i0 + STEP > seq.nq);
     }
     const bool mine = j < seq.nk;
     if (a.parts > 1) {

@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
             const int chunk = 2 * b + ((col & 3) >> 1);
             const uint16_t* lo = V + r * P + ((chunk ^ tile_swizzle<P>(r)) * 8) + 4 * (col & 1);
             const uint16_t* hi = V + (r + 16) * P + ((chunk ^ tile_swizzle<P>(r + 16)) * 8) + 4 * (col & 1);
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
+            const s16x4 x = lds_read_tr((lds_s16x4*)lo);
+            const s16x4 y = lds_read_tr((lds_s16x4*)hi);
             const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
             o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[b], 0, 0, 0);
         }
