@@ -12,12 +12,14 @@
 // lacks.  So the pass for dq also forms r and the mean key k' = sum_j p_j (1 - tanh^2) k_j, takes r k' off in the end and leaves delta + r for dk:
 // a product more, from operands that are there (8192 tokens, 32 heads of 128 on 8: dq 924 -> 1020 us).
 //
-// What bounds them, by counters (4096 tokens, 16 heads, no mask; shares of the time that the matrix pipe + the vector instructions take): d = 128
-// forward 53 + 51 %, dq 63 + 47 %, dkv 57 + 35 %; d = 64 37 + 61 %, 51 + 57 %, 49 + 44 %: they hardly overlap, with two to four waves per SIMD.  LDS
-// is busy for 18 to 43 %, without bank conflicts.  Interleaving a step's exponentials with the next step's products by hand gains nothing (8192 tokens,
-// 32 heads of 128 on 8, forward: 546 -> 558 us).
-// us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 584 (0.94), backward 2133 (0.64); 32 on 32, two
-// sequences: 338 (0.87), 1235 (0.60); 32 heads of 64, one sequence: 364 (0.76), 1149 (0.60).
+// What bounds them: the matrix pipe at the clock it holds under such a load, and the operands' way to it.  Forward, 8192 tokens, 16 heads of 128, no mask: 552 us;
+// the products alone, on operands in registers, 405 (1355 TFLOP/s); with the softmax 437; with LDS reads and no softmax 466; all but the direct loads 510.
+// By counters (4096 tokens, 16 heads; matrix pipe + vector instructions, of the time): d = 128 forward 53 + 51 %, dq 63 + 47 %, dkv 57 + 35 %; d = 64
+// 37 + 61 %, 51 + 57 %, 49 + 44 %; LDS is busy for 18 to 43 %, without bank conflicts.  Gains nothing (us, 8192 tokens, 32 heads of 128 on 8, forward):
+// a step's exponentials interleaved with the next step's products by hand 546 -> 558; 64 queries per wave 559 -> 703; 8 waves and 256 queries per
+// workgroup 564 -> 565, and 35 -> 45 for sequences of 315 tokens.
+// us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 564 (0.97), backward 2062 (0.67); 32 on 32, two
+// sequences: 329 (0.90), 1195 (0.62); 32 heads of 64, one sequence: 354 (0.78), 1111 (0.62).  The vendor's product of 8192^3 on the same card: 1.2.
 #include "qg_attention.h"
 
 namespace qg {
