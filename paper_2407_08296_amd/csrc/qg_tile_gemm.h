@@ -949,7 +949,7 @@ static bool lin_small(int64_t M, int64_t N, int count) {
 // the tiles of launch_tile_gemm, us, split / not: forward, 256 tokens, 768 -> 768 (T = 192) 4.0 / 6.6, 2048 -> 2048 (512) 9.2 /
 // 13.4, 500 tokens, 1024 -> 1024 (512) 6.5 / 7.4.  From 513 to 768 of them two groups of waves (64 x 64 tiles, at most a workgroup
 // per CU) take 0.93 of the split's time on average over 22 shapes and ten lengths of the contraction from 512 to 11008: 0.78 to 0.91
-// where rows start unaligned, 256 tokens, 2048 -> 3072 (768) 12.0 / 11.2, 4096 -> 3072 22.5 / 20.5, 2000 tokens, 11008 -> 384 (756)
+// where rows start unaligned, 2000 tokens, 11008 -> 384 (756)
 // 62.7 / 52.4, 1000 tokens, 768 -> 768 the same; they lose up to 8 % at K = 2048 with some hundred ragged rows (500 tokens, 1280
 // columns (640) 11.3 / 12.2, 1000 tokens, 768 columns 11.7 / 12.2) and 2 to 4 % on ragged tiles at K = 512.  Where they do not have
 // a CU each, 32 tokens, 2048 -> 17408 (544) 12.9 / 19.9, 4096 -> 24576 (768) 24.7 / 37.0.  A weight with k
@@ -1004,8 +1004,8 @@ static unsigned lin_grid(const LinProduct& p) { return (unsigned)((p.tiles_m * p
 //    48), and beyond T = 512 128 x 128 x 32 with four workgroups per CU (4096 tokens, 2048 -> 2048 (512): 64-deep 42.5, 32-deep
 //    44; 4100 tokens (528) 62 / 55; 3000 tokens, 4096 -> 4096 (768) 132 / 125).
 //    grad_W: 128 x 256 x 32 when that fills the chip twice, 128 x 128 x 32 below, with two register sets up to T = 256
-//    (1000 tokens, 2048 x 2048: 17.1 against 18.1, 2000 x 2000 17.1 / 20.7) and where everything is whole (2048 tokens, 3072 x
-//    2048, T = 384: 37.1 / 38.7; ragged, 2000 tokens, 3000 x 3000, T = 576: 55.3 / 54.7, 3001 x 2048, T = 384: 100 / 69).
+//    (1000 tokens, 2048 x 2048: 17.1 against 18.1, 2000 x 2000 17.1 / 20.7) and where everything is whole (T = 384 at 2048 tokens:
+//    37.1 / 38.7; ragged, 2000 tokens, 3000 x 3000, T = 576: 55.3 / 54.7, 3001 x 2048, T = 384: 100 / 69).
 //  * 64 x 64 x 64, four waves of one 32 x 32 block each, where 128 x 128 tiles would leave CUs idle: a K step of a lone
 //    workgroup is a serial chain (fragments, MFMAs, commit, barrier), 1.2 us for 128 x 128 x 64 before the commit and the
 //    fetches went between the MFMAs.  64 / 128: forward, 1000 tokens, 768 -> 2048 (T = 128) 9.7 / 12.8, 256 x 4096 -> 11008
