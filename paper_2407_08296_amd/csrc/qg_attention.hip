@@ -77,14 +77,15 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     const Visible see(a, seq);
     const ScoreRule rule = score_rule<CAP, BIAS>(a, head);
     const int kv = head / a.group;
-    const uint16_t* qp = a.q + (int64_t)seq.q0 * a.q_ts + (int64_t)head * a.q_hs;
+    const uint16_t* qp = a.q + (int64_t)(seq.q0 + row0) * a.q_ts + (int64_t)head * a.q_hs;
     const uint16_t* kp = a.k + (int64_t)seq.k0 * a.k_ts + (int64_t)kv * a.k_hs;
     const uint16_t* vp = a.v + (int64_t)seq.k0 * a.v_ts + (int64_t)kv * a.v_hs;
 
     const int w0 = row0 + 32 * wave, i = w0 + (lane & 31), w1 = min(w0 + 31, seq.nq - 1);
     bf16x8 qf[NS];
+    const RowFrags qr(qp, a.q_ts, wave, lane, i < seq.nq, a.d);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = row_frag(qp, a.q_ts, i, seq.nq, s, a.d, lane);
+    for (int s = 0; s < NS; ++s) qf[s] = qr.get(s);
     const int lo = see.lo(i), hi = see.hi(i);
     // steps that some row of the workgroup sees, of them the part's; and, of the wave, those that all rows see whole
     const int first = see.lo(row0) / kAttnStep, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
@@ -263,52 +264,12 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     const uint16_t* vp = a.v + (int64_t)seq.k0 * a.v_ts + (int64_t)kv * a.v_hs;
     const int w0 = row0 + 32 * wave, i = w0 + (lane & 31), w1 = min(w0 + 31, seq.nq - 1);
     const bool mine = i < seq.nq;
-    bf16x8 qf[NS], gf[PARKED ? 1 : NS];
-    float delta = 0.f;
-    {
-        const uint16_t* qp = a.q + (int64_t)seq.q0 * a.q_ts + (int64_t)head * a.q_hs;
-        const uint16_t* gp = a.dO + (int64_t)seq.q0 * a.do_ts + (int64_t)head * a.do_hs;
-        const uint16_t* op = a.o + (int64_t)seq.q0 * a.o_ts + (int64_t)head * a.o_hs;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            qf[s] = row_frag(qp, a.q_ts, i, seq.nq, s, a.d, lane);
-            const bf16x8 g = row_frag(gp, a.do_ts, i, seq.nq, s, a.d, lane);
-            if constexpr (!PARKED) gf[s] = g;
-            const bf16x8 of = row_frag(op, a.o_ts, i, seq.nq, s, a.d, lane);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)g[e], (float)of[e], delta);
-        }
-        delta += other_half(delta);
-        if constexpr (PARKED) {
-            RowsTile<P, kAttnRows, 256> g;
-            g.init(a.do_ts, a.d);
-            g.load(parked, gp + (int64_t)row0 * a.do_ts, a.do_ts, seq.nq - row0);
-        }
-    }
-    const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
-    // a row without a visible key, or none, has p = 0: its offset is -inf
-    const float lse = mine ? a.lse[at] : -INFINITY, offset = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
-    // For dkv, which begins its products at them, in accumulators read from LDS: -delta, and the offset in terms of the product where x is linear in it
-    // (its rounding then is the one it has in the exponent too).
-    auto keep_stats = [&](float d) {
-        if (mine && h == 0) {
-            a.stats[at] = CAP || BIAS ? offset : lse == -INFINITY ? -INFINITY : -lse / a.scale;
-            a.stats[(int64_t)a.heads_q * a.tokens_q + at] = -d;
-        }
-    };
     const int lo = see.lo(i), hi = see.hi(i);
     const int first = see.lo(row0) / STEP, most = see.hi(min(row0 + kAttnRows, seq.nq) - 1);
     const int all = most < 0 ? 0 : most / STEP - first + 1;
     int begin, steps;
     attn_share(all, a.parts, part, begin, steps);
     const int wave_lo = see.lo(w0), wave_hi = w0 < seq.nq ? see.hi(w1) : -1, all_lo = see.lo(w1), all_hi = see.hi(w0);
-    f32x16 dq[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) dq[b] = zero16();
-    f32x16 mean[NB];          // of the keys, and what the row's p (dp - delta) add up to: see above
-    float rest = 0.f;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) mean[b] = zero16();
     RowsTile<P, STEP, 256> kt, vt;
     kt.init(a.k_ts, a.d);
     vt.init(a.v_ts, a.d);
@@ -317,6 +278,53 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
         kt.load(smem + stage * 2 * STEP * P, kp + (int64_t)j * a.k_ts, a.k_ts, seq.nk - j);
         vt.load(smem + (stage * 2 + 1) * STEP * P, vp + (int64_t)j * a.v_ts, a.v_ts, seq.nk - j);
     };
+    if (steps > begin) fetch(begin, begin & 1);      // (ahead of the rows' own loads, which delta waits for)
+    const int64_t at = (int64_t)head * a.tokens_q + seq.q0 + i;
+    // a row without a visible key, or none, has p = 0: its offset is -inf
+    const float lse = mine ? a.lse[at] : -INFINITY, offset = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+    bf16x8 qf[NS], gf[PARKED ? 1 : NS];
+    float delta = 0.f;
+    {
+        const uint16_t* gp = a.dO + (int64_t)(seq.q0 + row0) * a.do_ts + (int64_t)head * a.do_hs;
+        if constexpr (PARKED) {
+            RowsTile<P, kAttnRows, 256> g;
+            g.init(a.do_ts, a.d);
+            g.load(parked, gp, a.do_ts, seq.nq - row0);
+        }
+        const RowFrags qr(a.q + (int64_t)(seq.q0 + row0) * a.q_ts + (int64_t)head * a.q_hs, a.q_ts, wave, lane, mine, a.d);
+        const RowFrags gr(gp, a.do_ts, wave, lane, mine, a.d);
+        const RowFrags fr(a.o + (int64_t)(seq.q0 + row0) * a.o_ts + (int64_t)head * a.o_hs, a.o_ts, wave, lane, mine, a.d);
+        bf16x8 g[NS], f[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            qf[s] = qr.get(s);
+            g[s] = gr.get(s);
+            f[s] = fr.get(s);
+        }
+        __builtin_amdgcn_sched_barrier(0);     // (all on their way before the first is waited for)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if constexpr (!PARKED) gf[s] = g[s];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)g[s][e], (float)f[s][e], delta);
+        }
+        delta += other_half(delta);
+    }
+    // For dkv, which begins its products at them, in accumulators read from LDS: -delta, and the offset in terms of the product where x is linear in it
+    // (its rounding then is the one it has in the exponent too).
+    auto keep_stats = [&](float d) {
+        if (mine && h == 0) {
+            a.stats[at] = CAP || BIAS ? offset : lse == -INFINITY ? -INFINITY : -lse / a.scale;
+            a.stats[(int64_t)a.heads_q * a.tokens_q + at] = -d;
+        }
+    };
+    f32x16 dq[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) dq[b] = zero16();
+    f32x16 mean[NB];          // of the keys, and what the row's p (dp - delta) add up to: see above
+    float rest = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mean[b] = zero16();
     const float pos = (float)(i + see.shift - 4 * h);
     using Reader = TileReader<P>;
     const Reader reader(lane);
@@ -378,7 +386,6 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);     // (one block of scores at a time: more of them in flight spill)
         }
     };
-    if (steps > begin) fetch(begin, begin & 1);
     for (int step = begin; step < steps; ++step) {
         wait_loads<0>();
         lds_barrier();
@@ -447,17 +454,18 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     const int w0 = row0 + 32 * wave, j = w0 + (lane & 31);
     bf16x8 kf[NS], vf[PARKED ? 1 : NS];
     {
-        const uint16_t* kp = a.k + (int64_t)seq.k0 * a.k_ts + (int64_t)kv * a.k_hs;
-        const uint16_t* vp = a.v + (int64_t)seq.k0 * a.v_ts + (int64_t)kv * a.v_hs;
+        const uint16_t* kp = a.k + (int64_t)(seq.k0 + row0) * a.k_ts + (int64_t)kv * a.k_hs;
+        const uint16_t* vp = a.v + (int64_t)(seq.k0 + row0) * a.v_ts + (int64_t)kv * a.v_hs;
+        const RowFrags kr(kp, a.k_ts, wave, lane, j < seq.nk, a.d), vr(vp, a.v_ts, wave, lane, j < seq.nk, a.d);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            kf[s] = row_frag(kp, a.k_ts, j, seq.nk, s, a.d, lane);
-            if constexpr (!PARKED) vf[s] = row_frag(vp, a.v_ts, j, seq.nk, s, a.d, lane);
+            kf[s] = kr.get(s);
+            if constexpr (!PARKED) vf[s] = vr.get(s);
         }
         if constexpr (PARKED) {
             RowsTile<P, kAttnRows, 256> v;
             v.init(a.v_ts, a.d);
-            v.load(parked, vp + (int64_t)row0 * a.v_ts, a.v_ts, seq.nk - row0);
+            v.load(parked, vp, a.v_ts, seq.nk - row0);
         }
     }
     // queries that see a key of the workgroup: causal, those from the key's position on (all, if the key lies in the prefix); with a
