@@ -243,9 +243,9 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
 
 // Joins the shares of a sequence's heads in a fixed order: WAVES waves per head, of each 64 / (d / 4) shares at once, four elements per lane.
 template <int WAVES>
-__global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
-    constexpr int HEADS = 4 / WAVES;
-    __shared__ __attribute__((aligned(16))) float sums[4][128 + 4];
+__global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void k_attention_join(PagedArgs a) {
+    constexpr int HEADS = WAVES > 4 ? 1 : 4 / WAVES;
+    __shared__ __attribute__((aligned(16))) float sums[HEADS * WAVES][128 + 4];
     const int heads = a.heads_k * a.group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % WAVES;
     const int64_t unit = min((int64_t)blockIdx.x * HEADS + wave / WAVES, (int64_t)a.sequences * heads - 1);
     const int seq = (int)(unit / heads), h = (int)(unit - (int64_t)seq * heads);
@@ -294,11 +294,15 @@ __global__ __launch_bounds__(256) void k_attention_join(PagedArgs a) {
 }
 
 // Positions of a workgroup: 512, and 256 where that leaves fewer than 512 workgroups (us with 256 / 512 / 1024: 128 sequences of up to 1000, 8 heads
-// on one: 14.7 / 16.4 / 16.4; one of 32768, 8 key heads of 128: 35.1 / 34.2 / 34.0; 64 of up to 4096, 16 of 64: - / 37.1 / 39.5; 8 of up to 8000, 32 of
-// 128: - / 136 / 138).
+// on one: 14.7 / 16.4 / 16.4; 64 of up to 4096, 16 of 64: - / 37.1 / 39.5; 8 of up to 8000, 32 of 128: - / 136 / 138).  One sequence's parts are all
+// of one length: as many as fill the chip's 512 places in as few whole rounds as parts of at most 512 make (us with the rule for several / this
+// one: 20000 positions, 8 key heads of 128: 24.0 / 22.3; 36000: 41.6 / 36.8; 100000, two: 33.4 / 29.4; 200000, one: 38.6 / 30.9; parts of up to 1024: 50000,
+// eight, 53.4 -> 49.0, but 100000, 8 of 64, 49.9 -> 55.9.  10 sequences of up to 10000, two: 15.7 / 19.1).
 static int part_length(const qg_cache* c, int heads_q) {
-    const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16);
-    return units * c->width * c->page_size < 512 * 512 ? 256 : 512;
+    const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16), all = units * c->width * c->page_size;
+    if (c->sequences > 1) return all < 512 * 512 ? 256 : 512;
+    const int64_t rounds = (all + 512 * 512 - 1) / (512 * 512), fit = (all + 512 * rounds - 1) / (512 * rounds);
+    return fit <= 256 ? 256 : (int)((fit + 4 * kPagedStep - 1) / (4 * kPagedStep) * (4 * kPagedStep));
 }
 static int64_t most_parts(const qg_cache* c, int heads_q) {
     const int length = part_length(c, heads_q);
@@ -357,7 +361,9 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     auto with_bias = [&](auto cp) { slopes != nullptr ? with_d(cp, std::true_type()) : with_d(cp, std::false_type()); };
     cap > 0.f ? with_bias(std::true_type()) : with_bias(std::false_type());
     const int64_t heads = (int64_t)a.sequences * heads_q;
-    if (a.shares > 16) hipLaunchKernelGGL(k_attention_join<4>, dim3((unsigned)heads), dim3(256), 0, (hipStream_t)stream, a);
+    // (one wave, four, sixteen per head; 100000 positions, 16 heads on two, 390 shares: four 35.7, sixteen 33.4)
+    if (a.shares > 64) hipLaunchKernelGGL(k_attention_join<16>, dim3((unsigned)heads), dim3(1024), 0, (hipStream_t)stream, a);
+    else if (a.shares > 16) hipLaunchKernelGGL(k_attention_join<4>, dim3((unsigned)heads), dim3(256), 0, (hipStream_t)stream, a);
     else if (a.shares > 1) hipLaunchKernelGGL(k_attention_join<1>, dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
     return check_launch();
 }

@@ -181,7 +181,8 @@ def test_paged_lengths(n):
 
 
 # (lengths, heads, heads_k, d, page): one share of a sequence, a few, many (joined by four waves per head)
-SHARES = [([100], 4, 2, 64, 16), ([700, 5], 4, 2, 64, 16), ([9000], 4, 2, 64, 16), ([9000, 0, 4000], 3, 1, 128, 100), ([6000], 2, 2, 40, 7)]
+SHARES = [([100], 4, 2, 64, 16), ([700, 5], 4, 2, 64, 16), ([9000], 4, 2, 64, 16), ([9000, 0, 4000], 3, 1, 128, 100), ([6000], 2, 2, 40, 7),
+          ([23000], 8, 8, 64, 16), ([20000], 2, 1, 128, 32), ([70000], 4, 4, 64, 64)]      # one sequence: parts of 384; 79 and 183 shares
 
 
 @pytest.mark.parametrize("lengths,heads,heads_k,d,page", SHARES)
