@@ -217,7 +217,7 @@ def test_every_kernel_is_launched_by_a_test(launches):
         calls += [(name, *s) for s in sizes]
     calls += [("rope", 7, 12, 12, 64, 64, layout, 1) for layout in (0, 1)]
     calls += [("paged", len(s[0]), s[1], s[2], s[3], s[4], -(-max(s[0]) // s[4]), 0) for s in more.SHARES]
-    calls += [("paged", 5, 4, 2, d, 16, 83, f) for d in (64, 128) for f in (0, 2, 4, 6)]
+    calls += [("paged", 5, 4, 2, d, 16, 83, f) for d in (64, 96, 128) for f in (0, 2, 4, 6)]
     held, *got = launches(calls)
     assert all(status == 0 for status, _ in got)
     launched = {k[0] for _, one in got for k in one}

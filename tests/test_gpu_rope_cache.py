@@ -213,13 +213,13 @@ def test_paged_page_sizes(page):
     run_paged([700, 5, 0, 64, 333], 4, 2, 64, page, seed=page)
 
 
-@pytest.mark.parametrize("heads,heads_k,d", [(1, 1, 8), (3, 3, 40), (16, 1, 64), (17, 1, 64), (40, 2, 72), (32, 8, 128), (8, 2, 120), (6, 6, 128)])
+@pytest.mark.parametrize("heads,heads_k,d", [(1, 1, 8), (3, 3, 40), (16, 1, 64), (17, 1, 64), (40, 2, 72), (12, 4, 88), (4, 4, 104), (32, 8, 128), (8, 2, 120), (6, 6, 128)])
 def test_paged_heads(heads, heads_k, d):
     run_paged([200, 33], heads, heads_k, d, 16, seed=heads)
 
 
 @pytest.mark.parametrize("how", [dict(cap=6.0), dict(slopes=True), dict(window=1), dict(window=50), dict(window=600, cap=5.0, slopes=True), dict(window=10 ** 6), dict(scale=1.0)])
-@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("d", [64, 96, 128])
 def test_paged_scores(how, d):
     how = dict(how, slopes=torch.tensor([0.5, 0.1, 0.02, 0.0], device=DEV)) if how.get("slopes") else how
     run_paged([1300, 49, 50, 51, 1], 4, 2, d, 16, seed=9, **how)
