@@ -700,12 +700,13 @@ static int attn_parts(int64_t parts, int64_t steps, int least) {
 // Keys: whole parts of 512 workgroups (us without / with; 2048 queries, 8 heads of 128 on one key head: forward 41 / 31; 4096, one head of 64: 56 / 22,
 // backward 196 / 70; but 2000, 24 heads, 432 tiles, in two parts: 27 / 34).  Queries: 1024 workgroups or more, since a causal mask gives
 // the first keys most of the work (us in one part / by the rule / for 2048: 8192 tokens, 32 heads on 8 of 128: backward 3140 / 2270 / 2230; 4096, 16 on
-// 4, four sequences: 343 / 184 / 207; 4096, 32 on 32 without a mask, 1088 tiles: 1092 / 1091 / 1225), of four steps or more; of two where the
+// 4, four sequences: 343 / 184 / 207; 4096, 32 on 32 without a mask, 1088 tiles: 1092 / 1091 / 1225), of 16 steps or more (backward with four / 16 / 24: 8 sequences
+// of 512, 12 heads of 64: 58 / 39 / -; 4 of 1024, 16 of 64: 86 / 67 / 67; 16 on 4 of 128: 145 / 134 / 164); of two where the
 // parts are few all the same (2000, 4 on 1, ten sequences: 32 / 29).
 static AttnParts attn_parts(const qg_attention* a) {
     const int64_t work_q = attn_tiles(a->tokens_q, a->sequences) * a->heads_q, work_k = attn_tiles(a->tokens_k, a->sequences) * a->heads_k;
     const int keys = attn_parts(512 / work_q, a->tokens_k / a->sequences / 64, 4);
-    return {keys, keys, attn_parts((1024 + work_k - 1) / work_k, a->tokens_q / a->sequences * (a->heads_q / a->heads_k) / 64, work_k < 128 ? 2 : 4)};
+    return {keys, keys, attn_parts((1024 + work_k - 1) / work_k, a->tokens_q / a->sequences * (a->heads_q / a->heads_k) / 64, work_k < 128 ? 2 : 16)};
 }
 // Floats of the parts' sums.
 static int64_t forward_floats(const qg_attention* a, int parts) { return parts > 1 ? (int64_t)parts * a->heads_q * a->tokens_q * (a->d + 2) : 0; }

@@ -107,7 +107,7 @@ def slopes_of(heads):
 
 # (tokens, tokens_k, heads, heads_k, d, sequences, flags: 1 causal, 2 cap, 4 slopes): calls that the host cuts into parts, and every kernel
 PARTS = [(2048, 2048, 2, 1, 128, 1, 1), (16, 3000, 2, 2, 64, 1, 1), (1, 3000, 1, 1, 80, 1, 1), (700, 700, 3, 1, 96, 1, 0), (3000, 40, 2, 1, 64, 1, 0), (1500, 1500, 1, 1, 72, 1, 7),
-         (1200, 1200, 6, 1, 128, 1, 3)]
+         (1200, 1200, 6, 1, 128, 1, 3), (2100, 2100, 8, 8, 64, 1, 1)]
 KERNELS = [(150, 150, 2, 1, d, 1, f) for d in (64, 96, 128) for f in (1, 3, 5, 7)]
 
 
