@@ -6,8 +6,8 @@
 // its own, so that nothing waits for another wave before the end.
 //   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
 // transposed.  Scores are [position][head]; register i of block b is position 16 b + 4 (l / 16) + i, the order in which V is read then.
-// us and what that is of a large copy's rate (4.9 TB/s): one sequence of 32768, 8 key heads of 128, 28.5 + 4.1 for the join (4.1 TB/s, 96 % without it); 8 of up
-// to 8000, 32 key heads of 128, 88 (4.9 TB/s); 64 of up to 4096, 16 of 64, capped, windowed, 33 + 4.5 (3.3 TB/s).
+// us and what that is of a large copy's rate (4.9 TB/s): one sequence of 32768, 8 key heads of 128, 30 + 4.4 for the join (91 % without it); 8 of up
+// to 8000, 32 key heads of 128, 87 (5.0 TB/s with the join); 64 of up to 4096, 16 of 64, capped, windowed, 35 + 4.1 (74 % without it).
 #include "qg_attention.h"
 
 namespace qg {
