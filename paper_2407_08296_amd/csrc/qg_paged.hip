@@ -309,10 +309,11 @@ static int64_t most_parts(const qg_cache* c, int heads_q) {
     return ((int64_t)c->width * c->page_size + kPagedStep - 1 + length - 1) / length;
 }
 // Workgroups per sequence and key head: all parts, but no more than make 8192 in all (a table is as wide as the longest sequence may get: 64 sequences of
-// 1000 positions, 8 key heads, in a table for 131072, one workgroup for each part 143 us, of which most had nothing to do).
+// 1000 positions, 8 key heads, in a table for 131072, one workgroup for each part 143 us, of which most had nothing to do; 200 of up to 1000, 32 key heads, one workgroup for both parts 54.5, two and their
+// join 63.6; with 4096 in all 128 of up to 4096, 16 key heads, 53.6 -> 63.4).
 static int64_t most_shares(const qg_cache* c, int heads_q) {
     const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16), parts = most_parts(c, heads_q);
-    const int64_t shares = (8192 + units - 1) / units;
+    const int64_t shares = units < 8192 ? 8192 / units : 1;
     return shares < parts ? shares : parts;
 }
 

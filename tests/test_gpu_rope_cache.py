@@ -193,7 +193,7 @@ def test_paged_shares(lengths, heads, heads_k, d, page, window):
 
 @pytest.mark.parametrize("d", [64, 128])
 def test_paged_more_parts_than_workgroups(d):
-    """700 sequences, 4 key heads: three workgroups each take a long sequence's eight parts in turn; a table far wider than most need."""
+    """700 sequences, 4 key heads: two workgroups each take a long sequence's eight parts in turn; a table far wider than most need."""
     lengths = [4000 if i in (0, 350, 699) else i % 40 for i in range(700)]
     page, width = 16, 400
     pages = sum(-(-n // page) for n in lengths)
