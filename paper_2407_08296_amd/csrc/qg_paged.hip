@@ -7,7 +7,7 @@
 //   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
 // transposed.  Scores are [position][head]; register i of block b is position 16 b + 4 (l / 16) + i, the order in which V is read then.
 // us and what that is of a large copy's rate (4.9 TB/s): one sequence of 32768, 8 key heads of 128, 30 + 4.4 for the join (91 % without it); 8 of up
-// to 8000, 32 key heads of 128, 87 (5.0 TB/s with the join); 64 of up to 4096, 16 of 64, capped, windowed, 35 + 4.1 (74 % without it).
+// to 8000, 32 key heads of 128, 87 (5.0 TB/s with the join); 64 of up to 4096, 16 of 64, capped, windowed, 33 + 4.1 (79 % without it).
 #include "qg_attention.h"
 
 namespace qg {
@@ -47,8 +47,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     const int groups = (a.group + 15) / 16, units = a.sequences * a.heads_k * groups;
     const int part0 = blockIdx.x / units, at = blockIdx.x - part0 * units;
     // ... and of every eight units another to each XCD from one part and eight to the next: with heads of 64 an XCD that always had the same one read
-    // every eighth 128-byte line, from few channels of its L2 (one of 130000, 8 heads: 64 us against 57)
-    const int unit = (at | 7) < units ? (at & ~7) | ((at + (at >> 3) + part0) & 7) : at;
+    // every eighth 128-byte line, from few channels of its L2 (one of 130000, 8 heads: 64 us against 57).  The eights take turns from part to part too: an
+    // XCD's workgroups go to its four engines in turn, and a long sequence among four (sixteen) short ones would have one engine of each
+    // (4 of up to 30000, 8 key heads of 128: 64 us against 35; 16 of up to 16000: 75 / 59; 64 of up to 4096, 16 of 64: 38.6 / 36.3)
+    int unit = at;
+    if ((at | 7) < units) {
+        const int eight = ((at >> 3) + (units == 16 ? part0 >> 1 : part0)) % (units >> 3);     // (16: two eights come around in four parts)
+        unit = 8 * eight + ((at + eight + part0) & 7);
+    }
     const int hg = unit % groups, kv = unit / groups % a.heads_k, seq = unit / groups / a.heads_k;
     int first, end;
     paged_range(a, seq, first, end);
