@@ -451,7 +451,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  * qg_attention_backward: dq, dk, dv from do, the forward pass's inputs and its o and lse (delta = sum do o from o as
  *   stored, corrected by what the sum of the scores' gradients over a row, which is 0, then comes to).  Sums of the heads that
  *   share k and v, and over tokens, are added in a fixed order.  Slopes have no gradient.
- *   d: a multiple of 8 up to 128.  scale from 2^-60 to 2^60.  No output may overlap an input.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
+ *   d: a multiple of 8 up to 128.  scale, and a cap that is not 0, from 2^-60 to 2^60.  No output may overlap an input.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
  *   workspace: qg_attention_forward_workspace_bytes(a) or qg_attention_backward_workspace_bytes(a) bytes, 16-byte aligned; NULL where that is 0;
  *   calls that may run at the same time need one each.
  *
@@ -464,7 +464,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  *   nothing is turned (freqs NULL).  Tokens of one call need places of
  *   their own: one that two of them share ends up with pieces of both.
  * qg_attention_paged: one new token per sequence: o = softmax over positions 0 .. lengths[s] - 1 of the cache, the query standing
- *   at lengths[s] - 1; scores, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  What the
+ *   at lengths[s] - 1; scores, scale, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  What the
  *   cache holds outside the visible positions is not looked at.  workspace: qg_attention_paged_workspace_bytes(c, heads_q) bytes, 16-byte
  *   aligned; calls that may run at the same time need one each. */
 typedef struct {

@@ -24,6 +24,10 @@ constexpr int64_t kHeadsMaxStride = int64_t(1) << 23;   // elements between toke
 
 int check_heads(const qg_heads* x, bool required);      // host, qg_attention.hip
 int check_cache(const qg_cache* c);                     // host, qg_rope.hip
+// Scale and cap such that their quotient, and its products with a score, are numbers of fp32 (a cap of 10^-40 made a score of 0 NaN).
+inline bool check_scores(float scale, float cap) {
+    return scale >= 0x1p-60f && scale <= 0x1p60f && (cap == 0.f || (cap >= 0x1p-60f && cap <= 0x1p60f));
+}
 
 struct AttnArgs {
     int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs, do_ts, do_hs, dq_ts, dq_hs, dk_ts, dk_hs, dv_ts, dv_hs;   // strides, elements
@@ -228,20 +232,38 @@ __device__ __forceinline__ f32x16 zero16() {
 // Index of accumulator register v's row within its block of 32.
 __device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v >> 2) + (v & 3); }
 
-// A score times log2(e): from the product s, c = scale log2(e) (capped: scale / cap, factor = 1 - tanh^2).
+// tanh(s c) of a product s, c = scale / cap:  |tanh y| = (1 - e) / (1 + e), e = exp(-2 |y|), off by some 2^-21 of it and by what the exponential's last
+// place makes, 2^-24, which the cap multiplies and which is all there is near 0.  Up to a cap of kFarCap that is 2^-18 of a score at most.  FAR: up to
+// |y| = 1/8 the series y - y^3 / 3 + 2 y^5 / 15 (its next term is 2^-22 of it), so that a score is off by 2^-20 of itself whatever its cap.
+constexpr float kFarCap = 64.f;
+template <bool FAR>
+__device__ __forceinline__ float score_tanh(float s, float c) {
+    const float y = s * (c * (2.f * kLog2e)), e = __builtin_amdgcn_exp2f(-fabsf(y));
+    float t = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
+    if constexpr (FAR) {
+        constexpr float k = 0.5f / kLog2e, k3 = -k * k * k / 3.f, k5 = k * k * k * k * k * (2.f / 15.f), most = 0.125f / k;
+        const float z = y * y, near = y * __builtin_fmaf(z, __builtin_fmaf(z, k5, k3), k);
+        t = z < most * most ? near : t;
+    }
+    return t;
+}
+// Blocks of products become tanh's, in one branch that a call takes always or never (us by the branch, cap 30 / cap 1000 / the far form always; 8192 tokens, 32
+// heads of 64: forward 567 / 711 / 761, backward 1623 / 1865 / 1937; 32 of 128 on 8: 773 / 892 / 881, 2507 / 2734 / 2749).  The exponentials stay outside:
+// with them in the branch the backward passes of d = 128 spill, 2507 -> 2740.
+template <typename... BLOCKS>
+__device__ __forceinline__ void cap_scores(float cap, float c, BLOCKS&... s) {
+    auto each = [&](auto far, f32x16& x) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = score_tanh<far.value>(x[v], c);
+    };
+    if (cap > kFarCap) (each(std::true_type(), s), ...);
+    else (each(std::false_type(), s), ...);
+}
+// A score times log2(e): from the product s, c = scale log2(e); capped: from s = tanh, factor = 1 - tanh^2.
 template <bool CAP>
 __device__ __forceinline__ float score_log2(float s, float c, float cap_log2e, float& factor) {
-    if constexpr (!CAP) {
-        factor = 1.f;
-        return s * c;
-    } else {
-        // |tanh y| = (1 - e) / (1 + e), e = exp(-2 |y|).  Near 0 off by half the exponential's rounding, 2^-25, which the cap multiplies (1 - 2 /
-        // (exp(2 y) + 1): six times that; a series for small y: none of it, but kernels a third longer).
-        const float y = s * (c * (2.f * kLog2e)), e = __builtin_amdgcn_exp2f(-fabsf(y));
-        const float t = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
-        factor = __builtin_fmaf(-t, t, 1.f);
-        return cap_log2e * t;
-    }
+    factor = CAP ? __builtin_fmaf(-s, s, 1.f) : 1.f;
+    return CAP ? cap_log2e * s : s * c;
 }
 
 // Columns of a transposed result (acc[b]: elements 32 b .. 32 b + 31 of a row of d, the row being this lane's column): 16-byte pieces.

@@ -125,6 +125,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
         float top = -INFINITY;
         if constexpr (kScaled) {
             const float away = pos - (float)j0;
+            if constexpr (CAP) cap_scores(a.cap, rule.c, s[0], s[1]);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(256) void k_attention_fwd_join(AttnArgs a) {
     *reinterpret_cast<u32x2*>(a.o + (int64_t)token * a.o_ts + (int64_t)head * a.o_hs + e) = w;
 }
 
-// s, a product, becomes p = exp2(x - lse), the exponent being s c + offset where x is linear in it and x + offset else; dp, less delta, becomes p (dp -
+// s, a product (capped: its tanh), becomes p = exp2(x - lse), the exponent being s c + offset where x is linear in it and x + offset else; dp, less delta, becomes p (dp -
 // delta).  Returns what that is multiplied by for the gradient of scale q.k (1 - tanh^2, or 1).
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ float score_gradient(float& s, float& dp, const ScoreRule& rule, float offset, float distance) {
@@ -353,6 +354,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
             __builtin_amdgcn_s_setprio(0);
             f32x16 factor;
             const float away = pos - (float)j0;
+            if constexpr (CAP) cap_scores(a.cap, rule.c, s);
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 float p = s[v], g = dp[v] - delta;
@@ -535,6 +537,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
                 });
             __builtin_amdgcn_s_setprio(0);
             const float away = (float)i0 - pos;
+            if constexpr (CAP) cap_scores(a.cap, rule.c, s);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f32x4 offset = {0.f, 0.f, 0.f, 0.f};
@@ -649,7 +652,7 @@ static int check_attention(const qg_attention* a) {
     if (a->heads_q <= 0 || a->heads_k <= 0 || a->heads_q % a->heads_k != 0 || a->heads_q > kAttnMaxHeads) return QG_ERR_SHAPE;
     if (a->d <= 0 || a->d > 128 || a->d % 8 != 0 || a->sequences <= 0 || a->sequences > kAttnMaxSequences) return QG_ERR_SHAPE;
     if (a->cu_k == nullptr && a->cu_q != nullptr && a->tokens_q != a->tokens_k) return QG_ERR_SHAPE;
-    if (!(a->scale >= 0x1p-60f && a->scale <= 0x1p60f) || !(a->cap >= 0.f && a->cap < INFINITY)) return QG_ERR_SHAPE;
+    if (!check_scores(a->scale, a->cap)) return QG_ERR_SHAPE;
     if (a->window < 0 || (!a->causal && (a->window > 0 || a->prefix != nullptr)) || (a->window > 0 && a->prefix != nullptr)) return QG_ERR_SHAPE;
     for (const void* p : {(const void*)a->cu_q, (const void*)a->cu_k, (const void*)a->prefix, (const void*)a->slopes})
         if (reinterpret_cast<uintptr_t>(p) & 3) return QG_ERR_ALIGN;

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
             for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[b][k], qf[k], s[b], 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float unused, x = score_log2<CAP>(s[b][i], c2, cap2, unused);
+                float unused, x = score_log2<CAP>(CAP ? score_tanh<true>(s[b][i], c2) : s[b][i], c2, cap2, unused);
                 const int r = 16 * b + 4 * g + i;
                 if constexpr (BIAS) x = __builtin_fmaf(-slope, (float)(end - 1 - (j0 + r)), x);
                 s[b][i] = there >> r & 1 ? x : -INFINITY;
@@ -345,7 +345,7 @@ extern "C" int qg_attention_paged(const qg_cache* c, const int32_t* lengths, con
     if (lengths == nullptr) return QG_ERR_NULL;
     for (const qg_heads* x : {q, o})
         if (int e = check_heads(x, true)) return e;
-    if (!(scale > 0.f && scale < INFINITY) || !(cap >= 0.f && cap < INFINITY) || window < 0) return QG_ERR_SHAPE;
+    if (!check_scores(scale, cap) || window < 0) return QG_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(lengths) & 3) || (reinterpret_cast<uintptr_t>(slopes) & 3) || !aligned16(workspace)) return QG_ERR_ALIGN;
     if (workspace == nullptr || workspace_bytes < qg_attention_paged_workspace_bytes(c, heads_q)) return QG_ERR_WORKSPACE;
     PagedArgs a = {};
