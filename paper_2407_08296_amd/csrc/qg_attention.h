@@ -62,6 +62,7 @@ __device__ __forceinline__ int attn_boundary(const int32_t* cu, int i, int seque
 // turn's lanes hold the sequence's own boundaries.  (Loading them again, and rows by loads with a branch each: 16 sequences of 256 tokens, 16 heads of 64,
 // forward 13.2 -> 13.6 us, backward 39.6 -> 42.4.)
 // KEYS: the rows are keys.  The rows behind the last sequence have no partners.
+// Boundaries that descend can give a tile ahead of its sequence, of a negative number: it has no rows (as rows they would be those of other sequences).
 template <int BM, bool KEYS>
 __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, int t) {
     const int lane = threadIdx.x & 63;

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd(AttnArgs a) {
     if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, false>(a, a.tiles - 1 - t);   // late tiles first: with a causal mask they have most keys
     const int row0 = seq.tile * kAttnRows;
-    if (row0 >= seq.nq) return;
+    if (row0 < 0 || row0 >= seq.nq) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const Visible see(a, seq);
     const ScoreRule rule = score_rule<CAP, BIAS>(a, head);
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttnArgs a) {
     if (!attn_place(a.heads_q, a.tiles, a.parts, head, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, false>(a, a.tiles - 1 - t);
     const int row0 = seq.tile * kAttnRows;
-    if (row0 >= seq.nq) return;
+    if (row0 < 0 || row0 >= seq.nq) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const Visible see(a, seq);
     const ScoreRule rule = score_rule<CAP, BIAS>(a, head);
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttnArgs a) {
     if (!attn_place(heads_k, a.tiles, a.parts, kv, t, part)) return;
     const AttnTile seq = attn_tile<kAttnRows, true>(a, t);        // early tiles first: with a causal mask they have most queries
     const int row0 = seq.tile * kAttnRows;
-    if (row0 >= seq.nk) return;
+    if (row0 < 0 || row0 >= seq.nk) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const Visible see(a, seq);
     const int w0 = row0 + 32 * wave, j = w0 + (lane & 31);
