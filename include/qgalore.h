@@ -432,7 +432,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  *     amplitude * (a cos t - b sin t, a sin t + b cos t),   t = positions[token] * freqs[pair];
  *   QG_ROPE_HALF: pair i is elements (i, i + rot/2), QG_ROPE_INTERLEAVED: (2i, 2i + 1); elements from rot on are copied.  rot is even, 2 <= rot <= d;
  *   1 <= d <= 1024; positions int64, freqs double [rot/2] (device).  Angles are formed in 64 bits.  An output may be its input,
- *   and overlap none otherwise.  tokens below 2^24, heads up to 1024.
+ *   and overlap neither an input nor an output otherwise.  tokens below 2^24, heads up to 1024.
  * qg_rope_backward: its gradients, turned back: dq and dk from those of the outputs (the same call with -t).
  * qg_rope_frequencies (HOST ONLY, `out` is a host pointer to rot/2 doubles): base^(-2i/rot); with a factor other than 1 stretched to longer
  *   contexts: frequencies that turn at most `low` times over `context` positions are divided by factor, those that turn at least `high`
@@ -451,7 +451,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  * qg_attention_backward: dq, dk, dv from do, the forward pass's inputs and its o and lse (delta = sum do o from o as
  *   stored, corrected by what the sum of the scores' gradients over a row, which is 0, then comes to).  Sums of the heads that
  *   share k and v, and over tokens, are added in a fixed order.  Slopes have no gradient.
- *   d: a multiple of 8 up to 128.  scale, and a cap that is not 0, from 2^-60 to 2^60.  No output may overlap an input.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
+ *   d: a multiple of 8 up to 128.  scale, and a cap that is not 0, from 2^-60 to 2^60.  No output may overlap an input or another output.  tokens below 2^24, heads up to 1024, sequences up to 2^20, tokens * heads below 2^30, sequences * heads below 2^23.
  *   workspace: qg_attention_forward_workspace_bytes(a) or qg_attention_backward_workspace_bytes(a) bytes, 16-byte aligned; NULL where that is 0;
  *   calls that may run at the same time need one each.
  *
@@ -462,9 +462,11 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  * qg_cache_append: k and v of `tokens` tokens to their place: token t belongs to sequence[t] (NULL: t) and stands at positions[t]; one without
  *   a place is left out.  k is turned as by qg_rope_forward on its way, and so is q (NULL, with heads_q = 0: none) to q_out (may be q); rot 0:
  *   nothing is turned (freqs NULL).  Tokens of one call need places of
- *   their own: one that two of them share ends up with pieces of both.
+ *   their own: one that two of them share ends up with pieces of both.  The pages of k and v, and q_out, may not overlap each other, and no place that
+ *   is written may hold an input of the call (but q_out q).
  * qg_attention_paged: one new token per sequence: o = softmax over positions 0 .. lengths[s] - 1 of the cache, the query standing
- *   at lengths[s] - 1; scores, scale, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  What the
+ *   at lengths[s] - 1; scores, scale, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  o may be q, and
+ *   overlap no input otherwise.  What the
  *   cache holds outside the visible positions is not looked at.  workspace: qg_attention_paged_workspace_bytes(c, heads_q) bytes, 16-byte
  *   aligned; calls that may run at the same time need one each. */
 typedef struct {

@@ -788,13 +788,76 @@ def _heads(t: torch.Tensor | None):
 
 
 def _written(t: torch.Tensor | None, like: torch.Tensor, what: str) -> torch.Tensor:
-    """Where an output of like's shape goes: t, or a new tensor.  An expanded tensor has no place for every element."""
+    """Where an output of like's shape goes: t, or a new tensor.  An expanded tensor has no place for every element, nor has a view whose heads overlap."""
     if t is None:
         return like.new_empty(*like.shape)      # (sizes as arguments: 1.5 us, as a torch.Size 2.6)
-    _expect(t, *like.shape)
-    if 0 in t.stride() and any(st == 0 and n > 1 for st, n in zip(t.stride(), t.shape)):
+    T, H, d = shape = like.shape
+    if t.shape != shape:
+        raise QGError(f"shape {tuple(t.shape)}, expected {tuple(shape)}")
+    ts, hs, _ = t.stride()
+    if hs >= d and ts >= (H - 1) * hs + d:          # (any slice of a layer's output)
+        return t
+    if ts == 0 and T > 1 or hs == 0 and H > 1:
         raise QGError(f"{what}: an expanded tensor cannot be written")
+    if not (hs >= (T - 1) * ts + d and ts >= d) and _meet(0, T, T, H, H, d, ts, hs, hs, itself=True):
+        raise QGError(f"{what}: a tensor whose elements overlap cannot be written")
     return t
+
+
+def _meet(D: int, T: int, U: int, H: int, K: int, d: int, ts: int, hs: int, ks: int, itself: bool = False) -> bool:
+    """Whether some t ts + h hs and D + u ts + k ks, t < T, h < H, u < U, k < K, are less than d apart (itself: other than at t = u, h = k)."""
+    heads = [(m * hs, m == 0) for m in range(1 - K, H)] if hs == ks else [(h * hs - k * ks, False) for h in range(H) for k in range(K)]
+    for apart, same in heads:
+        r = D - apart                           # (t - u) ts is to be nearer than d to this
+        for n in (r // ts, r // ts + 1) if ts else (0,):
+            if -U < n < T and abs(n * ts - r) < d and not (itself and same and n == 0):
+                return True
+    return False
+
+
+def _span(t: torch.Tensor):
+    """Where a [tokens][heads][d] tensor of 16-bit elements lies: begin and end in bytes, sizes, strides."""
+    T, H, d = t.shape
+    ts, hs, _ = t.stride()
+    at = t.data_ptr()
+    return at, at + 2 * ((T - 1) * ts + (H - 1) * hs + d), T, H, d, ts, hs
+
+
+def _overlap(x, y) -> bool:
+    """Whether two such places share an element.  (Of arrays that lie in between each other: exact where they step from token to token alike, as
+    slices of one layer's output do, and taken to do so where they do not.)"""
+    if x[1] <= y[0] or y[1] <= x[0]:
+        return False
+    a, _, T, H, d, ts, hs = x
+    b, _, U, K, _, us, ks = y
+    if T == 1:
+        ts = us
+    elif U != 1 and us != ts:
+        return True
+    D = (b - a) // 2
+    width, other = (H - 1) * hs + d, (K - 1) * ks + d      # of a token
+    if ts >= width > 0 and D % ts >= width and D % ts + other <= ts:
+        return False
+    return _meet(D, T, U, H, K, d, ts, hs, ks)
+
+
+def _apart(outs, ins, places=()) -> None:
+    """Refuses outputs that share memory with each other or with an input: workgroups read what others write.  An output may be the input beside it in `places`."""
+    spans = [_span(t) for t in outs]
+    for i in range(1, len(spans)):
+        for j in range(i):
+            if _overlap(spans[i], spans[j]):
+                raise QGError("out: two outputs overlap")
+    first, last = min([x[0] for x in spans]), max([x[1] for x in spans])
+    for u in ins:
+        if u is None or u.data_ptr() >= last:       # (most inputs need no more than that: 0.1 us, and what _span takes, 0.7, for those ahead of the outputs)
+            continue
+        y = _span(u)
+        if y[1] <= first:
+            continue
+        for i, x in enumerate(spans):
+            if _overlap(x, y) and not (places and u is places[i] and x[0] == y[0] and (x[5] == y[5] or x[2] == 1) and (x[6] == y[6] or x[3] == 1)):
+                raise QGError("out: an output overlaps an input")
 
 
 def _rope_layout(layout: str) -> int:
@@ -820,6 +883,9 @@ def _rope(f, q, k, positions, freqs, layout, amplitude, out):
     _expect(freqs, rot // 2)
     q_out = _written(None if out is None else out[0], q, "out")
     k_out = None if k is None else _written(None if out is None else out[1], k, "out")
+    if out is not None:
+        in_place = q_out is q and k_out is k
+        _apart((q_out,) if k is None else (q_out, k_out), () if in_place else (q, k), (q, k))
     _check(f(_heads(q), heads_q, _heads(k), 0 if k is None else k.shape[1], _ptr(positions, _I64), _ptr(freqs, _F64), tokens, d, rot,
              _rope_layout(layout), amplitude, _heads(q_out), _heads(k_out), _stream()))
     return q_out, k_out
@@ -828,7 +894,8 @@ def _rope(f, q, k, positions, freqs, layout, amplitude, out):
 def rope_forward(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half",
                  amplitude: float = 1.0, out=None):
     """Returns (q', k'): the first 2 * len(freqs) elements of every head of q [tokens][heads][d] and k (None: only q) turned by
-    positions[token] * freqs.  positions int64, freqs float64.  out: (q', k') to write into; the inputs themselves: in place."""
+    positions[token] * freqs.  positions int64, freqs float64.  out: (q', k') to write into; the inputs themselves: in place, and nothing else that
+    overlaps them or each other."""
     return _rope(lib().qg_rope_forward, q, k, positions, freqs, layout, amplitude, out)
 
 
@@ -870,9 +937,12 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: t
                       workspace: torch.Tensor | None = None):
     """Returns (o, lse): attention of q [tokens][heads][d] over k and v [tokens_k][heads_k][d], o bf16 [tokens][heads][d], lse fp32
     [heads][tokens].  cu_q, cu_k: int32 [sequences + 1], boundaries of packed sequences (None: one sequence; cu_k None: as cu_q).
-    scale: d^-0.5 if None; cap, slopes (fp32 [heads]), window, prefix (int32 [sequences]): as in qg_attention_forward."""
+    scale: d^-0.5 if None; cap, slopes (fp32 [heads]), window, prefix (int32 [sequences]): as in qg_attention_forward.  out: where o is written, apart
+    from the inputs."""
     a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
     o = _written(out, q, "out")
+    if out is not None:
+        _apart((o,), (q, k, v))
     lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
     ws, *at = _workspace(lib().qg_attention_forward_workspace_bytes(a), q, workspace)
     _check(lib().qg_attention_forward(a, _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *at, _stream()))
@@ -884,12 +954,14 @@ def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
                        scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0,
                        prefix: torch.Tensor | None = None, out=None, workspace: torch.Tensor | None = None):
     """Returns (dq, dk, dv) of attention_forward, from its inputs and results and do, the gradient of o.  out: (dq, dk, dv) to write into
-    (slices of one gradient of the layer that gave q, k and v, say)."""
+    (slices of one gradient of the layer that gave q, k and v, say), apart from the inputs and each other."""
     a = _attention(q, k, v, cu_q, cu_k, causal, scale, cap, slopes, window, prefix)
     for t in (do, o):
         _expect(t, *q.shape)
     _expect(lse, q.shape[1], q.shape[0])
     dq, dk, dv = (_written(None if out is None else out[i], t, "out") for i, t in enumerate((q, k, v)))
+    if out is not None:
+        _apart((dq, dk, dv), (do, q, k, v, o))
     ws, *at = _workspace(lib().qg_attention_backward_workspace_bytes(a), q, workspace)
     _check(lib().qg_attention_backward(a, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse, _F32), _heads(dq),
                                        _heads(dk), _heads(dv), *at, _stream()))
@@ -908,7 +980,8 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posit
                  layout: str = "half", amplitude: float = 1.0, out: torch.Tensor | None = None):
     """Puts k and v [tokens][heads_k][d] of new tokens into the pages [pages][page_size][heads_k][d] of a cache: token t to
     position positions[t] (int64) of sequence[t] (int32; None: t), whose pages table[sequence] (int32 [sequences][width]) lists.  k is turned on its
-    way if freqs is given, and so is q, which is returned (None without q).  out: where q goes (q itself: in place)."""
+    way if freqs is given, and so is q, which is returned (None without q).  out: where q goes (q itself: in place), apart from all else.  k and v may be
+    rows of the pages, if none of them is among those written."""
     c = _cache(k_pages, v_pages, table)
     tokens = k.shape[0]
     heads, d = k_pages.shape[2:]
@@ -924,6 +997,10 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posit
     if q is not None:
         _expect(q, tokens, q.shape[1], d)
         q_out = _written(out, q, "out")
+        if out is not None:
+            _apart((q_out,), (q, k, v, k_pages.view(-1, heads, d), v_pages.view(-1, heads, d)), (q,))
+    if abs(k_pages.data_ptr() - v_pages.data_ptr()) < 2 * k_pages.numel():
+        raise QGError("k_pages and v_pages overlap")
     _check(lib().qg_cache_append(c, _heads(q), 0 if q is None else q.shape[1], _heads(k), _heads(v), _ptr(positions, _I64),
                                  _ptr(sequence, _I32), tokens, _ptr(freqs, _F64), rot, _rope_layout(layout), amplitude, _heads(q_out), _stream()))
     return q_out
@@ -933,13 +1010,15 @@ def attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
                     scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0,
                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of one new token per sequence, q [sequences][heads][d], over the first lengths[s] (int32) positions of its pages; the token is
-    the last of them.  Returns o [sequences][heads][d].  workspace: uint8, qg_attention_paged_workspace_bytes of them (allocated if None)."""
+    the last of them.  Returns o [sequences][heads][d].  out: where it is written (q itself, or apart from all inputs).  workspace: uint8, qg_attention_paged_workspace_bytes of them (allocated if None)."""
     c = _cache(k_pages, v_pages, table)
     sequences, heads, d = table.shape[0], q.shape[1], k_pages.shape[3]
     _expect(q, sequences, heads, d)
     _expect(lengths, sequences)
     _expect(slopes, heads)
     o = _written(out, q, "out")
+    if out is not None:
+        _apart((o,), (q, k_pages.view(-1, *k_pages.shape[2:]), v_pages.view(-1, *k_pages.shape[2:])), (q,))
     ws, *at = _workspace(lib().qg_attention_paged_workspace_bytes(c, heads), q, workspace)
     _check(lib().qg_attention_paged(c, _ptr(lengths, _I32), _heads(q), heads, d ** -0.5 if scale is None else scale, cap, window,
                                     _ptr(slopes, _F32), _heads(o), *at, _stream()))
