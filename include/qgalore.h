@@ -431,7 +431,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  * qg_rope_forward: the pairs (a, b) of the first `rot` elements of every head of q and k (k may be NULL, with heads_k = 0) become
  *     amplitude * (a cos t - b sin t, a sin t + b cos t),   t = positions[token] * freqs[pair];
  *   QG_ROPE_HALF: pair i is elements (i, i + rot/2), QG_ROPE_INTERLEAVED: (2i, 2i + 1); elements from rot on are copied.  rot is even, 2 <= rot <= d;
- *   1 <= d <= 1024; positions int64, freqs double [rot/2] (device).  Angles are formed in 64 bits.  An output may be its input,
+ *   1 <= d <= 1024, and where d is no multiple of 8 strides may be any and data 2-byte aligned; positions int64, freqs double [rot/2] (device).  Angles are formed in 64 bits.  An output may be its input,
  *   and overlap neither an input nor an output otherwise.  tokens below 2^24, heads up to 1024.
  * qg_rope_backward: its gradients, turned back: dq and dk from those of the outputs (the same call with -t).
  * qg_rope_frequencies (HOST ONLY, `out` is a host pointer to rot/2 doubles): base^(-2i/rot); with a factor other than 1 stretched to longer

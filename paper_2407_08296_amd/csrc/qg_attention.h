@@ -22,7 +22,7 @@ constexpr int64_t kAttnMaxTokens = int64_t(1) << 24;
 constexpr int kAttnMaxHeads = 1024, kAttnMaxSequences = 1 << 20;
 constexpr int64_t kHeadsMaxStride = int64_t(1) << 23;   // elements between tokens: 128 rows are addressed in 31 bits from one base
 
-int check_heads(const qg_heads* x, bool required);      // host, qg_attention.hip
+int check_heads(const qg_heads* x, bool required, int unit = 8);    // host, qg_attention.hip; unit: elements that address and strides are multiples of
 int check_cache(const qg_cache* c);                     // host, qg_rope.hip
 // Scale and cap such that their quotient, and its products with a score, are numbers of fp32 (a cap of 10^-40 made a score of 0 NaN).
 inline bool check_scores(float scale, float cap) {

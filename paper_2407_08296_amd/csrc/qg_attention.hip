@@ -662,11 +662,11 @@ static int check_attention(const qg_attention* a) {
     return QG_OK;
 }
 
-int check_heads(const qg_heads* x, bool required) {
+int check_heads(const qg_heads* x, bool required, int unit) {
     if (x == nullptr || x->data == nullptr) return required ? QG_ERR_NULL : QG_OK;
-    if (!aligned16(x->data)) return QG_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(x->data) % (2 * unit)) return QG_ERR_ALIGN;
     if (x->token_stride < 0 || x->head_stride < 0 || x->token_stride >= kHeadsMaxStride || x->head_stride >= (int64_t(1) << 40)) return QG_ERR_SHAPE;
-    return ((x->token_stride | x->head_stride) & 7) ? QG_ERR_ALIGN : QG_OK;
+    return (x->token_stride | x->head_stride) % unit ? QG_ERR_ALIGN : QG_OK;
 }
 
 static AttnArgs attn_args(const qg_attention* a, const qg_heads* q, const qg_heads* k, const qg_heads* v, const qg_heads* o, float* lse) {

@@ -180,10 +180,11 @@ static RopeStream rope_stream(const qg_heads* from, const qg_heads* to, int head
 static int rope(const qg_heads* q, int heads_q, const qg_heads* k, int heads_k, const int64_t* positions, const double* freqs, int64_t tokens,
                 int d, int rot, int layout, float amplitude, const qg_heads* q_out, const qg_heads* k_out, float sign, void* stream) {
     if (heads_q <= 0 || heads_q > kAttnMaxHeads || heads_k < 0 || heads_k > kAttnMaxHeads || rot < 2) return QG_ERR_SHAPE;
+    const int unit = d % 8 == 0 ? 8 : 1;       // (pieces of 16 bytes are read and written at any element)
     for (const qg_heads* x : {q, q_out})
-        if (int e = check_heads(x, true)) return e;
+        if (int e = check_heads(x, true, unit)) return e;
     for (const qg_heads* x : {k, k_out})
-        if (int e = heads_k > 0 ? check_heads(x, true) : QG_OK) return e;
+        if (int e = heads_k > 0 ? check_heads(x, true, unit) : QG_OK) return e;
     if (int e = check_rope(tokens, d, rot, layout, amplitude, positions, freqs)) return e;
     RopeArgs a = {};
     a.s[0] = rope_stream(q, q_out, heads_q, d, rot, layout);

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2407_08296_amd import qgalore as qg
-from test_abi_attention import FAKE, SHAPE, WORKSPACE, attention, cache, heads
+from test_abi_attention import ALIGN, FAKE, NULL, SHAPE, WORKSPACE, attention, cache, heads
 
 
 @pytest.fixture(scope="module")
@@ -27,3 +27,21 @@ def test_scales_and_caps(L):
     for cap in (0.0, 2.0 ** -60, 2.0 ** 60):
         for scale in (2.0 ** -60, 1.0, 2.0 ** 60):
             assert codes(cap=cap, scale=scale) == {WORKSPACE}, (cap, scale)
+
+
+def test_strides_of_rotary_heads_that_are_no_multiple_of_8(L):
+    """Any strides and any element's address for such heads, as contiguous ones have; else multiples of 8.  (What is not refused for them is refused
+    for its amplitude here.)"""
+    for f in (L.qg_rope_forward, L.qg_rope_backward):
+        def call(d, bad=None, at=0):
+            x = [heads(FAKE, 3 * d, d)] * 4
+            x[at] = x[at] if bad is None else bad
+            return f(x[0], 3, x[1], 3, FAKE, FAKE, 10, d, 2, 0, float("nan"), x[2], x[3], None)
+        for d in (2, 7, 20, 33, 100, 1023):
+            assert call(d) == SHAPE
+            for at in range(4):
+                assert call(d, heads(FAKE + 2, 3 * d + 1, d + 1), at) == SHAPE and call(d, heads(FAKE + 1, 3 * d, d), at) == ALIGN
+                assert call(d, heads(FAKE, 1 << 23, d), at) == SHAPE and call(d, heads(0), at) == NULL and call(d, heads(FAKE, -2, d), at) == SHAPE
+        for d in (8, 64, 1024):
+            for at in range(4):
+                assert call(d, heads(FAKE + 2, 3 * d, d), at) == ALIGN and call(d, heads(FAKE, 3 * d + 1, d), at) == ALIGN and call(d, heads(FAKE, 3 * d, d + 4), at) == ALIGN
