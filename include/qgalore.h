@@ -465,7 +465,7 @@ int qg_head_loss_backward(const uint16_t* x_bf16, const uint16_t* W_bf16, const 
  *   their own: one that two of them share ends up with pieces of both.  The pages of k and v, and q_out, may not overlap each other, and no place that
  *   is written may hold an input of the call (but q_out q).
  * qg_attention_paged: one new token per sequence: o = softmax over positions 0 .. lengths[s] - 1 of the cache, the query standing
- *   at lengths[s] - 1; scores, scale, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  o may be q, and
+ *   at lengths[s] - 1 (a length beyond width * page_size counts as that); scores, scale, cap, slopes and window as above; d up to 128, sequences * heads_q below 2^24.  No length (or no page): o = 0.  o may be q, and
  *   overlap no input otherwise.  What the
  *   cache holds outside the visible positions is not looked at.  workspace: qg_attention_paged_workspace_bytes(c, heads_q) bytes, 16-byte
  *   aligned; calls that may run at the same time need one each. */

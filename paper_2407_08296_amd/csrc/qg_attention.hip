@@ -14,8 +14,9 @@
 //
 // What bounds them: the matrix pipe at the clock it holds under such a load, and the operands' way to it.  Forward, 8192 tokens, 16 heads of 128, no mask: 552 us;
 // the products alone, on operands in registers, 405 (1355 TFLOP/s); with the softmax 437; with LDS reads and no softmax 466; all but the direct loads 510.
-// By counters (4096 tokens, 16 heads; matrix pipe + vector instructions, of the time): d = 128 forward 53 + 50 %, dq 66 + 49 %, dkv 54 + 34 %; d = 64
-// 36 + 60 %, 52 + 58 %, 47 + 41 %; LDS is busy for 18 to 43 %, without bank conflicts.  Gains nothing (us, 8192 tokens, 32 heads of 128 on 8, forward):
+// By counters (4096 tokens, 16 heads, no mask; matrix pipe + vector instructions, of the time): d = 128 forward 53 + 51 %, dq 67 + 50 %, dkv 54 + 33 %; d = 64
+// 36 + 59 %, 50 + 56 %, 46 + 41 %; LDS is busy for 18 to 40 %, without bank conflicts; with a cap 32 + 70 %, 45 + 69 %, 40 + 55 % and 20 + 82 %, 28 + 77 %,
+// 28 + 68 %.  Gains nothing (us, 8192 tokens, 32 heads of 128 on 8, forward):
 // a step's exponentials interleaved with the next step's products by hand 546 -> 558; 64 queries per wave 559 -> 703; 8 waves and 256 queries per
 // workgroup 564 -> 565, and 35 -> 45 for sequences of 315 tokens.
 // us (PFLOP/s by 4 and 10 d per visible pair; 8192 tokens, causal): 32 heads of 128 on 8, one sequence: forward 549 (1.0), backward 1992 (0.69); 32 on 32, two

@@ -7,7 +7,7 @@
 //   K straight into operands: lane l holds position l % 16 and 8 elements of d.  V by direct loads into LDS (rows as in qg_attention.h), read
 // transposed.  Scores are [position][head]; register i of block b is position 16 b + 4 (l / 16) + i, the order in which V is read then.
 // us and what that is of a large copy's rate (4.9 TB/s): one sequence of 32768, 8 key heads of 128, 30 + 4.4 for the join (91 % without it); 8 of up
-// to 8000, 32 key heads of 128, 87 (5.0 TB/s with the join); 64 of up to 4096, 16 of 64, capped, windowed, 33 + 4.1 (79 % without it).
+// to 8000, 32 key heads of 128, 87 (5.0 TB/s with the join); 64 of up to 4096, 16 of 64, capped, windowed, 33.5 + 4.5 (76 % without it).
 #include "qg_attention.h"
 
 namespace qg {
@@ -49,10 +49,12 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
     // ... and of every eight units another to each XCD from one part and eight to the next: with heads of 64 an XCD that always had the same one read
     // every eighth 128-byte line, from few channels of its L2 (one of 130000, 8 heads: 64 us against 57).  The eights take turns from part to part too: an
     // XCD's workgroups go to its four engines in turn, and a long sequence among four (sixteen) short ones would have one engine of each
-    // (4 of up to 30000, 8 key heads of 128: 64 us against 35; 16 of up to 16000: 75 / 59; 64 of up to 4096, 16 of 64: 38.6 / 36.3)
+    // (4 of up to 30000, 8 key heads of 128: 64 us against 35; 16 of up to 16000: 75 / 59; 64 of up to 4096, 16 of 64: 38.6 / 36.3).  Two eights would come
+    // around in step with the four parts (2 of up to 16000, 8 key heads of 128: 23.9 / 22.7; taking turns every second part with 24 and 32 units too: of
+    // 16 calls two changed by more than a hundredth, 4 of up to 30000, 8 key heads, 36.2 / 35.1, 4 of 7500 27.8 / 27.4).
     int unit = at;
     if ((at | 7) < units) {
-        const int eight = ((at >> 3) + (units == 16 ? part0 >> 1 : part0)) % (units >> 3);     // (16: two eights come around in four parts)
+        const int eight = ((at >> 3) + (units == 16 ? part0 >> 1 : part0)) % (units >> 3);
         unit = 8 * eight + ((at + eight + part0) & 7);
     }
     const int hg = unit % groups, kv = unit / groups % a.heads_k, seq = unit / groups / a.heads_k;
@@ -131,6 +133,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_paged(PagedArgs a) {
             for (int k = 0; k < NS; ++k) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[b][k], qf[k], s[b], 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                // (the far form whatever the cap: 64 of up to 4096, 16 of 64, 36.0 -> 36.8 us; a branch for the near one needs more than 128 registers, 39.1)
                 float unused, x = score_log2<CAP>(CAP ? score_tanh<true>(s[b][i], c2) : s[b][i], c2, cap2, unused);
                 const int r = 16 * b + 4 * g + i;
                 if constexpr (BIAS) x = __builtin_fmaf(-slope, (float)(end - 1 - (j0 + r)), x);
@@ -303,7 +306,10 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void k_attention_join
 // on one: 14.7 / 16.4 / 16.4; 64 of up to 4096, 16 of 64: - / 37.1 / 39.5; 8 of up to 8000, 32 of 128: - / 136 / 138).  One sequence's parts are all
 // of one length: as many as fill the chip's 512 places in as few whole rounds as parts of at most 512 make (us with the rule for several / this
 // one: 20000 positions, 8 key heads of 128: 24.0 / 22.3; 36000: 41.6 / 36.8; 100000, two: 33.4 / 29.4; 200000, one: 38.6 / 30.9; parts of up to 1024: 50000,
-// eight, 53.4 -> 49.0, but 100000, 8 of 64, 49.9 -> 55.9.  10 sequences of up to 10000, two: 15.7 / 19.1).
+// eight, 53.4 -> 49.0, but 100000, 8 of 64, 49.9 -> 55.9.  10 sequences of up to 10000, two: 15.7 / 19.1; two to four sequences by this rule, the rule
+// for several / this one: 2 of 50000, two, 28.1 / 25.0; 4 of 9000, eight, 33.5 / 31.7; 3 of 4000, 16 of 64, 16.0 / 16.4; one of 20000 and three of a tenth, eight,
+// 25.6 / 25.5).  A window may begin inside a step, so a table is taken to hold one part more than its length has; without a window that one has no work (32768
+// positions, 8 key heads, fill 512 places and launch 520: 29.3 us, 512 of them and the join for up to 64 shares 29.1).
 static int part_length(const qg_cache* c, int heads_q) {
     const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16), all = units * c->width * c->page_size;
     if (c->sequences > 1) return all < 512 * 512 ? 256 : 512;
@@ -316,7 +322,9 @@ static int64_t most_parts(const qg_cache* c, int heads_q) {
 }
 // Workgroups per sequence and key head: all parts, but no more than make 8192 in all (a table is as wide as the longest sequence may get: 64 sequences of
 // 1000 positions, 8 key heads, in a table for 131072, one workgroup for each part 143 us, of which most had nothing to do; 200 of up to 1000, 32 key heads, one workgroup for both parts 54.5, two and their
-// join 63.6; with 4096 in all 128 of up to 4096, 16 key heads, 53.6 -> 63.4).
+// join 63.6; with 4096 in all 128 of up to 4096, 16 key heads, 53.6 -> 63.4).  So beyond 4096 sequences and key heads one workgroup walks all parts, long ones
+// too: 512 / 513 sequences of 300, 8 key heads of 128, and one of 32768 among them, 370 / 503; with 65536 workgroups in all 248 / 269, but 513 and one of 4000
+// 127 -> 182, 1000 of 500 354 -> 400, 700 of up to 1000 257 -> 301.
 static int64_t most_shares(const qg_cache* c, int heads_q) {
     const int64_t units = (int64_t)c->sequences * c->heads * ((heads_q / c->heads + 15) / 16), parts = most_parts(c, heads_q);
     const int64_t shares = units < 8192 ? 8192 / units : 1;
