@@ -9,6 +9,7 @@ been built, importing a symbol from it raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 from dataclasses import dataclass
@@ -824,21 +825,21 @@ def _span(t: torch.Tensor):
 
 
 def _overlap(x, y) -> bool:
-    """Whether two such places share an element.  (Of arrays that lie in between each other: exact where they step from token to token alike, as
-    slices of one layer's output do, and taken to do so where they do not.)"""
+    """Whether two such places share an element.  Of arrays that lie in between each other: exact where they step from token to token alike, as slices of
+    one layer's output do; where they do not, unless they keep to other columns of the rows that both step by, they are taken to."""
     if x[1] <= y[0] or y[1] <= x[0]:
         return False
     a, _, T, H, d, ts, hs = x
     b, _, U, K, _, us, ks = y
+    alike = T == 1 or U == 1 or us == ts
     if T == 1:
         ts = us
-    elif U != 1 and us != ts:
-        return True
     D = (b - a) // 2
     width, other = (H - 1) * hs + d, (K - 1) * ks + d      # of a token
-    if ts >= width > 0 and D % ts >= width and D % ts + other <= ts:
+    by = ts if alike else math.gcd(ts, us)
+    if by >= width > 0 and D % by >= width and D % by + other <= by:
         return False
-    return _meet(D, T, U, H, K, d, ts, hs, ks)
+    return not alike or _meet(D, T, U, H, K, d, ts, hs, ks)
 
 
 def _apart(outs, ins, places=()) -> None:
@@ -998,7 +999,7 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posit
         _expect(q, tokens, q.shape[1], d)
         q_out = _written(out, q, "out")
         if out is not None:
-            _apart((q_out,), (q, k, v, k_pages.view(-1, heads, d), v_pages.view(-1, heads, d)), (q,))
+            _apart((q_out,), (q, k, v, k_pages.flatten(0, 1), v_pages.flatten(0, 1)), (q,))
     if abs(k_pages.data_ptr() - v_pages.data_ptr()) < 2 * k_pages.numel():
         raise QGError("k_pages and v_pages overlap")
     _check(lib().qg_cache_append(c, _heads(q), 0 if q is None else q.shape[1], _heads(k), _heads(v), _ptr(positions, _I64),
@@ -1018,7 +1019,7 @@ def attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     _expect(slopes, heads)
     o = _written(out, q, "out")
     if out is not None:
-        _apart((o,), (q, k_pages.view(-1, *k_pages.shape[2:]), v_pages.view(-1, *k_pages.shape[2:])), (q,))
+        _apart((o,), (q, k_pages.flatten(0, 1), v_pages.flatten(0, 1)), (q,))
     ws, *at = _workspace(lib().qg_attention_paged_workspace_bytes(c, heads), q, workspace)
     _check(lib().qg_attention_paged(c, _ptr(lengths, _I32), _heads(q), heads, d ** -0.5 if scale is None else scale, cap, window,
                                     _ptr(slopes, _F32), _heads(o), *at, _stream()))

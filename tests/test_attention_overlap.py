@@ -64,6 +64,7 @@ def test_slices_of_one_layers_output_lie_apart():
     qg._apart((q, k), (v, None))
     qg._apart((q, k), (q, k), (q, k))                             # in place
     qg._apart((q.view(50, 4, 64),), (q, k, v), (q,))              # the same place by another view
+    qg._apart((q[::2],), (k, k[::2], v[1::3]))                    # other columns of some of the rows
     outside = torch.empty(4, 100, 64, dtype=torch.bfloat16).transpose(0, 1)
     qg._apart((outside[:40], outside[40:]), ())                   # heads outside the tokens
     for outs, ins, places in [((q, k), (q, k), ()), ((k, q), (q[:, :2], k), (q[:, :2], k)), ((q, q), (), ()), ((q[1:],), (q[:-1],), (q[:-1],)), ((q[:, 1:],), (q[:, :3],), (q[:, :3],)),
